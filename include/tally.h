@@ -62,7 +62,10 @@ typedef enum {
   TALLY_K_ATTN_DECODE_BF16 = 7, /* one query per head over a bf16 K/V cache (native only)   */
   TALLY_K_GEMM_BF16_SMALL = 8,  /* same operator as GEMM_BF16 with 32x32 tiles, ragged edges */
   TALLY_K_GEMM_BF16_N128 = 9,   /* same operator with tiles of 256 rows x 128 columns         */
-  TALLY_K_COUNT = 10
+  TALLY_K_ATTN_PROMPT_BF16 = 10,  /* causal attention over whole prompts, packed            */
+  TALLY_K_ATTN_PREFIX_BF16 = 11,  /* one token per sequence of a batch behind a shared prefix (native only) */
+  TALLY_K_GEMV_W4_BF16 = 12,      /* products with 4-bit weights, one to sixteen vectors     */
+  TALLY_K_COUNT = 13
 } tally_kernel_id;
 
 typedef struct { uint32_t x, y, z; } tally_dim3;
@@ -117,6 +120,67 @@ typedef struct {
   uint32_t tokens, heads, dim;
 } tally_attn_decode_args;
 
+/* Causal attention over whole prompts, packed one behind the other: sequence s has the tokens
+ * cu_seqlens[s] .. cu_seqlens[s + 1] - 1 (n_seqs + 1 ascending int32 in DEVICE memory, none above
+ * total), and its token i attends to its tokens up to and including i:
+ *   out[i][h] = sum_j p_ij v[j][h / (heads / kv_heads)] / sum_j p_ij,
+ *   p_ij = exp(scale q[i][h] . k[j][h / (heads / kv_heads)]).
+ * q, out: total x heads x dim; k, v: total x kv_heads x dim; all bf16.  heads a multiple of
+ * kv_heads, dim 64 or 128; scale 0 stands for 1 / sqrt(dim), negative or not finite is refused.
+ * ld_*: elements between tokens (multiples of 8, at most 2^20, 0: dense), pointers 16-byte aligned, total at
+ * most 2^30.  Sequences may be empty.  Rows of out that belong to no sequence stay as they are;
+ * a token that a row may not attend to does not reach it, whatever it holds (NaN and
+ * infinities included).  The values of cu_seqlens are read by the kernel: entries outside [0, total] count
+ * as its ends, a sequence whose end lies before its start as empty; nothing outside the
+ * tensors is touched.
+ * Logical grid: heads x (total / 128 + n_seqs) blocks in one dimension, below 2^24; block heads x b + h owns up
+ * to 128 rows of head h of one sequence s, which has the slots b from cu_seqlens[s] / 128 + s on that its
+ * rows fill, last rows first. */
+typedef struct {
+  const uint16_t *q; const uint16_t *k; const uint16_t *v; uint16_t *out;
+  const int32_t *cu_seqlens;
+  uint32_t total, n_seqs, heads, kv_heads, dim;
+  uint32_t ld_q, ld_k, ld_v, ld_out;
+  float scale;
+} tally_attn_prompt_args;
+
+/* Single-token attention of a batch behind a shared prefix: query head h of sequence b attends to the
+ * prefix's tokens and to the first own_len[b] of its own,
+ *   out[b][h] = sum_t p_t v_t / sum_t p_t,  p_t = exp(scale q[b][h] . k_t),
+ * with k_t and v_t those of K/V head h / (heads / kv_heads).  Zeros where there is no token at all.
+ * q, out: batch x heads x dim; K, V: prefix x kv_heads x dim; Ko, Vo: batch x own_cap x kv_heads x dim; all
+ * bf16.  heads a multiple of kv_heads, dim 64 or 128.  prefix or own_cap may be 0 (their pointers
+ * are then not looked at; own_len neither without own_cap).  own_len: batch int32 in DEVICE memory; values
+ * outside [0, own_cap] count as its ends.  What lies in the caches behind own_len is not read.
+ * ld_*: elements between sequences (q, out) or tokens (prefix, own), multiples of 8, at most 2^20, 0: dense;
+ * stride_own: elements between the sequences' caches, a multiple of 8, 0: dense.  scale as above.
+ * scratch: caller-owned device memory of tally_attn_prefix_scratch_bytes() bytes, 16-byte aligned; two calls
+ * that may overlap need one each.  batch * heads at most 2^20, prefix and own_cap at most 2^28. */
+typedef struct {
+  const uint16_t *q; const uint16_t *K; const uint16_t *V; const uint16_t *Ko; const uint16_t *Vo;
+  const int32_t *own_len; uint16_t *out; void *scratch;
+  uint64_t stride_own;
+  uint32_t batch, prefix, own_cap, heads, kv_heads, dim;
+  uint32_t ld_q, ld_prefix, ld_own, ld_out;
+  float scale;
+} tally_attn_prefix_args;
+
+/* y[v][r] = sum_k x[v][k] (code[r][k] - zero[r][k / group]) scale[r][k / group], v < m <= 16, r < n.
+ * x: m x k, y: m x n, scales: bf16; codes 0 .. 15; zeros: bytes 0 .. 128, or NULL for 8 everywhere.
+ * k a multiple of 8; group 32, 64 or a multiple of 128; the last group may be short.  x finite
+ * (an infinity gives NaN).  Sums are held in fp32 and rounded once.
+ * Layout of the weights, with N = ceil(n / 16), B = ceil(k / 128), G = ceil(k / group):
+ *   W: N x B tiles of 64 x 4 words; word i of entry 16 q + r of tile (t, b) holds the codes of row 16 t + r,
+ *      columns c = 128 b + 32 i + 8 q up to c + 7: c + 2 j in bits 4 j and c + 2 j + 1 in bits 16 + 4 j;
+ *   scales, zeros: N x G x 16, entry (t, g, r) for row 16 t + r.
+ * What stands for rows and columns that do not exist does not matter.  x and W 16-byte aligned, ld_x (elements
+ * between vectors, a multiple of 8) and ld_y 0: dense, at most 2^24.
+ * Logical grid: ceil(n / 16) blocks of 16 rows. */
+typedef struct {
+  const uint16_t *x; const uint32_t *W; const uint16_t *scales; const uint8_t *zeros; uint16_t *y;
+  uint32_t m, n, k, group, ld_x, ld_y;
+} tally_gemv_w4_args;
+
 typedef struct {
   uint32_t kernel_id;        /* tally_kernel_id                                           */
   tally_dim3 grid, block;    /* LOGICAL grid and block, as the original kernel is launched */
@@ -152,6 +216,9 @@ int tally_destroy(tally_ctx *ctx); /* all jobs must have been freed */
 int tally_logical_grid(uint32_t kernel_id, const void *args, size_t args_size,
                        tally_dim3 *grid, tally_dim3 *block);
 size_t tally_attn_decode_scratch_bytes(uint32_t heads);
+/* Scratch of TALLY_K_ATTN_PREFIX_BF16; 0 for sizes that it refuses. */
+size_t tally_attn_prefix_scratch_bytes(uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t dim,
+                                       uint32_t prefix, uint32_t own_cap);
 
 /* ---- the three launch forms ------------------------------------------------------- */
 

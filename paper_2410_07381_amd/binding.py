@@ -34,7 +34,7 @@ LIB_PATH = os.path.join(_HERE, "libtally.so")
 # ---------------------------------------------------------------- enums
 K_SAXPY, K_REDUCE_SUM, K_REDUCE_FINAL, K_GEMM_BF16, K_GEMV_BF16 = 0, 1, 2, 3, 4
 K_SOFTMAX_F32, K_LAYERNORM_F32, K_ATTN_DECODE_BF16, K_GEMM_BF16_SMALL = 5, 6, 7, 8
-K_GEMM_BF16_N128 = 9
+K_GEMM_BF16_N128, K_ATTN_PROMPT_BF16, K_ATTN_PREFIX_BF16, K_GEMV_W4_BF16 = 9, 10, 11, 12
 JOB_QUEUED, JOB_RUNNING, JOB_STOPPED, JOB_COMPLETE = 0, 1, 2, 3
 OK, ERR_INVALID_ARG, ERR_BAD_STATE, ERR_HIP, ERR_NOMEM, ERR_UNSUPPORTED = 0, -1, -2, -3, -4, -5
 CFG_PTB, CFG_SLICED, CFG_NATIVE, CFG_AUTO = 0, 1, 2, 3
@@ -44,6 +44,7 @@ POLICY_TALLY, POLICY_PRIORITY_NATIVE, POLICY_NONE = 0, 1, 2
 
 EXPORTS = [
     "tally_create", "tally_destroy", "tally_logical_grid", "tally_attn_decode_scratch_bytes",
+    "tally_attn_prefix_scratch_bytes",
     "tally_launch_native", "tally_launch_sliced", "tally_launch_ptb", "tally_preempt",
     "tally_resume", "tally_progress", "tally_pump", "tally_wait", "tally_job_free",
     "tally_launch_ptb_until", "tally_resume_until", "tally_coverage", "tally_marker",
@@ -99,6 +100,29 @@ class AttnDecodeArgs(C.Structure):
     _fields_ = [("q", C.c_void_p), ("K", C.c_void_p), ("V", C.c_void_p), ("out", C.c_void_p),
                 ("scratch", C.c_void_p), ("tokens", C.c_uint32), ("heads", C.c_uint32),
                 ("dim", C.c_uint32)]
+
+
+class AttnPromptArgs(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("out", C.c_void_p),
+                ("cu_seqlens", C.c_void_p), ("total", C.c_uint32), ("n_seqs", C.c_uint32),
+                ("heads", C.c_uint32), ("kv_heads", C.c_uint32), ("dim", C.c_uint32),
+                ("ld_q", C.c_uint32), ("ld_k", C.c_uint32), ("ld_v", C.c_uint32),
+                ("ld_out", C.c_uint32), ("scale", C.c_float)]
+
+
+class AttnPrefixArgs(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("K", C.c_void_p), ("V", C.c_void_p), ("Ko", C.c_void_p),
+                ("Vo", C.c_void_p), ("own_len", C.c_void_p), ("out", C.c_void_p), ("scratch", C.c_void_p),
+                ("stride_own", C.c_uint64), ("batch", C.c_uint32), ("prefix", C.c_uint32),
+                ("own_cap", C.c_uint32), ("heads", C.c_uint32), ("kv_heads", C.c_uint32),
+                ("dim", C.c_uint32), ("ld_q", C.c_uint32), ("ld_prefix", C.c_uint32),
+                ("ld_own", C.c_uint32), ("ld_out", C.c_uint32), ("scale", C.c_float)]
+
+
+class GemvW4Args(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("W", C.c_void_p), ("scales", C.c_void_p), ("zeros", C.c_void_p),
+                ("y", C.c_void_p), ("m", C.c_uint32), ("n", C.c_uint32), ("k", C.c_uint32),
+                ("group", C.c_uint32), ("ld_x", C.c_uint32), ("ld_y", C.c_uint32)]
 
 
 class KernelDesc(C.Structure):
@@ -175,6 +199,7 @@ def _load():
         "tally_destroy": ([vp], i32),
         "tally_logical_grid": ([u32, vp, C.c_size_t, P(Dim3), P(Dim3)], i32),
         "tally_attn_decode_scratch_bytes": ([u32], C.c_size_t),
+        "tally_attn_prefix_scratch_bytes": ([u32] * 6, C.c_size_t),
         "tally_launch_native": ([vp, P(KernelDesc), i32], i32),
         "tally_launch_attn_decode_static": ([vp, P(AttnDecodeArgs), i32], i32),
         "tally_launch_sliced": ([vp, P(KernelDesc), u32, u32, i32, P(vp)], i32),
@@ -247,6 +272,7 @@ _ARGS_FOR = {
     K_GEMM_BF16: GemmArgs, K_GEMM_BF16_SMALL: GemmArgs, K_GEMM_BF16_N128: GemmArgs,
     K_GEMV_BF16: GemvArgs,
     K_SOFTMAX_F32: SoftmaxArgs, K_LAYERNORM_F32: LayerNormArgs, K_ATTN_DECODE_BF16: AttnDecodeArgs,
+    K_ATTN_PROMPT_BF16: AttnPromptArgs, K_ATTN_PREFIX_BF16: AttnPrefixArgs, K_GEMV_W4_BF16: GemvW4Args,
 }
 
 
@@ -335,6 +361,116 @@ def attn_decode_bf16(q, Kc, Vc, out, scratch):
 
 def attn_decode_scratch_bytes(heads):
     return int(_lib.tally_attn_decode_scratch_bytes(heads))
+
+
+def _rows(t, dim=None):
+    """Elements between the rows of a tensor: its outermost stride but one if `dim` is None, else
+    that of the tokens of a [..., tokens, heads, dim] tensor whose heads lie side by side."""
+    if dim is None:
+        n, row, width = t.shape[-2], t.stride(-2), t.shape[-1]
+    else:
+        n, row, width = t.shape[-3], t.stride(-3), t.shape[-2] * dim
+        assert t.shape[-1] == dim and (t.shape[-2] == 1 or t.stride(-2) == dim)
+    assert t.stride(-1) == 1 or t.shape[-1] == 1
+    row = row if n > 1 else width
+    assert row >= width, "rows overlap"
+    return row
+
+
+def attn_prompt_bf16(q, k, v, out, cu_seqlens, scale=None):
+    """Causal attention over prompts packed one behind the other: q, out [total, heads, dim]; k, v
+    [total, kv_heads, dim]; 16-bit storage tensors that may be views with padded tokens (one
+    fused projection's output).  cu_seqlens: int32 [sequences + 1] on the device, where each begins and
+    the last one ends.  scale: None for dim ** -0.5."""
+    total, heads, dim = q.shape
+    kv_heads = k.shape[1]
+    assert out.shape == q.shape and k.shape == v.shape == (total, kv_heads, dim)
+    assert all(t.element_size() == 2 for t in (q, k, v, out))
+    assert cu_seqlens.dim() == 1 and cu_seqlens.element_size() == 4 and cu_seqlens.is_contiguous() and cu_seqlens.numel() >= 2
+    args = AttnPromptArgs(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), cu_seqlens.data_ptr(),
+                          total, cu_seqlens.numel() - 1, heads, kv_heads, dim,
+                          _rows(q, dim), _rows(k, dim), _rows(v, dim), _rows(out, dim), _scale(scale))
+    return Kernel(K_ATTN_PROMPT_BF16, args, (q, k, v, out, cu_seqlens))
+
+
+def attn_prefix_bf16(q, K, V, Ko, Vo, own_len, out, scratch, scale=None):
+    """One query per head and sequence of a batch behind a shared prefix: q, out [batch, heads, dim];
+    K, V [prefix, kv_heads, dim]; Ko, Vo [batch, own_cap, kv_heads, dim], of which own_len (int32 [batch]
+    on the device) tokens count; 16-bit storage tensors, padded tokens allowed.  K and V (or Ko and Vo) with
+    no tokens, or None, where there is no prefix (no cache).  scratch: attn_prefix_scratch_bytes() bytes."""
+    batch, heads, dim = q.shape
+    held = lambda t, tokens: t is not None and t.shape[tokens] > 0
+    prefix, own_cap, ld_prefix, ld_own, stride = 0, 0, 0, 0, 0
+    kv_heads = K.shape[1] if K is not None else Ko.shape[2]
+    if held(K, 0):
+        prefix, ld_prefix = K.shape[0], _rows(K, dim)
+        assert V.shape == K.shape == (prefix, kv_heads, dim) and _rows(V, dim) == ld_prefix
+        assert K.element_size() == V.element_size() == 2
+    if held(Ko, 1):
+        own_cap, ld_own = Ko.shape[1], _rows(Ko, dim)
+        assert Vo.shape == Ko.shape == (batch, own_cap, kv_heads, dim) and _rows(Vo, dim) == ld_own
+        assert Ko.element_size() == Vo.element_size() == 2
+        assert own_len.shape == (batch,) and own_len.element_size() == 4 and own_len.is_contiguous()
+        stride = Ko.stride(0) if batch > 1 else 0
+        assert batch == 1 or (stride == Vo.stride(0) and stride > 0)
+    assert out.shape == q.shape and q.element_size() == out.element_size() == 2
+    assert scratch.is_contiguous() and (scratch.numel() * scratch.element_size() >=
+                                        attn_prefix_scratch_bytes(batch, heads, kv_heads, dim, prefix, own_cap))
+    ptr = lambda t, n: t.data_ptr() if n else None
+    args = AttnPrefixArgs(q.data_ptr(), ptr(K, prefix), ptr(V, prefix), ptr(Ko, own_cap), ptr(Vo, own_cap),
+                          ptr(own_len, own_cap), out.data_ptr(), scratch.data_ptr(), stride,
+                          batch, prefix, own_cap, heads, kv_heads, dim, _rows(q, dim), ld_prefix, ld_own,
+                          _rows(out, dim), _scale(scale))
+    return Kernel(K_ATTN_PREFIX_BF16, args, (q, K, V, Ko, Vo, own_len, out, scratch))
+
+
+def attn_prefix_scratch_bytes(batch, heads, kv_heads, dim, prefix, own_cap):
+    return int(_lib.tally_attn_prefix_scratch_bytes(batch, heads, kv_heads, dim, prefix, own_cap))
+
+
+def _scale(scale):
+    """0 stands for the usual scale in the C structs, so it is no scale of its own."""
+    if scale is None:
+        return 0.0
+    assert scale > 0
+    return float(scale)
+
+
+def gemv_w4_bf16(x, W, scales, y, zeros=None, group=128):
+    """y = x (codes - zeros)^T with a scale per row and group: x [m, k], y [m, n], m <= 16, 16-bit storage
+    tensors whose rows may be padded; W, scales and zeros as pack_w4() and pack_w4_groups() lay them out."""
+    (m, k), n = x.shape, y.shape[1]
+    tiles, blocks, groups = -(-n // 16), -(-k // 128), -(-k // group)
+    assert y.shape[0] == m and x.element_size() == y.element_size() == scales.element_size() == 2
+    assert W.shape == (tiles, blocks, 64, 4) and W.element_size() == 4 and W.is_contiguous()
+    assert scales.shape == (tiles, groups, 16) and scales.is_contiguous()
+    assert zeros is None or (zeros.shape == scales.shape and zeros.element_size() == 1 and zeros.is_contiguous())
+    args = GemvW4Args(x.data_ptr(), W.data_ptr(), scales.data_ptr(), zeros.data_ptr() if zeros is not None else None,
+                      y.data_ptr(), m, n, k, group, _rows(x), _rows(y))
+    return Kernel(K_GEMV_W4_BF16, args, (x, W, scales, y) + (() if zeros is None else (zeros,)))
+
+
+def pack_w4(codes):
+    """4-bit codes [n, k] (any integer tensor of values 0 .. 15) as gemv_w4_bf16 reads them: int32 tiles
+    [ceil(n / 16), ceil(k / 128), 64, 4] of 16 rows by 128 columns, filled up with zeros."""
+    import torch
+    n, k = codes.shape
+    tiles, blocks = -(-n // 16), -(-k // 128)
+    full = torch.zeros((tiles * 16, blocks * 128), dtype=torch.int64, device=codes.device)
+    full[:n, :k] = codes
+    at = torch.tensor([0, 16, 4, 20, 8, 24, 12, 28], device=codes.device)
+    words = (full.view(tiles, 16, blocks, 4, 4, 8) << at).sum(-1)      # tile, row, block, word, quarter
+    words = words.permute(0, 2, 4, 1, 3).reshape(tiles, blocks, 64, 4)
+    return torch.where(words >= 1 << 31, words - (1 << 32), words).to(torch.int32).contiguous()
+
+
+def pack_w4_groups(t):
+    """Scales or zero points [n, groups] as gemv_w4_bf16 reads them: [ceil(n / 16), groups, 16]."""
+    import torch
+    n, groups = t.shape
+    full = torch.zeros((-(-n // 16) * 16, groups), dtype=t.dtype, device=t.device)
+    full[:n] = t
+    return full.view(-1, 16, groups).transpose(1, 2).contiguous()
 
 
 # ---------------------------------------------------------------- context / jobs

@@ -22,8 +22,11 @@
 #include "admission.h"
 #include "gemm_cover.h"
 #include "kernels_attn.h"
+#include "kernels_flash.h"
 #include "kernels_gemm.h"
+#include "kernels_prefix.h"
 #include "kernels_stream.h"
+#include "kernels_w4.h"
 #include "launch_forms.h"
 
 using namespace tally;
@@ -519,6 +522,143 @@ int grid_attn(const void *p, tally_dim3 *g, tally_dim3 *b) {
   return TALLY_OK;
 }
 
+// What the attention operators share: heads in groups, a row of `dim` per head and token, pointers and
+// strides that 16-byte accesses and 32-bit offsets within a tile allow
+bool attn_heads_ok(uint32_t heads, uint32_t kv_heads, uint32_t dim) {
+  return heads && kv_heads && heads <= (1u << 16) && heads % kv_heads == 0 && (dim == 64 || dim == 128);
+}
+bool attn_ld_ok(uint32_t ld, uint64_t row) { return (ld ? ld >= row : row <= (1u << 20)) && ld % 8 == 0 && ld <= (1u << 20); }
+bool attn_scale_ok(float scale) { return scale >= 0.f && scale <= 3.4e38f; }
+int grid_prompt(const void *p, tally_dim3 *g, tally_dim3 *b) {
+  auto *a = static_cast<const tally_attn_prompt_args *>(p);
+  if (!a->q || !a->k || !a->v || !a->out || !a->cu_seqlens || !a->total || !a->n_seqs || a->total > (1u << 30) ||
+      a->n_seqs > (1u << 24) || !attn_heads_ok(a->heads, a->kv_heads, a->dim) || !attn_scale_ok(a->scale))
+    return TALLY_ERR_INVALID_ARG;
+  if (!aligned16(a->q) || !aligned16(a->k) || !aligned16(a->v) || !aligned16(a->out) ||
+      (reinterpret_cast<uintptr_t>(a->cu_seqlens) & 3u))
+    return TALLY_ERR_INVALID_ARG;
+  const uint64_t rq = (uint64_t)a->heads * a->dim, rk = (uint64_t)a->kv_heads * a->dim;
+  if (!attn_ld_ok(a->ld_q, rq) || !attn_ld_ok(a->ld_out, rq) || !attn_ld_ok(a->ld_k, rk) || !attn_ld_ok(a->ld_v, rk))
+    return TALLY_ERR_INVALID_ARG;
+  const uint64_t blocks = (uint64_t)a->heads * prompt_slots(*a);
+  if (blocks >= (1u << 24)) return TALLY_ERR_INVALID_ARG;   // (a launch has fewer than 2^32 threads)
+  *g = {(uint32_t)blocks, 1, 1};
+  *b = kBlock256;
+  return TALLY_OK;
+}
+
+bool prefix_sizes_ok(uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t dim, uint32_t prefix, uint32_t own_cap) {
+  return batch && attn_heads_ok(heads, kv_heads, dim) && (uint64_t)batch * heads <= (1u << 20) && prefix <= (1u << 28) &&
+         own_cap <= (1u << 28);
+}
+int grid_prefix(const void *p, tally_dim3 *g, tally_dim3 *b) {
+  auto *a = static_cast<const tally_attn_prefix_args *>(p);
+  if (!prefix_sizes_ok(a->batch, a->heads, a->kv_heads, a->dim, a->prefix, a->own_cap) || !attn_scale_ok(a->scale))
+    return TALLY_ERR_INVALID_ARG;
+  if (!a->q || !a->out || !aligned16(a->q) || !aligned16(a->scratch)) return TALLY_ERR_INVALID_ARG;
+  if ((a->prefix || a->own_cap) && !a->scratch) return TALLY_ERR_INVALID_ARG;
+  if (a->prefix && (!a->K || !a->V || !aligned16(a->K) || !aligned16(a->V))) return TALLY_ERR_INVALID_ARG;
+  if (a->own_cap && (!a->Ko || !a->Vo || !a->own_len || !aligned16(a->Ko) || !aligned16(a->Vo) ||
+                     (reinterpret_cast<uintptr_t>(a->own_len) & 3u)))
+    return TALLY_ERR_INVALID_ARG;
+  const uint64_t rq = (uint64_t)a->heads * a->dim, rk = (uint64_t)a->kv_heads * a->dim;
+  if (!attn_ld_ok(a->ld_q, rq) || !attn_ld_ok(a->ld_out, rq) || !attn_ld_ok(a->ld_prefix, rk) || !attn_ld_ok(a->ld_own, rk))
+    return TALLY_ERR_INVALID_ARG;
+  if (a->stride_own % 8 || a->stride_own > (1ull << 48) ||
+      (a->stride_own && a->own_cap && a->stride_own < (uint64_t)(a->own_cap - 1) * (a->ld_own ? a->ld_own : rk) + rk))
+    return TALLY_ERR_INVALID_ARG;
+  *g = {a->heads, a->batch, 1};
+  *b = kBlock256;
+  return TALLY_OK;
+}
+int grid_gemv_w4(const void *p, tally_dim3 *g, tally_dim3 *b) {
+  auto *a = static_cast<const tally_gemv_w4_args *>(p);
+  if (!a->x || !a->W || !a->scales || !a->y || !a->m || a->m > kW4Vectors || !a->n || !a->k || a->n > (1u << 30) ||
+      a->k > (1u << 24) || a->k % 8 || !a->group || a->group > (1u << 24) || (a->group != 32 && a->group != 64 && a->group % 128))
+    return TALLY_ERR_INVALID_ARG;
+  if (!aligned16(a->x) || !aligned16(a->W) || (a->ld_x && (a->ld_x < a->k || a->ld_x % 8 || a->ld_x > (1u << 24))) ||
+      (a->ld_y && a->ld_y < a->n))
+    return TALLY_ERR_INVALID_ARG;
+  *g = {cdiv(a->n, kW4Rows), 1, 1};
+  *b = kBlock256;
+  return TALLY_OK;
+}
+hipError_t launch_native_prefix(hipStream_t s, const void *args, tally_dim3, uint32_t how) {
+  return launch_attn_prefix(s, args, how & kUrgent);
+}
+uint32_t prefix_choice(const void *args, uint32_t, uint64_t *groups) {
+  tally_attn_prefix_args a;
+  memcpy(&a, args, sizeof(a));
+  const PrefixPlan p = prefix_plan(a);
+  *groups = (uint64_t)p.prefix_groups + p.own_groups;
+  return (a.dim == 64 ? 2 : 0) + p.many;
+}
+template <int DIM, bool MANY>
+hipError_t footprint_prefix(uint32_t *lds_bytes, uint32_t *waves, uint32_t *regs_per_lane) {
+  hipFuncAttributes attr;
+  hipError_t e = hipFuncGetAttributes(&attr, (const void *)attn_prefix_partial<DIM, MANY>);
+  if (e != hipSuccess) return e;
+  *lds_bytes = (uint32_t)attr.sharedSizeBytes + prefix_lds<DIM, MANY>();
+  *waves = 4;
+  *regs_per_lane = ((uint32_t)attr.numRegs + 7u) & ~7u;
+  return hipSuccess;
+}
+// 4-bit products: one kernel for each way that groups divide a tile
+uint32_t w4_range(const void *args) {
+  tally_gemv_w4_args a;
+  memcpy(&a, args, sizeof(a));
+  return a.group == 32 ? 0 : a.group == 64 ? 1 : 2;
+}
+uint32_t w4_choice(const void *args, uint32_t, uint64_t *) { return w4_range(args); }
+hipError_t launch_native_w4(hipStream_t s, const void *args, tally_dim3 g, uint32_t how) {
+  switch (w4_range(args)) {
+    case 0: return launch_native_t<GemvW4BodyT<1>>(s, args, g, how);
+    case 1: return launch_native_t<GemvW4BodyT<2>>(s, args, g, how);
+    default: return launch_native_t<GemvW4BodyT<4>>(s, args, g, how);
+  }
+}
+hipError_t launch_sliced_w4(hipStream_t s, const void *args, uint32_t nblocks, const SliceCtl &c) {
+  switch (w4_range(args)) {
+    case 0: return launch_sliced_t<GemvW4BodyT<1>>(s, args, nblocks, c);
+    case 1: return launch_sliced_t<GemvW4BodyT<2>>(s, args, nblocks, c);
+    default: return launch_sliced_t<GemvW4BodyT<4>>(s, args, nblocks, c);
+  }
+}
+hipError_t launch_ptb_w4(hipStream_t s, const void *args, const PtbCtl &c) {
+  switch (w4_range(args)) {
+    case 0: return launch_ptb_t<GemvW4BodyT<1>>(s, args, c);
+    case 1: return launch_ptb_t<GemvW4BodyT<2>>(s, args, c);
+    default: return launch_ptb_t<GemvW4BodyT<4>>(s, args, c);
+  }
+}
+
+// One operator, a kernel for each width of a head.  No worker occupies more than `Wide`'s.
+template <class Wide, class Narrow>
+uint32_t dim_range(const void *args) {
+  typename Wide::Args a;
+  memcpy(&a, args, sizeof(a));
+  return a.dim == 64 ? 1 : 0;
+}
+template <class Wide, class Narrow>
+uint32_t dim_choice(const void *args, uint32_t, uint64_t *) { return dim_range<Wide, Narrow>(args); }
+template <class Wide, class Narrow>
+hipError_t launch_native_dim_t(hipStream_t s, const void *args, tally_dim3 g, uint32_t how) {
+  return dim_range<Wide, Narrow>(args) ? launch_native_t<Narrow>(s, args, g, how) : launch_native_t<Wide>(s, args, g, how);
+}
+template <class Wide, class Narrow>
+hipError_t launch_sliced_dim_t(hipStream_t s, const void *args, uint32_t nblocks, const SliceCtl &c) {
+  return dim_range<Wide, Narrow>(args) ? launch_sliced_t<Narrow>(s, args, nblocks, c) : launch_sliced_t<Wide>(s, args, nblocks, c);
+}
+template <class Wide, class Narrow>
+hipError_t launch_ptb_dim_t(hipStream_t s, const void *args, const PtbCtl &c) {
+  return dim_range<Wide, Narrow>(args) ? launch_ptb_t<Narrow>(s, args, c) : launch_ptb_t<Wide>(s, args, c);
+}
+template <class Wide, class Narrow>
+hipError_t init_dim_t() {
+  const hipError_t e = init_t<Wide>();
+  return e == hipSuccess ? init_t<Narrow>() : e;
+}
+
 template <class Body>
 double pause_fraction_t(const void *args, uint32_t every, uint32_t, uint32_t) {
   if constexpr (Body::YIELDS) {
@@ -568,6 +708,13 @@ struct TakesTogether<Body, std::enable_if_t<Body::TOGETHER>> : std::true_type {}
                        GEMM_WAVE_TILES(false) GEMM_RINGS(GEMM_RING_FOOT_F)},                                                           \
    gemm_native_choice<Body::TILE_N>, gemm_sliced_choice<slices>, GemmParts<Body>::parts, nullptr, nullptr, false, true}
 
+#define OPS_DIM(Wide, Narrow, nm, gridfn)                                                                 \
+  {nm, sizeof(Wide::Args), true, gridfn, launch_native_dim_t<Wide, Narrow>,                               \
+   launch_sliced_dim_t<Wide, Narrow>, launch_ptb_dim_t<Wide, Narrow>, init_dim_t<Wide, Narrow>,           \
+   occupancy_t<Wide>, pause_fraction_t<Wide>, footprint_t<Wide>,                                          \
+   {footprint_native_t<Wide>, footprint_native_t<Narrow>}, dim_choice<Wide, Narrow>, dim_range<Wide, Narrow>, \
+   nullptr, nullptr, nullptr, false, false}
+
 const KernelOps kOps[TALLY_K_COUNT] = {
     OPS(SaxpyBody, "saxpy", grid_saxpy),
     OPS(ReduceSumBody, "reduce_sum", grid_reduce_sum),
@@ -588,9 +735,18 @@ const KernelOps kOps[TALLY_K_COUNT] = {
      gemm_sliced_choice<GemmCover::k32>, nullptr, block_bytes<GemmSmallBody>, GemmSmallBody::team_bytes,
      false, true},
     OPS_GEMM(GemmN128Body, "gemm_bf16_n128", grid_gemm_n128, GemmCover::k256x128),
+    OPS_DIM(PromptBody, PromptNarrowBody, "attn_prompt_bf16", grid_prompt),
+    {"attn_prefix_bf16", sizeof(tally_attn_prefix_args), false, grid_prefix, launch_native_prefix,
+     nullptr, nullptr, nullptr, nullptr, nullptr, nullptr,
+     {footprint_prefix<128, false>, footprint_prefix<128, true>, footprint_prefix<64, false>, footprint_prefix<64, true>},
+     prefix_choice, nullptr, nullptr, nullptr, nullptr, false, false},
+    {"gemv_w4_bf16", sizeof(tally_gemv_w4_args), true, grid_gemv_w4, launch_native_w4, launch_sliced_w4, launch_ptb_w4,
+     nullptr, occupancy_t<GemvW4BodyT<1>>, pause_fraction_t<GemvW4BodyT<1>>, footprint_t<GemvW4BodyT<1>>,
+     {footprint_native_t<GemvW4BodyT<1>>, footprint_native_t<GemvW4BodyT<2>>, footprint_native_t<GemvW4BodyT<4>>},
+     w4_choice, w4_range, nullptr, nullptr, nullptr, false, false},
 };
 
-constexpr size_t kMaxArgs = 96;
+constexpr size_t kMaxArgs = 128;
 constexpr int kSlots = 64;
 constexpr int kMaxShunned = 64;
 constexpr int kMaxSide = 2 * 8 + 2;
@@ -1325,6 +1481,11 @@ int tally_logical_grid(uint32_t kernel_id, const void *args, size_t args_size, t
 }
 
 size_t tally_attn_decode_scratch_bytes(uint32_t heads) { return attn_decode_scratch_bytes(heads); }
+size_t tally_attn_prefix_scratch_bytes(uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t dim, uint32_t prefix,
+                                       uint32_t own_cap) {
+  return prefix_sizes_ok(batch, heads, kv_heads, dim, prefix, own_cap)
+             ? prefix_scratch_bytes(batch, heads, kv_heads, dim, prefix, own_cap) : 0;
+}
 
 int tally_launch_native(tally_ctx *ctx, const tally_kernel_desc *desc, int on_hi_stream) {
   if (!ctx) return TALLY_ERR_INVALID_ARG;

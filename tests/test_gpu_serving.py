@@ -1,0 +1,591 @@
+"""GPU parity of the serving operators (prompt attention, shared-prefix attention, 4-bit products)
+against their fp64 statements, in every launch form, at the sizes and masks where they can go wrong.
+
+Tolerances, all of them from the arithmetic.  bf16 rounds by at most 2^-8 of a value.
+  attention: the output is rounded once, and each p once before the second product:
+    |d| <= 2^-8 |want| + (2^-8 + 2^-12) M, with M = sum p |v| / sum p.  2^-12 covers fp32: scores of magnitude s
+    have an absolute error below (dim + 2) s 2^-24 (130 x 40 x 2^-24 < 2^-11.6 only beyond s = 40; inputs here stay
+    below s = 20) and sums of up to 4096 terms at most 2^-12 of M, in practice far less.
+  4-bit products: rounded once; a group's sums and the sum over groups are fp32 chains of at most 2 k + 300
+    additions of terms whose magnitudes sum to M = sum (256 + code + zero) |x| s >= what is added:
+    |d| <= 2^-8 |want| + (2 k + 300) 2^-24 M.
+"""
+import numpy as np
+import pytest
+
+import tally_inputs as TI
+from oracle import bf16 as obf16
+from oracle import serving as OS
+
+pytestmark = pytest.mark.gpu
+SENTINEL = 0x7ABC                                          # a bf16 that no output is
+
+
+@pytest.fixture(scope="module")
+def env():
+    import torch
+    import paper_2410_07381_amd.binding as B
+    assert torch.cuda.is_available()
+    hi, be = torch.cuda.Stream(), torch.cuda.Stream()
+    ctx = B.Context(hi, be)
+    yield B, ctx, torch
+    ctx.close()
+
+
+def _bits(rng, shape, scale=1.0):
+    return TI.to_bf16_bits((rng.standard_normal(shape) * scale).astype(np.float32))
+
+
+def _dev(torch, bits):
+    return torch.from_numpy(np.ascontiguousarray(bits).view(np.int16)).cuda()
+
+
+def _host(t):
+    return t.cpu().numpy().view(np.uint16)
+
+
+def _attn_ok(got_bits, want, mass):
+    got = obf16.decode(got_bits)
+    bound = 2.0 ** -8 * np.abs(want) + (2.0 ** -8 + 2.0 ** -12) * mass
+    assert np.isfinite(got).all()
+    err = np.abs(got - want)
+    assert (err <= bound).all(), f"{(err > bound).sum()} of {err.size} off; worst {(err / np.maximum(bound, 1e-30)).max():.2f} bounds"
+
+
+def _run(ctx, torch, kernel, form):
+    """The whole kernel in one of its forms."""
+    if form == "hi" or form == "be":
+        ctx.launch_native(kernel, hi=form == "hi")
+    elif form == "sliced":
+        job = ctx.launch_sliced(kernel, max(kernel.total_blocks // 3, 1))
+        while job.wait() != 3:
+            job.resume()
+        job.free()
+    else:
+        total = kernel.total_blocks
+        job = ctx.launch_ptb(kernel, min(ctx.max_workers(kernel), max(total // 2, 1)), coverage=True, stop_at=total // 2)
+        job.wait()
+        assert job.progress()[0] == total // 2 or job.progress()[2] == 3
+        job.resume()
+        assert job.wait() == 3
+        assert (job.coverage()["count"] == 1).all()
+        job.free()
+    torch.cuda.synchronize()
+
+
+# ---------------------------------------------------------------- whole prompts
+def _prompt(torch, seed, edges, total, heads, kv_heads, dim, scale=1.0):
+    rng = np.random.default_rng(seed)
+    q, k, v = (_bits(rng, (total, h, dim), scale) for h in (heads, kv_heads, kv_heads))
+    cu = torch.tensor(edges, dtype=torch.int32, device="cuda")
+    return q, k, v, cu
+
+
+CASES = [
+    ([0, 1], 1, 1, 1, 128), ([0, 2], 2, 2, 1, 64), ([0, 31], 31, 1, 1, 128), ([0, 32], 32, 3, 3, 64), ([0, 33], 33, 2, 2, 128),
+    ([0, 63], 63, 1, 1, 64), ([0, 64], 64, 2, 1, 128), ([0, 65], 65, 1, 1, 128), ([0, 127], 127, 1, 1, 64),
+    ([0, 128], 128, 1, 1, 128), ([0, 129], 129, 2, 1, 128), ([0, 300], 300, 7, 1, 128), ([0, 300], 301, 4, 2, 64),
+    # packed: empty sequences, single tokens, starts away from any tile, rows before and behind them
+    ([0, 1, 1, 2, 66, 66, 193], 193, 4, 2, 128), ([5, 5, 20, 148, 150], 160, 3, 1, 64),
+    ([0, 127, 128, 129, 257, 258], 300, 2, 2, 128), ([100, 229], 400, 1, 1, 128),
+]
+
+
+@pytest.mark.parametrize("form", ["hi", "be", "sliced", "ptb"])
+@pytest.mark.parametrize("edges,total,heads,kv_heads,dim", CASES)
+def test_prompt_attention(env, edges, total, heads, kv_heads, dim, form):
+    B, ctx, torch = env
+    q, k, v, cu = _prompt(torch, total + dim, edges, total, heads, kv_heads, dim)
+    out = torch.full((total, heads, dim), SENTINEL, dtype=torch.int16, device="cuda")
+    kern = B.attn_prompt_bf16(_dev(torch, q), _dev(torch, k), _dev(torch, v), out, cu)
+    torch.cuda.synchronize()
+    _run(ctx, torch, kern, form)
+    want, mass = OS.attn_prompt(obf16.decode(q), obf16.decode(k), obf16.decode(v), edges)
+    mine = ~np.isnan(want[:, 0, 0])
+    got = _host(out)
+    _attn_ok(got[mine], want[mine], mass[mine])
+    assert (got[~mine] == SENTINEL).all()                  # rows of no sequence stay as they were
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_prompt_forms_give_the_same_bits(env, dim):
+    B, ctx, torch = env
+    edges = [0, 700, 701, 1500]
+    q, k, v, cu = _prompt(torch, 3, edges, 1500, 4, 2, dim)
+    q, k, v = (_dev(torch, t) for t in (q, k, v))
+    outs = []
+    for form in ("hi", "be", "sliced", "ptb", "ptb"):
+        out = torch.zeros_like(q)
+        kern = B.attn_prompt_bf16(q, k, v, out, cu)
+        torch.cuda.synchronize()
+        _run(ctx, torch, kern, form)
+        outs.append(_host(out))
+    assert all((o == outs[0]).all() for o in outs)
+
+
+@pytest.mark.parametrize("scale", [0.02, 1.5])
+def test_prompt_scale_and_large_scores(env, scale):
+    """A maximum that keeps rising (scores up to some hundreds): rescaling, and weights far below it."""
+    B, ctx, torch = env
+    total, dim = 260, 64
+    rng = np.random.default_rng(8)
+    ramp = np.linspace(0.1, 2.0, total)[:, None, None]
+    q, k, v = _bits(rng, (total, 2, dim)), TI.to_bf16_bits((rng.standard_normal((total, 1, dim)) * ramp).astype(np.float32)), _bits(rng, (total, 1, dim))
+    out = torch.zeros((total, 2, dim), dtype=torch.int16, device="cuda")
+    cu = torch.tensor([0, total], dtype=torch.int32, device="cuda")
+    kern = B.attn_prompt_bf16(_dev(torch, q), _dev(torch, k), _dev(torch, v), out, cu, scale=scale)
+    torch.cuda.synchronize()
+    _run(ctx, torch, kern, "hi")
+    want, mass = OS.attn_prompt(obf16.decode(q), obf16.decode(k), obf16.decode(v), [0, total], scale)
+    _attn_ok(_host(out), want, mass)
+
+
+def test_prompt_strided_views_of_one_buffer(env):
+    """q, k and v of a fused projection's padded output, out a view with padding of its own."""
+    B, ctx, torch = env
+    total, heads, kv, dim = 200, 6, 2, 128
+    rng = np.random.default_rng(4)
+    whole = _bits(rng, (total, heads + 2 * kv + 1, dim))
+    buf = _dev(torch, whole)
+    out = torch.full((total, heads + 3, dim), SENTINEL, dtype=torch.int16, device="cuda")
+    kern = B.attn_prompt_bf16(buf[:, :heads], buf[:, heads:heads + kv], buf[:, heads + kv:heads + 2 * kv], out[:, 1:1 + heads],
+                              torch.tensor([0, 50, total], dtype=torch.int32, device="cuda"))
+    torch.cuda.synchronize()
+    _run(ctx, torch, kern, "hi")
+    w = obf16.decode(whole)
+    want, mass = OS.attn_prompt(w[:, :heads], w[:, heads:heads + kv], w[:, heads + kv:heads + 2 * kv], [0, 50, total])
+    got = _host(out)
+    _attn_ok(got[:, 1:1 + heads], want, mass)
+    assert (got[:, 0] == SENTINEL).all() and (got[:, 1 + heads:] == SENTINEL).all()
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("poison", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("where", [0, 17, 40, 63, 64, 100, 129])
+def test_prompt_rows_do_not_see_what_is_hidden_from_them(env, where, poison, dim):
+    """K and V of one token are no numbers: rows before it, and other sequences, are what they are without
+    it; rows from it on are not finite where the definition's are not."""
+    B, ctx, torch = env
+    edges, total = [0, 130, 190], 195
+    q, k, v, cu = _prompt(torch, where, edges, total, 2, 1, dim)
+    bad = TI.to_bf16_bits(np.float32([poison]))[0]
+    want, mass = OS.attn_prompt(obf16.decode(q), obf16.decode(k), obf16.decode(v), edges)
+    for keys in (False, True):
+        k2, v2 = k.copy(), v.copy()
+        v2[where, 0, 3:9] = bad
+        v2[192:] = bad                                     # rows behind the last sequence
+        k2[192:] = bad
+        if keys:
+            k2[where] = bad
+        out = torch.zeros((total, 2, dim), dtype=torch.int16, device="cuda")
+        kern = B.attn_prompt_bf16(_dev(torch, q), _dev(torch, k2), _dev(torch, v2), out, cu)
+        torch.cuda.synchronize()
+        _run(ctx, torch, kern, "hi")
+        got = _host(out)
+        fine = np.r_[0:where, 130:190]
+        _attn_ok(got[fine], want[fine], mass[fine])
+        seen = obf16.decode(got[where:130])
+        if not keys:
+            hit = seen[:, :, 3:9]
+            assert np.isnan(hit).all() if np.isnan(poison) else (hit == poison).all()
+            rest = np.r_[0:3, 9:dim]
+            _attn_ok(got[where:130][:, :, rest], want[where:130][:, :, rest], mass[where:130][:, :, rest])
+        else:
+            # (q has both signs, so a key of infinities has a score of NaN as well: the whole row is NaN)
+            assert np.isnan(seen).all()
+
+
+@pytest.mark.parametrize("seqs", [63, 64, 65, 700, 5000])
+def test_prompt_many_sequences(env, seqs):
+    """The search for a block's sequence, with one, two and three rounds of 64 candidates."""
+    B, ctx, torch = env
+    rng = np.random.default_rng(seqs)
+    lens = rng.integers(0, 4, seqs)
+    lens[rng.integers(0, seqs)] = 140
+    edges = np.concatenate([[0], np.cumsum(lens)]).astype(int).tolist()
+    total = edges[-1]
+    q, k, v, cu = _prompt(torch, seqs, edges, total, 1, 1, 64)
+    out = torch.full((total, 1, 64), SENTINEL, dtype=torch.int16, device="cuda")
+    kern = B.attn_prompt_bf16(_dev(torch, q), _dev(torch, k), _dev(torch, v), out, cu)
+    torch.cuda.synchronize()
+    _run(ctx, torch, kern, "hi")
+    want, mass = OS.attn_prompt(obf16.decode(q), obf16.decode(k), obf16.decode(v), edges)
+    _attn_ok(_host(out), want, mass)
+
+
+@pytest.mark.parametrize("edges", [[-5, 40, 20, 100, 9000], [90, 10], [0, 0, 0], [200, 300], [-9, -1, 7]])
+def test_prompt_with_edges_that_make_no_sense_stays_in_bounds(env, edges):
+    """Entries outside [0, total] count as its ends and an end before its start as an empty sequence (the
+    kernel clamps what it reads); neighbours of the tensors stay as they were."""
+    B, ctx, torch = env
+    total, dim = 100, 64
+    room = torch.full((3 * total, 2, dim), SENTINEL, dtype=torch.int16, device="cuda")
+    x = _dev(torch, _bits(np.random.default_rng(1), (total, 2, dim)))
+    kern = B.attn_prompt_bf16(x, x, x, room[total:2 * total], torch.tensor(edges, dtype=torch.int32, device="cuda"))
+    torch.cuda.synchronize()
+    _run(ctx, torch, kern, "hi")
+    got = _host(room)
+    assert (got[:total] == SENTINEL).all() and (got[2 * total:] == SENTINEL).all()
+    assert np.isfinite(obf16.decode(got[total:2 * total])).all()
+
+
+def test_prompt_offsets_beyond_32_bits(env):
+    """Tokens so far apart that the last ones lie 4 GB and more behind the first."""
+    B, ctx, torch = env
+    total, ld, dim = 2200, 1 << 20, 64
+    rng = np.random.default_rng(6)
+    q, k, v = (_bits(rng, (total, 1, dim)) for _ in range(3))
+    big = torch.empty(total * ld, dtype=torch.int16, device="cuda").view(total, ld // dim, dim)
+    big[:, 0:1], big[:, 1:2], big[:, 2:3] = _dev(torch, q), _dev(torch, k), _dev(torch, v)
+    kern = B.attn_prompt_bf16(big[:, 0:1], big[:, 1:2], big[:, 2:3], big[:, 3:4], torch.tensor([0, 2050, total], dtype=torch.int32, device="cuda"))
+    torch.cuda.synchronize()
+    _run(ctx, torch, kern, "hi")
+    rows = np.r_[0:3, 2046:2200]
+    got = _host(big[:, 3:4].contiguous())
+    del big, kern
+    qd, kd, vd = (obf16.decode(t) for t in (q, k, v))
+    for a, b in ((0, 3), (2050, total)):
+        want, mass = OS.attn_prompt(qd, kd, vd, [0 if a == 0 else 2050, b])
+        _attn_ok(got[a:b], want[a:b], mass[a:b])
+    want, mass = OS._attend(qd[2049, 0], kd[:2050, 0], vd[:2050, 0], dim ** -0.5)
+    _attn_ok(got[2049, 0], want, mass)
+    assert rows.size
+
+
+def test_prompt_workers_pause_inside_a_block_and_go_on(env):
+    """A pausing request while a long prompt runs as workers: the job stops or pauses, goes on, and gives the
+    original form's bits."""
+    B, ctx, torch = env
+    total = 12000
+    g = torch.Generator(device="cuda").manual_seed(1)
+    q, k, v = (torch.randn((total, 8, 128), generator=g, device="cuda").to(torch.bfloat16) for _ in range(3))
+    cu = torch.tensor([0, total], dtype=torch.int32, device="cuda")
+    a, b = torch.zeros_like(q), torch.zeros_like(q)
+    torch.cuda.synchronize()
+    ctx.launch_native(B.attn_prompt_bf16(q, k, v, a, cu))
+    torch.cuda.synchronize()
+    kern = B.attn_prompt_bf16(q, k, v, b, cu)
+    job = ctx.launch_ptb(kern, 256, coverage=True)
+    stops = 0
+    for _ in range(200):
+        job.preempt(pause=True)
+        job.end_pause()
+        if job.wait() == B.JOB_COMPLETE:
+            break
+        stops += 1
+        job.resume()
+    assert job.wait() == B.JOB_COMPLETE
+    assert (job.coverage()["count"] == 1).all()
+    job.free()
+    torch.cuda.synchronize()
+    assert torch.equal(a.view(torch.int16), b.view(torch.int16))
+
+
+# ---------------------------------------------------------------- behind a shared prefix
+def _prefix(seed, batch, heads, kv, dim, prefix, cap):
+    rng = np.random.default_rng(seed)
+    return (_bits(rng, (batch, heads, dim)), _bits(rng, (prefix, kv, dim)), _bits(rng, (prefix, kv, dim)),
+            _bits(rng, (batch, cap, kv, dim)), _bits(rng, (batch, cap, kv, dim)))
+
+
+def _scratch(B, torch, batch, heads, kv, dim, prefix, cap):
+    n = B.attn_prefix_scratch_bytes(batch, heads, kv, dim, prefix, cap)
+    return torch.full((max(n, 1) + 64,), 0x7F, dtype=torch.uint8, device="cuda")   # (as floats: NaN-like garbage)
+
+
+PREFIX = [
+    # batch, heads, kv_heads, dim, prefix, own_cap, lens
+    (1, 1, 1, 128, 1, 0, None), (1, 1, 1, 64, 0, 1, [1]), (2, 2, 1, 128, 31, 5, [0, 5]), (3, 4, 2, 64, 32, 33, [33, 0, 1]),
+    (3, 4, 2, 128, 33, 64, [64, 63, 32]), (5, 7, 1, 128, 127, 65, [65, 0, 31, 33, 64]), (4, 12, 12, 64, 300, 20, [3, 0, 20, 7]),
+    # nothing to attend to, lengths outside the cache
+    (3, 2, 2, 128, 0, 40, [0, 40, -3]), (3, 2, 1, 64, 10, 8, [99, -1, 8]), (2, 2, 2, 64, 0, 0, None),
+    # more than 64 rows to a K/V head (128-row workgroups), several tiles of them, more than 64 heads to one
+    (40, 4, 2, 128, 200, 9, "even"), (70, 8, 4, 64, 129, 3, "even"), (300, 1, 1, 128, 64, 2, "even"), (3, 96, 1, 128, 70, 90, [90, 0, 45]),
+    (2, 140, 2, 64, 65, 66, [66, 1]), (1, 70, 1, 128, 40, 0, None),
+]
+
+
+@pytest.mark.parametrize("batch,heads,kv,dim,prefix,cap,lens", PREFIX)
+@pytest.mark.parametrize("hi", [True, False])
+def test_prefix_attention(env, batch, heads, kv, dim, prefix, cap, lens, hi):
+    B, ctx, torch = env
+    q, K, V, Ko, Vo = _prefix(batch + prefix, batch, heads, kv, dim, prefix, cap)
+    lens = [i % (cap + 1) for i in range(batch)] if lens == "even" else lens or [0] * batch
+    hidden = [min(max(n, 0), cap) for n in lens]
+    Kn, Vn = Ko.copy(), Vo.copy()
+    for b, n in enumerate(hidden):                         # what lies behind is no numbers
+        Kn[b, n:], Vn[b, n:] = 0x7FC0, 0xFF80
+    out = torch.full((batch, heads, dim), SENTINEL, dtype=torch.int16, device="cuda")
+    kern = B.attn_prefix_bf16(_dev(torch, q), _dev(torch, K), _dev(torch, V), _dev(torch, Kn), _dev(torch, Vn),
+                              torch.tensor(lens, dtype=torch.int32, device="cuda"), out, _scratch(B, torch, batch, heads, kv, dim, prefix, cap))
+    torch.cuda.synchronize()
+    _run(ctx, torch, kern, "hi" if hi else "be")
+    want, mass = OS.attn_prefix(*(obf16.decode(t) for t in (q, K, V, Ko, Vo)), lens)
+    got = _host(out)
+    _attn_ok(got, want, mass)
+    for b, n in enumerate(hidden):
+        if prefix + n == 0:
+            assert (got[b] == 0).all()
+
+
+def test_prefix_many_parts(env):
+    """A prefix and replies that are split into many parts, some of them beyond a reply's end."""
+    B, ctx, torch = env
+    batch, heads, kv, dim, prefix, cap = 2, 2, 1, 128, 20000, 9000
+    q, K, V, Ko, Vo = _prefix(5, batch, heads, kv, dim, prefix, cap)
+    lens = [9000, 130]
+    out = torch.zeros((batch, heads, dim), dtype=torch.int16, device="cuda")
+    kern = B.attn_prefix_bf16(_dev(torch, q), _dev(torch, K), _dev(torch, V), _dev(torch, Ko), _dev(torch, Vo),
+                              torch.tensor(lens, dtype=torch.int32, device="cuda"), out, _scratch(B, torch, batch, heads, kv, dim, prefix, cap))
+    torch.cuda.synchronize()
+    _run(ctx, torch, kern, "hi")
+    want, mass = OS.attn_prefix(*(obf16.decode(t) for t in (q, K, V, Ko, Vo)), lens)
+    _attn_ok(_host(out), want, mass)
+
+
+def test_prefix_strides_and_caches_beyond_32_bits(env):
+    """Padded tokens everywhere, and sequences' caches 2^31 elements apart."""
+    B, ctx, torch = env
+    batch, heads, kv, dim, prefix, cap = 2, 4, 2, 64, 50, 40
+    q, K, V, Ko, Vo = _prefix(6, batch, heads, kv, dim, prefix, cap)
+    lens = [40, 17]
+    both = _dev(torch, np.concatenate([K, V], 1))          # [prefix, 2 kv, dim]
+    big = torch.empty((1 << 31) + cap * 2 * kv * dim, dtype=torch.int16, device="cuda")
+    own = big.as_strided((batch, cap, 2 * kv, dim), (1 << 31, 2 * kv * dim, dim, 1))
+    own.copy_(_dev(torch, np.concatenate([Ko, Vo], 2)))
+    qq = torch.zeros((batch, heads + 2, dim), dtype=torch.int16, device="cuda")
+    qq[:, 1:1 + heads] = _dev(torch, q)
+    out = torch.full((batch, heads + 1, dim), SENTINEL, dtype=torch.int16, device="cuda")
+    kern = B.attn_prefix_bf16(qq[:, 1:1 + heads], both[:, :kv], both[:, kv:], own[:, :, :kv], own[:, :, kv:],
+                              torch.tensor(lens, dtype=torch.int32, device="cuda"), out[:, :heads],
+                              _scratch(B, torch, batch, heads, kv, dim, prefix, cap), scale=0.2)
+    torch.cuda.synchronize()
+    _run(ctx, torch, kern, "hi")
+    got = _host(out)
+    del big, own, kern
+    want, mass = OS.attn_prefix(*(obf16.decode(t) for t in (q, K, V, Ko, Vo)), lens, 0.2)
+    _attn_ok(got[:, :heads], want, mass)
+    assert (got[:, heads:] == SENTINEL).all()
+
+
+def test_prefix_is_not_transformable(env):
+    B, ctx, torch = env
+    z = torch.zeros((1, 1, 64), dtype=torch.int16, device="cuda")
+    kern = B.attn_prefix_bf16(z, z, z, None, None, None, z.clone(), torch.zeros(4096, dtype=torch.uint8, device="cuda"))
+    for launch in (lambda: ctx.launch_ptb(kern, 1), lambda: ctx.launch_sliced(kern, 1)):
+        with pytest.raises(B.TallyError) as e:
+            launch()
+        assert e.value.status == B.ERR_UNSUPPORTED
+
+
+# ---------------------------------------------------------------- 4-bit products
+def _w4(rng, m, n, k, group, zeros):
+    groups = -(-k // group)
+    return (_bits(rng, (m, k)), rng.integers(0, 16, (n, k)), TI.to_bf16_bits(rng.uniform(0.5, 2.0, (n, groups)).astype(np.float32)),
+            rng.integers(0, 16, (n, groups)).astype(np.uint8) if zeros else None)
+
+
+def _w4_ok(got_bits, x, codes, scales, zeros, group):
+    want, mass = OS.gemv_w4(obf16.decode(x), codes, obf16.decode(scales), zeros, group)
+    err = np.abs(obf16.decode(got_bits) - want)
+    bound = 2.0 ** -8 * np.abs(want) + (2 * x.shape[1] + 300) * 2.0 ** -24 * mass
+    assert (err <= bound).all(), f"worst {(err / bound).max():.2f} bounds"
+
+
+W4 = [(1, 1, 8, 32, False), (1, 16, 128, 128, True), (2, 17, 120, 32, True), (3, 15, 136, 64, False), (16, 33, 1000, 32, True),
+      (5, 100, 512, 64, True), (4, 50, 640, 256, False), (16, 64, 1288, 128, True), (7, 31, 2056, 64, False), (1, 300, 4096, 128, False),
+      (9, 48, 4104, 384, True), (16, 16, 72, 64, True), (1, 40, 11008, 64, True)]
+
+
+@pytest.mark.parametrize("form", ["hi", "be", "sliced", "ptb"])
+@pytest.mark.parametrize("m,n,k,group,zeros", W4)
+def test_gemv_w4(env, m, n, k, group, zeros, form):
+    B, ctx, torch = env
+    rng = np.random.default_rng(n + k)
+    x, codes, scales, z = _w4(rng, m, n, k, group, zeros)
+    W = B.pack_w4(torch.from_numpy(codes))
+    s, zp = B.pack_w4_groups(torch.from_numpy(scales.view(np.int16))), B.pack_w4_groups(torch.from_numpy(z)) if zeros else None
+    # rows and columns that do not exist hold garbage
+    junk = torch.from_numpy(rng.integers(0, 16, (W.shape[0] * 16, W.shape[1] * 128)))
+    junk[:n, :k] = torch.from_numpy(codes)
+    W = B.pack_w4(junk)
+    if n % 16:
+        s[-1, :, n % 16:] = 0x7FC0
+    y = torch.full((m, n), SENTINEL, dtype=torch.int16, device="cuda")
+    kern = B.gemv_w4_bf16(_dev(torch, x), W.cuda(), s.cuda(), y, zeros=zp.cuda() if zeros else None, group=group)
+    torch.cuda.synchronize()
+    _run(ctx, torch, kern, form)
+    _w4_ok(_host(y), x, codes, scales, z, group)
+
+
+def test_gemv_w4_strides_and_neighbours(env):
+    """Vectors and outputs with padded rows; what lies between and behind them is left alone, and not read
+    into sums even if it is no number."""
+    B, ctx, torch = env
+    m, n, k, group = 3, 37, 200, 32
+    rng = np.random.default_rng(11)
+    x, codes, scales, z = _w4(rng, m, n, k, group, True)
+    wide = np.full((m + 1, k + 24), 0x7FC0, np.uint16)
+    wide[:m, :k] = x
+    xd = _dev(torch, wide)
+    y = torch.full((m + 2, n + 5), SENTINEL, dtype=torch.int16, device="cuda")
+    kern = B.gemv_w4_bf16(xd[:m, :k], B.pack_w4(torch.from_numpy(codes)).cuda(), B.pack_w4_groups(torch.from_numpy(scales.view(np.int16))).cuda(),
+                          y[1:1 + m, 2:2 + n], zeros=B.pack_w4_groups(torch.from_numpy(z)).cuda(), group=group)
+    torch.cuda.synchronize()
+    _run(ctx, torch, kern, "hi")
+    got = _host(y)
+    _w4_ok(got[1:1 + m, 2:2 + n], x, codes, scales, z, group)
+    assert (got[0] == SENTINEL).all() and (got[1 + m:] == SENTINEL).all()
+    assert (got[1:1 + m, :2] == SENTINEL).all() and (got[1:1 + m, 2 + n:] == SENTINEL).all()
+
+
+def test_gemv_w4_rows_do_not_depend_on_the_number_of_vectors(env):
+    B, ctx, torch = env
+    n, k, group = 100, 1000, 64
+    x, codes, scales, z = _w4(np.random.default_rng(12), 16, n, k, group, False)
+    W, s, xd = B.pack_w4(torch.from_numpy(codes)).cuda(), B.pack_w4_groups(torch.from_numpy(scales.view(np.int16))).cuda(), _dev(torch, x)
+    outs = []
+    for m in (1, 2, 5, 16):
+        y = torch.zeros((m, n), dtype=torch.int16, device="cuda")
+        kern = B.gemv_w4_bf16(xd[:m], W, s, y, group=group)
+        torch.cuda.synchronize()
+        _run(ctx, torch, kern, "hi")
+        outs.append(_host(y))
+    assert all((o == outs[-1][:len(o)]).all() for o in outs)
+
+
+# ---------------------------------------------------------------- as a program uses them
+def _decode_step(B, torch, g, batch, heads, kv, dim, prefix_kv, cap):
+    """A batch's decode step behind a prefix: attention, then two 4-bit products of its output."""
+    hidden = heads * dim
+    t = lambda *s: torch.randn(s, generator=g, device="cuda").to(torch.bfloat16)
+    q, own = t(batch, heads, dim), t(batch, cap, 2 * kv, dim)
+    lens = torch.arange(batch, dtype=torch.int32, device="cuda") * cap // max(batch - 1, 1)
+    out, mid, y = torch.zeros_like(q), torch.zeros((batch, 512), dtype=torch.bfloat16, device="cuda"), torch.zeros((batch, hidden), dtype=torch.bfloat16, device="cuda")
+    prefix = prefix_kv.shape[0]
+    room = torch.empty(B.attn_prefix_scratch_bytes(batch, heads, kv, dim, prefix, cap), dtype=torch.uint8, device="cuda")
+    def w(n, k):
+        return (B.pack_w4(torch.randint(0, 16, (n, k), generator=g, device="cuda")),
+                B.pack_w4_groups((torch.rand((n, k // 128), generator=g, device="cuda") / k ** 0.5).to(torch.bfloat16)))
+    (w1, s1), (w2, s2) = w(512, hidden), w(hidden, 512)
+    kernels = [B.attn_prefix_bf16(q, prefix_kv[:, :kv], prefix_kv[:, kv:], own[:, :, :kv], own[:, :, kv:], lens, out, room),
+               B.gemv_w4_bf16(out.view(batch, hidden), w1, s1, mid), B.gemv_w4_bf16(mid, w2, s2, y)]
+    return kernels, (out, mid, y)
+
+
+def test_decode_requests_beside_prompts_under_the_scheduler(env):
+    """The operators together: prompts of a best-effort client run as the profiler chooses beside a
+    high-priority client's decode steps, whose prefix is a prompt's K and V; every output is what the calls
+    give one after another."""
+    B, ctx, torch = env
+    heads, kv, dim, total = 8, 2, 128, 3000
+    g = torch.Generator(device="cuda").manual_seed(2)
+    qkv = torch.randn((total, heads + 2 * kv, dim), generator=g, device="cuda").to(torch.bfloat16)
+    cu = torch.tensor([0, 1, 1500, total], dtype=torch.int32, device="cuda")
+    out = torch.zeros((total, heads, dim), dtype=torch.bfloat16, device="cuda")
+    prompt = B.attn_prompt_bf16(qkv[:, :heads], qkv[:, heads:heads + kv], qkv[:, heads + kv:], out, cu)
+    step, results = _decode_step(B, torch, g, 5, heads, kv, dim, qkv[1500:, heads:], 30)
+    torch.cuda.synchronize()
+    ctx.launch_native(prompt)
+    for kern in step:
+        ctx.launch_native(kern, hi=True)
+    torch.cuda.synchronize()
+    want = [t.clone() for t in (out,) + results]
+    assert all(torch.isfinite(t.float()).all() and t.float().abs().sum() > 0 for t in want)
+    for t in (out,) + results:
+        t.zero_()
+    torch.cuda.synchronize()
+    sched = ctx.scheduler()
+    try:
+        sched.submit_be(prompt, loop=True)
+        sched.submit_be(step[1], (B.CFG_PTB, 16, 1), loop=False)   # (a product as best-effort work, too)
+        for _ in range(40):
+            sched.submit_hi(step)
+            while sched.poll():
+                pass
+        import time
+        t0 = time.perf_counter()
+        while sched.stats()["be_kernels_done"] < 5 and time.perf_counter() - t0 < 20:
+            time.sleep(0.001)
+        assert sched.stats()["hi_requests_done"] == 40 and sched.stats()["be_kernels_done"] >= 5
+    finally:
+        sched.close()
+    torch.cuda.synchronize()
+    for name, a, b in zip(("prompt", "attention", "first product", "second product"), (out,) + results, want):
+        assert torch.equal(a.view(torch.int16), b.view(torch.int16)), name
+
+
+def test_captured_decode_step_replays_beside_eager_work(env):
+    """A captured decode step, replayed with the program's own work and waits between; new inputs in the
+    same buffers give new outputs."""
+    B, ctx, torch = env
+    heads, kv, dim = 4, 1, 64
+    g = torch.Generator(device="cuda").manual_seed(3)
+    shared = torch.randn((300, 2 * kv, dim), generator=g, device="cuda").to(torch.bfloat16)
+    step, results = _decode_step(B, torch, g, 6, heads, kv, dim, shared, 40)
+    prompt_in = torch.randn((200, heads, dim), generator=g, device="cuda").to(torch.bfloat16)
+    prompt_out = torch.zeros_like(prompt_in)
+    step = [B.attn_prompt_bf16(prompt_in, prompt_in, prompt_in, prompt_out, torch.tensor([0, 90, 200], dtype=torch.int32, device="cuda"))] + step
+    results = (prompt_out,) + results
+    torch.cuda.synchronize()
+    for kern in step:
+        ctx.launch_native(kern, hi=True)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=ctx._streams[0]):
+        for kern in step:
+            ctx.launch_native(kern, hi=True)
+    for turn in range(4):
+        shared.copy_(torch.randn(shared.shape, generator=g, device="cuda"))
+        prompt_in.copy_(torch.randn(prompt_in.shape, generator=g, device="cuda"))
+        torch.cuda.synchronize()
+        for kern in step:
+            ctx.launch_native(kern, hi=True)
+        torch.cuda.synchronize()
+        want = [t.clone() for t in results]
+        for t in results:
+            t.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(results, want):
+            assert torch.equal(a.view(torch.int16), b.view(torch.int16)), turn
+
+
+def test_two_calls_at_once_on_two_streams(env):
+    """Decode steps of two batches on the two streams, each with scratch of its own."""
+    B, ctx, torch = env
+    g = torch.Generator(device="cuda").manual_seed(4)
+    shared = torch.randn((2000, 4, 128), generator=g, device="cuda").to(torch.bfloat16)
+    steps = [_decode_step(B, torch, g, n, 8, 2, 128, shared, 300) for n in (3, 16)]
+    torch.cuda.synchronize()
+    want = []
+    for kernels, results in steps:
+        for kern in kernels:
+            ctx.launch_native(kern, hi=True)
+        torch.cuda.synchronize()
+        want.append([t.clone() for t in results])
+    for _ in range(10):
+        for _, results in steps:
+            for t in results:
+                t.zero_()
+        torch.cuda.synchronize()
+        for pair in zip(*(kernels for kernels, _ in steps)):
+            ctx.launch_native(pair[0], hi=True)
+            ctx.launch_native(pair[1], hi=False)
+        torch.cuda.synchronize()
+        for (_, results), w in zip(steps, want):
+            assert all(torch.equal(a.view(torch.int16), b.view(torch.int16)) for a, b in zip(results, w))
+
+
+def test_footprints_leave_room_for_a_paused_product(env):
+    """A decode step's kernels of few rows, and the 4-bit products, fit beside a paused 256 x 256 GEMM tile, and
+    the prompt's workers are known to the admission rules."""
+    B, ctx, _ = env
+    lds, waves, regs = ctx.kernel_footprint(B.K_GEMM_BF16, 0)
+    room = B.device_info()["lds_bytes_per_cu"] - lds
+    for form in (0, 1):
+        l4, w4, r4 = ctx.kernel_footprint(B.K_GEMV_W4_BF16, form)
+        assert l4 <= room and w4 == 4 and regs + r4 <= 512
+    lp, wp, rp = ctx.kernel_footprint(B.K_ATTN_PROMPT_BF16, 0)
+    assert 2 * lp <= B.device_info()["lds_bytes_per_cu"] and wp == 4 and rp <= 256

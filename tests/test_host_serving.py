@@ -1,0 +1,144 @@
+"""CPU-side checks of the serving operators: logical grids, refusals, layouts.  No kernel runs."""
+import ctypes as C
+
+import numpy as np
+import pytest
+
+from oracle import serving as OS
+
+P = 4096                                                   # any 16-byte aligned address: nothing is read
+
+
+@pytest.fixture(scope="module")
+def B():
+    import paper_2410_07381_amd.binding as B
+    return B
+
+
+def _prompt(B, **other):
+    a = dict(q=P, k=P, v=P, out=P, cu_seqlens=P, total=1000, n_seqs=3, heads=8, kv_heads=2, dim=128, scale=0.0)
+    return B.AttnPromptArgs(**dict(a, **other))
+
+
+def _prefix(B, **other):
+    a = dict(q=P, K=P, V=P, Ko=P, Vo=P, own_len=P, out=P, scratch=P, batch=3, prefix=100, own_cap=50, heads=8,
+             kv_heads=2, dim=128, scale=0.0)
+    return B.AttnPrefixArgs(**dict(a, **other))
+
+
+def _w4(B, **other):
+    a = dict(x=P, W=P, scales=P, zeros=P, y=P, m=4, n=100, k=256, group=64)
+    return B.GemvW4Args(**dict(a, **other))
+
+
+def test_struct_sizes(B):
+    assert C.sizeof(B.AttnPromptArgs) == 80 and C.sizeof(B.AttnPrefixArgs) == 120 and C.sizeof(B.GemvW4Args) == 64
+
+
+@pytest.mark.parametrize("total,seqs,heads", [(1, 1, 1), (127, 1, 2), (128, 1, 2), (1000, 3, 8), (1 << 26, 1 << 20, 8)])
+def test_prompt_grid_has_room_for_every_sequence(B, total, seqs, heads):
+    grid, block = B.logical_grid(B.K_ATTN_PROMPT_BF16, _prompt(B, total=total, n_seqs=seqs, heads=heads, kv_heads=1))
+    assert block == (256, 1, 1) and grid[0] % heads == 0 and grid[1:] == (1, 1)
+    # sequence s has the slots from cu[s] / 128 + s up to the next one's: enough wherever it begins
+    rng = np.random.default_rng(total)
+    cu = np.sort(rng.integers(0, total + 1, min(seqs, 1000) + 1))
+    slots = cu // 128 + np.arange(len(cu))
+    assert (np.diff(slots) >= -(-np.diff(cu) // 128)).all() and (np.diff(slots) <= np.diff(cu) // 128 + 2).all()
+    assert cu[-1] // 128 + seqs <= grid[0] // heads
+
+
+@pytest.mark.parametrize("bad", [
+    dict(q=None), dict(k=None), dict(v=None), dict(out=None), dict(cu_seqlens=None), dict(q=P + 8), dict(k=P + 2),
+    dict(v=P + 4), dict(out=P + 8), dict(cu_seqlens=P + 2), dict(total=0), dict(total=(1 << 30) + 1), dict(n_seqs=0),
+    dict(n_seqs=1 << 21), dict(total=1 << 28),
+    dict(heads=0), dict(kv_heads=0), dict(heads=7), dict(kv_heads=16), dict(dim=96), dict(dim=0), dict(dim=256),
+    dict(ld_q=1016), dict(ld_q=1028), dict(ld_k=255), dict(ld_v=128), dict(ld_out=(1 << 20) + 8), dict(scale=-1.0),
+    dict(scale=float("nan")), dict(scale=float("inf"))])
+def test_prompt_refusals(B, bad):
+    with pytest.raises(B.TallyError) as e:
+        B.logical_grid(B.K_ATTN_PROMPT_BF16, _prompt(B, **bad))
+    assert e.value.status == B.ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("bad", [
+    dict(q=None), dict(out=None), dict(scratch=None), dict(K=None), dict(V=None), dict(Ko=None), dict(Vo=None),
+    dict(own_len=None), dict(q=P + 8), dict(K=P + 8), dict(Vo=P + 8), dict(own_len=P + 1), dict(scratch=P + 8),
+    dict(batch=0), dict(batch=1 << 20), dict(prefix=(1 << 28) + 1), dict(own_cap=(1 << 28) + 1), dict(heads=9),
+    dict(kv_heads=0), dict(dim=80), dict(ld_q=1000), dict(ld_prefix=264 - 16), dict(ld_own=260), dict(ld_out=1016),
+    dict(stride_own=4), dict(stride_own=50 * 256 - 8), dict(scale=-0.5), dict(scale=float("nan"))])
+def test_prefix_refusals(B, bad):
+    with pytest.raises(B.TallyError) as e:
+        B.logical_grid(B.K_ATTN_PREFIX_BF16, _prefix(B, **bad))
+    assert e.value.status == B.ERR_INVALID_ARG
+
+
+def test_prefix_without_a_part_does_not_look_at_its_pointers(B):
+    for a in (_prefix(B, prefix=0, K=None, V=None), _prefix(B, own_cap=0, Ko=None, Vo=None, own_len=None),
+              _prefix(B, prefix=0, own_cap=0, K=None, V=None, Ko=None, Vo=None, own_len=None, scratch=None)):
+        assert B.logical_grid(B.K_ATTN_PREFIX_BF16, a)[0] == (8, 3, 1)
+    assert B.attn_prefix_scratch_bytes(3, 8, 2, 128, 0, 0) == 0
+    assert B.attn_prefix_scratch_bytes(3, 8, 2, 128, 1, 0) == 3 * 8 * 130 * 4
+    for refused in ((0, 8, 2, 128, 1, 1), (3, 8, 3, 128, 1, 1), (3, 8, 2, 72, 1, 1), (1 << 20, 8, 2, 128, 1, 1)):
+        assert B.attn_prefix_scratch_bytes(*refused) == 0
+
+
+@pytest.mark.parametrize("bad", [
+    dict(x=None), dict(W=None), dict(scales=None), dict(y=None), dict(x=P + 8), dict(W=P + 4), dict(m=0), dict(m=17),
+    dict(n=0), dict(k=0), dict(k=252), dict(group=0), dict(group=16), dict(group=96), dict(group=192), dict(ld_x=248),
+    dict(ld_x=260), dict(ld_y=99)])
+def test_w4_refusals(B, bad):
+    with pytest.raises(B.TallyError) as e:
+        B.logical_grid(B.K_GEMV_W4_BF16, _w4(B, **bad))
+    assert e.value.status == B.ERR_INVALID_ARG
+
+
+def test_w4_grid_and_optional_zeros(B):
+    assert B.logical_grid(B.K_GEMV_W4_BF16, _w4(B, zeros=None))[0] == (7, 1, 1)
+    assert B.logical_grid(B.K_GEMV_W4_BF16, _w4(B, n=112, k=8, group=256))[0] == (7, 1, 1)
+
+
+@pytest.mark.parametrize("n,k", [(1, 8), (16, 128), (37, 264), (50, 1000)])
+def test_pack_w4_lays_out_what_the_header_says(B, n, k):
+    import torch
+    rng = np.random.default_rng(n)
+    codes = rng.integers(0, 16, (n, k))
+    W = B.pack_w4(torch.from_numpy(codes))
+    assert W.dtype == torch.int32 and W.shape == (-(-n // 16), -(-k // 128), 64, 4)
+    assert (OS.w4_codes(W.numpy(), n, k) == codes).all()
+    full = OS.w4_codes(W.numpy(), W.shape[0] * 16, W.shape[1] * 128)
+    assert full[n:].sum() == 0 and full[:, k:].sum() == 0
+    t = torch.arange(n * 3, dtype=torch.float32).view(n, 3)
+    g = B.pack_w4_groups(t)
+    assert g.shape == (W.shape[0], 3, 16)
+    assert all(g[r // 16, j, r % 16] == t[r, j] for r in range(n) for j in range(3))
+
+
+def test_the_binding_checks_shapes_and_strides(B):
+    import torch
+    z = lambda *s: torch.zeros(s, dtype=torch.bfloat16)
+    cu = torch.tensor([0, 5], dtype=torch.int32)
+    q, kv = z(5, 4, 64), z(5, 4, 64)
+    B.attn_prompt_bf16(q, kv[:, :2], kv[:, 2:], z(5, 4, 64), cu)
+    for args in ((q, kv[:, :2], kv[:, 1:], q, cu), (q[:, :, ::2], q, q, q, cu), (q, kv[:, ::2], kv[:, ::2], q, cu),
+                 (q, z(1, 2, 64).expand(5, 2, 64), kv[:, :2], q, cu), (q.float(), kv, kv, q, cu),
+                 (q, kv, kv, q, cu.long()), (q, kv, kv, q, cu[:1])):
+        with pytest.raises(AssertionError):
+            B.attn_prompt_bf16(*args)
+    with pytest.raises(AssertionError):
+        B.attn_prompt_bf16(q, kv, kv, z(5, 4, 64), cu, scale=0.0)
+    own, lens = z(3, 7, 2, 64), torch.zeros(3, dtype=torch.int32)
+    room = torch.zeros(B.attn_prefix_scratch_bytes(3, 4, 2, 64, 5, 7), dtype=torch.uint8)
+    q3 = z(3, 4, 64)
+    B.attn_prefix_bf16(q3, kv[:, :2], kv[:, 2:], own, own, lens, z(3, 4, 64), room)
+    for args in ((q3, kv[:, :2], z(5, 2, 64), own, own, lens, q3, room), (q3, kv[:, :2], kv[:, 2:], own, own[:, :6], lens, q3, room),
+                 (q3, kv[:, :2], kv[:, 2:], own, own, lens[:2], q3, room), (q3, kv[:, :2], kv[:, 2:], own, own, lens, q3, room[:-4]),
+                 (q3, kv[:, :2], kv[:, 2:], own[:1].expand(3, 7, 2, 64), own[:1].expand(3, 7, 2, 64), lens, q3, room)):
+        with pytest.raises(AssertionError):
+            B.attn_prefix_bf16(*args)
+    x, y = z(2, 256), z(2, 20)
+    W, s = B.pack_w4(torch.zeros(20, 256, dtype=torch.uint8)), z(2, 2, 16)
+    B.gemv_w4_bf16(x, W, s, y)
+    for args in ((x, W[:1], s, y), (x, W, s[:, :1], y), (x, W, s, y[:1]), (z(2, 512)[:, ::2], W, s, y),
+                 (x[:1].expand(2, 256), W, s, y)):
+        with pytest.raises(AssertionError):
+            B.gemv_w4_bf16(*args)
