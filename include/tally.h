@@ -167,7 +167,8 @@ typedef struct {
 
 /* y[v][r] = sum_k x[v][k] (code[r][k] - zero[r][k / group]) scale[r][k / group], v < m <= 16, r < n.
  * x: m x k, y: m x n, scales: bf16; codes 0 .. 15; zeros: bytes 0 .. 128, or NULL for 8 everywhere.
- * k a multiple of 8; group 32, 64 or a multiple of 128; the last group may be short.  x finite
+ * n at most 2^26, k a multiple of 8 and at most 2^24; group 32, 64 or a multiple of 128 up to 2^20; the last group
+ * may be short.  x finite
  * (an infinity gives NaN).  Sums are held in fp32 and rounded once.
  * Layout of the weights, with N = ceil(n / 16), B = ceil(k / 128), G = ceil(k / group):
  *   W: N x B tiles of 64 x 4 words; word i of entry 16 q + r of tile (t, b) holds the codes of row 16 t + r,
@@ -175,7 +176,7 @@ typedef struct {
  *   scales, zeros: N x G x 16, entry (t, g, r) for row 16 t + r.
  * What stands for rows and columns that do not exist does not matter.  x and W 16-byte aligned, ld_x (elements
  * between vectors, a multiple of 8) and ld_y 0: dense, at most 2^24.
- * Logical grid: ceil(n / 16) blocks of 16 rows. */
+ * Logical grid: blocks of 16, 32, 48 or 64 rows, by m and n (tally_logical_grid). */
 typedef struct {
   const uint16_t *x; const uint32_t *W; const uint16_t *scales; const uint8_t *zeros; uint16_t *y;
   uint32_t m, n, k, group, ld_x, ld_y;

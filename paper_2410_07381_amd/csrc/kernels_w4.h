@@ -12,6 +12,10 @@
 // reads with one 16-byte load a lane; word i of lane 16 q + r holds weights 32 i + 8 q to 32 i + 8 q + 7
 // of row r, the even ones in its low half.  So MFMA i of a tile takes 32 neighbouring weights of each
 // row, which always belong to one group.
+//
+// The eight waves of a workgroup share the tiles of a row of tiles and join their sums in LDS.  Which wave takes
+// a tile and in what order sums are added depends on k alone, so a result's bits depend neither on the
+// number of vectors nor on the variant.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -23,67 +27,217 @@
 
 namespace tally {
 
-constexpr uint32_t kW4Rows = 16, kW4Block = 128, kW4Vectors = 16;
+constexpr uint32_t kW4Rows = 16, kW4Block = 128, kW4Vectors = 16, kW4MaxGroup = 1u << 20;
+constexpr int kW4Waves = 8;
+constexpr uint32_t kW4Staged = 24 * 1024;                  // bytes of LDS for the vectors, where they go there
+constexpr uint32_t kW4LongK = 8192;                        // ... from this k on
+constexpr uint32_t kW4Piece = 1024;                        // bytes of a vector that one direct load brings
 
-// SUB: MFMAs of a tile that share a scale (groups of 32, of 64, of 128 and more)
+// bytes from a vector to the next in LDS: whole pieces, and a step that spreads them over the banks
+__host__ __device__ constexpr uint32_t w4_pitch(uint32_t k) { return (k * 2 + kW4Piece - 1) / kW4Piece * kW4Piece + 64; }
+
+// Rows of tiles that a workgroup takes.  It reads x once for all of them (from the L2s, 24 bytes a clock and compute
+// unit where all of them read the same): with many vectors that is more than the codes, so fewer workgroups
+// with more rows each are faster, as long as each of the 256 compute units has the same number of them.  Cost of
+// a workgroup: its rows, and a quarter of a row per vector; of equals the one with more rows.  More than 2 (3, 4)
+// rows did not pay with 4 or 5 (8, 16) vectors, and with 1 or 2 vectors only large products gain from a second.
+// us by rows, k = 4096, groups of 128: 1 vector, n = 11008 6.7 7.1 7.2, 50256 25.4 20.6 21.4; 4 vectors, 11008 8.3 7.5
+// 7.3 8.3, 16384 10.0 8.1 9.8 9.1; 16 vectors, 4096 5.9 6.7 7.4 8.3, 11008 13.8 11.0 8.0 8.8, 16384 17.5 11.1 12.6
+// 9.5, 50256 52.4 32.6 28.1 26.9.
+inline uint32_t w4_rows(uint32_t m, uint32_t n) {
+  const uint32_t tiles = (n + kW4Rows - 1) / kW4Rows, most = m <= 6 ? 2 : m <= 10 ? 3 : 4;
+  if (m <= 2) return tiles > 1024 ? 2 : 1;
+  uint32_t best = 1;
+  uint64_t least = ~0ull;
+  for (uint32_t r = 1; r <= most; ++r) {
+    const uint64_t groups = (tiles + r - 1) / r, cost = (groups + 255) / 256 * (4 * r + m);
+    if (cost <= least) { least = cost; best = r; }
+  }
+  return best;
+}
+// x goes to LDS where it fits and a wave has many tiles to take one after the other: the loads of the next
+// are then asked for while it waits for none of x.  (us, straight from the L2s / so, 1 vector: 4096 x 11008, groups of
+// 64 with zero points, 9.1 / 7.8; of 128 7.5 / 6.4; 11008 x 11008 13.4 / 12.8; but 11008 x 1024 3.4 / 3.8.)
+inline bool w4_staged(const tally_gemv_w4_args &a) {
+  return a.k >= kW4LongK && (uint64_t)a.m * w4_pitch(a.k) <= kW4Staged && w4_rows(a.m, a.n) == 1;
+}
+
+// One tile of 16 rows by 128 weights, as loaded.  SUB: MFMAs of a tile that share a scale (groups of 32, of
+// 64, of 128 and more).  Scales and zero points: a lane has those of row l % 16 and of the group that the
+// quarter l / 16 of the tile lies in.
 template <int SUB>
-struct GemvW4BodyT {
+struct W4Tile {
+  uint4 w;
+  uint32_t scale, zero;
+#ifdef __HIP_DEVICE_COMPILE__
+  struct From {
+    buf_t w, scales, zeros;
+    uint32_t inverse;                                      // 2^31 over the tiles of a group, rounded up
+    bool has_zeros;
+    __device__ __forceinline__ From(const tally_gemv_w4_args &a, uint32_t rows, uint32_t blocks, uint32_t groups)
+        : w(make_buf(reinterpret_cast<const unsigned char *>(a.W) + (uint64_t)rows * blocks * 1024, blocks * 1024)),
+          scales(make_buf(a.scales + (uint64_t)rows * groups * 16, groups * 32)),
+          zeros(make_buf(a.zeros ? a.zeros + (uint64_t)rows * groups * 16 : nullptr, a.zeros ? groups * 16 : 0)),
+          inverse(SUB == 4 ? (0x7FFFFFFFu + a.group / kW4Block) / (a.group / kW4Block) : 0u), has_zeros(a.zeros != nullptr) {}
+  };
+  // (past the last block nothing is read, and zeros come back)
+  __device__ __forceinline__ void load(const From &f, uint32_t b, uint32_t lane) {
+    w = buf_ld16(f.w, lane * 16, b * 1024);
+    const uint32_t at = SUB == 4 ? __umulhi(2 * b, f.inverse) * 16 + (lane & 15)
+                                 : b * (4 / SUB) * 16 + (SUB == 1 ? lane : (lane >> 5) * 16 + (lane & 15));
+    scale = __builtin_amdgcn_raw_buffer_load_b16(f.scales, at * 2, 0, 0);
+    zero = f.has_zeros ? __builtin_amdgcn_raw_buffer_load_b8(f.zeros, at, 0, 0) : 8u;
+  }
+  // acc += this tile's rows times the vectors; x(i): the vectors' 32 elements for MFMA i
+  template <class X>
+  __device__ __forceinline__ void add(f32x4_t &acc, uint32_t lane, X x) const {
+    const uint32_t word[4] = {w.x, w.y, w.z, w.w};
+    // (in registers, or there would be an AND and an OR: an instruction has room for one constant)
+    uint32_t mask = 0x000F000Fu, base = 0x43004300u;
+    asm("" : "+s"(mask), "+v"(base));
+    // scale in the upper half, -(128 + zero) in the lower
+    const uint32_t both = scale << 16 | __float_as_uint(-(float)(128u + zero)) >> 16;
+#pragma unroll
+    for (int g = 0; g < 4; g += SUB) {
+      const uint32_t u = SUB == 4 ? both : (uint32_t)__builtin_amdgcn_ds_bpermute((g * 16 + (lane & 15)) * 4, (int)both);
+      const uint32_t cc = __builtin_amdgcn_perm(u, u, 0x01000100u);
+      const bf16x8_t less = __builtin_bit_cast(bf16x8_t, make_uint4(cc, cc, cc, cc));
+      f32x4_t part = {0.f, 0.f, 0.f, 0.f}, off = {0.f, 0.f, 0.f, 0.f};   // (two chains: an MFMA waits for the one before)
+#pragma unroll
+      for (int i = g; i < g + SUB; ++i) {
+        const bf16x8_t xv = x(i);
+        uint32_t q[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) q[j] = (word[i] >> (4 * j) & mask) | base;
+        off = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xv, less, off, 0, 0, 0);
+        part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xv, __builtin_bit_cast(bf16x8_t, make_uint4(q[0], q[1], q[2], q[3])), part, 0, 0, 0);
+      }
+      const float s = bf16_hi(u);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] = __builtin_fmaf(s, part[e] + off[e], acc[e]);
+    }
+  }
+#endif
+};
+
+// What the variants have in common.  ROWS: rows of tiles of a block.
+template <int ROWS_>
+struct W4Base {
   using Args = tally_gemv_w4_args;
-  static constexpr int THREADS = 256;
-  static constexpr int MIN_WAVES = 4;
-  static constexpr unsigned DYN_LDS = 0;
+  static constexpr int ROWS = ROWS_, THREADS = 64 * kW4Waves;
   static constexpr bool YIELDS = false;
   static constexpr bool RANGE = false;
-  static constexpr bool END_BARRIER = true;                // (the waves' sums are joined in LDS)
+  static constexpr bool END_BARRIER = true;                // (LDS holds the waves' sums, and x)
+  // The waves' sums, joined in LDS, one row of tiles at a time; lane 16 q + r, element e: vector 4 q + e, row r
+  static __device__ __forceinline__ void store(const Args &a, const f32x4_t (&acc)[ROWS], uint32_t block, uint32_t wave, uint32_t lane) {
+    __shared__ f32x4_t s_acc[kW4Waves][64];
+#pragma unroll
+    for (int o = 0; o < ROWS; ++o) {
+      if (o) __syncthreads();
+      s_acc[wave][lane] = acc[o];
+      __syncthreads();
+      const uint32_t v = threadIdx.x >> 4, l = (v >> 2) * 16 + (threadIdx.x & 15), e = v & 3;
+      const uint32_t row = (block * ROWS + o) * kW4Rows + (threadIdx.x & 15);
+      if (v < a.m && row < a.n) {
+        float y = 0.f;
+#pragma unroll
+        for (int w = 0; w < kW4Waves; ++w) y += s_acc[w][l][e];
+        a.y[(uint64_t)v * (a.ld_y ? a.ld_y : a.n) + row] = f32_to_bf16(y);
+      }
+    }
+  }
+};
+
+// x in LDS, straight from memory; behind its loads each wave keeps two tiles of codes on their way.
+template <int SUB>
+struct GemvW4StagedT : W4Base<1> {
+  static constexpr int MIN_WAVES = 7;                      // 72 registers: two waves fit beside a paused GEMM tile
+  static constexpr unsigned DYN_LDS = kW4Staged - 2048;
+  static constexpr int DEEP = 2;
   static __device__ __forceinline__ void run(const Args &a, uint32_t bx, uint32_t, uint32_t) { run_t(a, bx); }
   static __device__ __forceinline__ void run_be(const Args &a, uint32_t bx, uint32_t, uint32_t) { run_t(a, bx); }
   static __device__ __forceinline__ void run_t(const Args &a, uint32_t tile) {
 #ifdef __HIP_DEVICE_COMPILE__
-    __shared__ f32x4_t s_acc[4][64];
-    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint32_t col = lane & 15, quarter = lane >> 4;
+    extern __shared__ __align__(1024) unsigned char tally_dyn_lds[];
+    uint32_t lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t blocks = (a.k + kW4Block - 1) / kW4Block, groups = (a.k + a.group - 1) / a.group;
-    const uint32_t LDX = a.ld_x ? a.ld_x : a.k;
-    const uint4 *W = reinterpret_cast<const uint4 *>(a.W) + (uint64_t)tile * blocks * 64 + lane;
-    const buf_t scales = make_buf(a.scales + (uint64_t)tile * groups * 16, groups * 32);
-    const buf_t zeros = make_buf(a.zeros ? a.zeros + (uint64_t)tile * groups * 16 : nullptr, a.zeros ? groups * 16 : 0);
-    const buf_t x = make_buf(a.x, 0x7fffffff);
-    const uint32_t xrow = col < a.m ? (col * LDX + quarter * 8) * 2 : 0x80000000u;
-    f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
-    for (uint32_t b = wave; b < blocks; b += 4) {
-      const uint4 w = W[(uint64_t)b * 64];
-      const uint32_t word[4] = {w.x, w.y, w.z, w.w};
+    const uint32_t LDX = a.ld_x ? a.ld_x : a.k, pitch = w4_pitch(a.k), pieces = (a.k * 2 + kW4Piece - 1) / kW4Piece;
+    const uint32_t lds = (uint32_t)(uintptr_t)(lptr_t)tally_dyn_lds;
+    for (uint32_t i = wave; i < a.m * pieces; i += kW4Waves) {
+      const uint32_t v = i / pieces, c = i % pieces;
+      const uint64_t p = (uint64_t)(uintptr_t)(a.x + (uint64_t)v * LDX);
+      const u32x4_t b = {(uint32_t)p, (uint32_t)(p >> 32) & 0xFFFFu, a.k * 2, 0x00027000u};
+      // (as in Flash::ask: what is past the vector's end is left as zeros)
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                   ::"s"(lds + v * pitch + c * kW4Piece), "v"(lane * 16 + c * kW4Piece), "s"(b) : "memory");
+    }
+    const typename W4Tile<SUB>::From from(a, tile, blocks, groups);
+    W4Tile<SUB> t[DEEP];
 #pragma unroll
-      for (int g = 0; g < 4; g += SUB) {
-        const uint32_t k0 = b * kW4Block + g * 32, at = k0 / a.group;
-        const float s = bf16_lo(__builtin_amdgcn_raw_buffer_load_b16(scales, (at * 16 + col) * 2, 0, 0));
-        const uint32_t z = a.zeros ? __builtin_amdgcn_raw_buffer_load_b8(zeros, at * 16 + col, 0, 0) : 8u;
-        const uint32_t c = __float_as_uint(-(float)(128u + z)) >> 16, cc = c << 16 | c;
-        f32x4_t part = {0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < DEEP; ++j) t[j].load(from, wave + j * kW4Waves, lane);
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * DEEP) : "memory");   // (at least so many loads are behind those of x)
+    __syncthreads();
+    const uint32_t col = lane & 15, at = lds + (col < a.m ? col : 0u) * pitch + (lane >> 4) * 16;
+    f32x4_t acc[1] = {{0.f, 0.f, 0.f, 0.f}};
+    for (uint32_t b = wave; b < blocks; b += DEEP * kW4Waves) {
 #pragma unroll
-        for (int i = g; i < g + SUB; ++i) {
-          // (8 elements of x at a time: k is a multiple of 8, and past it x counts as zero)
-          const uint32_t k1 = b * kW4Block + i * 32;
-          const uint32_t off = k1 + quarter * 8 < a.k ? xrow + k1 * 2 : 0x80000000u;
-          const bf16x8_t xv = __builtin_bit_cast(bf16x8_t, buf_ld16(x, off, 0));
-          uint32_t q[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) q[j] = (word[i] >> (4 * j) & 0x000F000Fu) | 0x43004300u;
-          part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xv, __builtin_bit_cast(bf16x8_t, make_uint4(q[0], q[1], q[2], q[3])), part, 0, 0, 0);
-          part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xv, __builtin_bit_cast(bf16x8_t, make_uint4(cc, cc, cc, cc)), part, 0, 0, 0);
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[e] = __builtin_fmaf(s, part[e], acc[e]);
+      for (int j = 0; j < DEEP; ++j) {
+        const uint32_t mine = b + j * kW4Waves;
+        if (mine < blocks)
+          t[j].add(acc[0], lane, [&](int i) {
+            typedef const __attribute__((address_space(3))) bf16x8_t *frag_t;
+            return *(frag_t)(at + mine * (kW4Block * 2) + i * 64);
+          });
+        t[j].load(from, mine + DEEP * kW4Waves, lane);
       }
     }
-    s_acc[wave][lane] = acc;
-    __syncthreads();
-    // lane 16 q + r, element e: vector 4 q + e, row r
-    const uint32_t v = threadIdx.x >> 4, r = threadIdx.x & 15, from = (v >> 2) * 16 + r, e = v & 3, row = tile * kW4Rows + r;
-    if (v < a.m && row < a.n) {
-      const float y = (s_acc[0][from][e] + s_acc[1][from][e]) + (s_acc[2][from][e] + s_acc[3][from][e]);
-      a.y[(uint64_t)v * (a.ld_y ? a.ld_y : a.n) + row] = f32_to_bf16(y);
+    store(a, acc, tile, wave, lane);
+#endif
+  }
+};
+
+// x as each wave needs it, from the L2s, together with the codes of one tile of each row.
+template <int SUB, int ROWS>
+struct GemvW4T : W4Base<ROWS> {
+  using Args = tally_gemv_w4_args;
+  static constexpr int MIN_WAVES = ROWS <= 2 ? 8 : ROWS == 3 ? 7 : 4;   // (up to 72 registers: two waves fit beside a paused GEMM tile)
+  static constexpr unsigned DYN_LDS = 0;
+  static __device__ __forceinline__ void run(const Args &a, uint32_t bx, uint32_t, uint32_t) { run_t(a, bx); }
+  static __device__ __forceinline__ void run_be(const Args &a, uint32_t bx, uint32_t, uint32_t) { run_t(a, bx); }
+  static __device__ __forceinline__ void run_t(const Args &a, uint32_t block) {
+#ifdef __HIP_DEVICE_COMPILE__
+    uint32_t lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t blocks = (a.k + kW4Block - 1) / kW4Block, groups = (a.k + a.group - 1) / a.group;
+    const uint32_t tiles = (a.n + kW4Rows - 1) / kW4Rows;
+    const uint32_t LDX = a.ld_x ? a.ld_x : a.k, col = lane & 15, k0 = (lane >> 4) * 8;
+    // (a vector that does not exist lies past the buffer's end, and so does what is past the end of one)
+    const buf_t x = make_buf(a.x, 0x7fffffff);
+    const uint32_t xrow = col < a.m ? (col * LDX + k0) * 2 : 0x80000000u;
+    f32x4_t acc[ROWS];
+#pragma unroll
+    for (int o = 0; o < ROWS; ++o) acc[o] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (uint32_t b = wave; b < blocks; b += kW4Waves) {
+      W4Tile<SUB> t[ROWS];
+      uint4 xv[4];
+#pragma unroll
+      for (int o = 0; o < ROWS; ++o) {
+        const uint32_t tile = block * ROWS + o;
+        const typename W4Tile<SUB>::From from(a, tile < tiles ? tile : tiles - 1, blocks, groups);
+        t[o].load(from, b, lane);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t k1 = b * kW4Block + i * 32;
+        xv[i] = buf_ld16(x, k1 + k0 < a.k ? xrow + k1 * 2 : 0x80000000u, 0);
+      }
+#pragma unroll
+      for (int o = 0; o < ROWS; ++o) t[o].add(acc[o], lane, [&](int i) { return __builtin_bit_cast(bf16x8_t, xv[i]); });
     }
+    W4Base<ROWS>::store(a, acc, block, wave, lane);
 #endif
   }
 };

@@ -573,14 +573,14 @@ int grid_prefix(const void *p, tally_dim3 *g, tally_dim3 *b) {
 }
 int grid_gemv_w4(const void *p, tally_dim3 *g, tally_dim3 *b) {
   auto *a = static_cast<const tally_gemv_w4_args *>(p);
-  if (!a->x || !a->W || !a->scales || !a->y || !a->m || a->m > kW4Vectors || !a->n || !a->k || a->n > (1u << 30) ||
-      a->k > (1u << 24) || a->k % 8 || !a->group || a->group > (1u << 24) || (a->group != 32 && a->group != 64 && a->group % 128))
+  if (!a->x || !a->W || !a->scales || !a->y || !a->m || a->m > kW4Vectors || !a->n || !a->k || a->n > (1u << 26) ||
+      a->k > (1u << 24) || a->k % 8 || !a->group || a->group > kW4MaxGroup || (a->group != 32 && a->group != 64 && a->group % 128))
     return TALLY_ERR_INVALID_ARG;
   if (!aligned16(a->x) || !aligned16(a->W) || (a->ld_x && (a->ld_x < a->k || a->ld_x % 8 || a->ld_x > (1u << 24))) ||
       (a->ld_y && a->ld_y < a->n))
     return TALLY_ERR_INVALID_ARG;
-  *g = {cdiv(a->n, kW4Rows), 1, 1};
-  *b = kBlock256;
+  *g = {cdiv(a->n, kW4Rows * w4_rows(a->m, a->n)), 1, 1};
+  *b = {64 * kW4Waves, 1, 1};
   return TALLY_OK;
 }
 hipError_t launch_native_prefix(hipStream_t s, const void *args, tally_dim3, uint32_t how) {
@@ -603,33 +603,58 @@ hipError_t footprint_prefix(uint32_t *lds_bytes, uint32_t *waves, uint32_t *regs
   *regs_per_lane = ((uint32_t)attr.numRegs + 7u) & ~7u;
   return hipSuccess;
 }
-// 4-bit products: one kernel for each way that groups divide a tile
+// 4-bit products: a kernel for each way that groups divide a tile, and for each number of rows and x in LDS
+#define W4_VARIANTS(SUB, X) X(SUB * 5, GemvW4T<1 << SUB, 1>) X(SUB * 5 + 1, GemvW4T<1 << SUB, 2>) X(SUB * 5 + 2, GemvW4T<1 << SUB, 3>) \
+  X(SUB * 5 + 3, GemvW4T<1 << SUB, 4>) X(SUB * 5 + 4, GemvW4StagedT<1 << SUB>)
+#define W4_ALL(X) W4_VARIANTS(0, X) W4_VARIANTS(1, X) W4_VARIANTS(2, X)
 uint32_t w4_range(const void *args) {
   tally_gemv_w4_args a;
   memcpy(&a, args, sizeof(a));
-  return a.group == 32 ? 0 : a.group == 64 ? 1 : 2;
+  return (a.group == 32 ? 0 : a.group == 64 ? 5 : 10) + (w4_staged(a) ? 4 : w4_rows(a.m, a.n) - 1);
 }
 uint32_t w4_choice(const void *args, uint32_t, uint64_t *) { return w4_range(args); }
 hipError_t launch_native_w4(hipStream_t s, const void *args, tally_dim3 g, uint32_t how) {
-  switch (w4_range(args)) {
-    case 0: return launch_native_t<GemvW4BodyT<1>>(s, args, g, how);
-    case 1: return launch_native_t<GemvW4BodyT<2>>(s, args, g, how);
-    default: return launch_native_t<GemvW4BodyT<4>>(s, args, g, how);
-  }
+#define W4_CASE(i, ...) case i: return launch_native_t<__VA_ARGS__>(s, args, g, how);
+  switch (w4_range(args)) { W4_ALL(W4_CASE) }
+#undef W4_CASE
+  return hipErrorInvalidValue;
 }
 hipError_t launch_sliced_w4(hipStream_t s, const void *args, uint32_t nblocks, const SliceCtl &c) {
-  switch (w4_range(args)) {
-    case 0: return launch_sliced_t<GemvW4BodyT<1>>(s, args, nblocks, c);
-    case 1: return launch_sliced_t<GemvW4BodyT<2>>(s, args, nblocks, c);
-    default: return launch_sliced_t<GemvW4BodyT<4>>(s, args, nblocks, c);
-  }
+#define W4_CASE(i, ...) case i: return launch_sliced_t<__VA_ARGS__>(s, args, nblocks, c);
+  switch (w4_range(args)) { W4_ALL(W4_CASE) }
+#undef W4_CASE
+  return hipErrorInvalidValue;
 }
 hipError_t launch_ptb_w4(hipStream_t s, const void *args, const PtbCtl &c) {
-  switch (w4_range(args)) {
-    case 0: return launch_ptb_t<GemvW4BodyT<1>>(s, args, c);
-    case 1: return launch_ptb_t<GemvW4BodyT<2>>(s, args, c);
-    default: return launch_ptb_t<GemvW4BodyT<4>>(s, args, c);
+#define W4_CASE(i, ...) case i: return launch_ptb_t<__VA_ARGS__>(s, args, c);
+  switch (w4_range(args)) { W4_ALL(W4_CASE) }
+#undef W4_CASE
+  return hipErrorInvalidValue;
+}
+// What a worker occupies, and how many are resident at once: the most and the fewest of any variant's, which
+// stand for all of them.
+hipError_t footprint_w4(uint32_t *lds_bytes, uint32_t *waves, uint32_t *regs_per_lane) {
+  *lds_bytes = *waves = *regs_per_lane = 0;
+  hipError_t e = hipSuccess;
+  uint32_t f[3];
+#define W4_MOST(i, ...)                                                                                    \
+  if (e == hipSuccess && (e = footprint_t<__VA_ARGS__>(&f[0], &f[1], &f[2])) == hipSuccess) {              \
+    if (f[0] > *lds_bytes) *lds_bytes = f[0];                                                              \
+    if (f[1] > *waves) *waves = f[1];                                                                      \
+    if (f[2] > *regs_per_lane) *regs_per_lane = f[2];                                                      \
   }
+  W4_ALL(W4_MOST)
+#undef W4_MOST
+  return e;
+}
+int occupancy_w4(int *blocks_per_cu) {
+  int rc = TALLY_OK, n = 0;
+  *blocks_per_cu = 0x7fffffff;
+#define W4_LEAST(i, ...)                                                                                   \
+  if (rc == TALLY_OK && (rc = occupancy_t<__VA_ARGS__>(&n)) == TALLY_OK && n < *blocks_per_cu) *blocks_per_cu = n;
+  W4_ALL(W4_LEAST)
+#undef W4_LEAST
+  return rc;
 }
 
 // One operator, a kernel for each width of a head.  No worker occupies more than `Wide`'s.
@@ -715,6 +740,7 @@ struct TakesTogether<Body, std::enable_if_t<Body::TOGETHER>> : std::true_type {}
    {footprint_native_t<Wide>, footprint_native_t<Narrow>}, dim_choice<Wide, Narrow>, dim_range<Wide, Narrow>, \
    nullptr, nullptr, nullptr, false, false}
 
+#define W4_FOOT(i, ...) footprint_native_t<__VA_ARGS__>,
 const KernelOps kOps[TALLY_K_COUNT] = {
     OPS(SaxpyBody, "saxpy", grid_saxpy),
     OPS(ReduceSumBody, "reduce_sum", grid_reduce_sum),
@@ -741,8 +767,7 @@ const KernelOps kOps[TALLY_K_COUNT] = {
      {footprint_prefix<128, false>, footprint_prefix<128, true>, footprint_prefix<64, false>, footprint_prefix<64, true>},
      prefix_choice, nullptr, nullptr, nullptr, nullptr, false, false},
     {"gemv_w4_bf16", sizeof(tally_gemv_w4_args), true, grid_gemv_w4, launch_native_w4, launch_sliced_w4, launch_ptb_w4,
-     nullptr, occupancy_t<GemvW4BodyT<1>>, pause_fraction_t<GemvW4BodyT<1>>, footprint_t<GemvW4BodyT<1>>,
-     {footprint_native_t<GemvW4BodyT<1>>, footprint_native_t<GemvW4BodyT<2>>, footprint_native_t<GemvW4BodyT<4>>},
+     nullptr, occupancy_w4, pause_fraction_t<GemvW4T<1, 1>>, footprint_w4, {W4_ALL(W4_FOOT)},
      w4_choice, w4_range, nullptr, nullptr, nullptr, false, false},
 };
 

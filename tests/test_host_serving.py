@@ -92,6 +92,14 @@ def test_w4_refusals(B, bad):
     assert e.value.status == B.ERR_INVALID_ARG
 
 
+@pytest.mark.parametrize("m,n,rows", [(1, 1, 1), (1, 16384, 1), (2, 16385, 2), (4, 4096, 1), (4, 11008, 2), (8, 11008, 3), (8, 16384, 2),
+                                      (16, 4096, 1), (16, 11008, 3), (16, 16384, 4), (16, 50256, 4), (5, 50257, 2)])
+def test_w4_rows_of_tiles_by_vectors_and_rows(B, m, n, rows):
+    """The rule's measured best: workgroups of as many rows as keep x from being read again and again, with the
+    same number of workgroups on every compute unit."""
+    assert B.logical_grid(B.K_GEMV_W4_BF16, _w4(B, m=m, n=n))[0] == (-(-n // (16 * rows)), 1, 1)
+
+
 def test_w4_grid_and_optional_zeros(B):
     assert B.logical_grid(B.K_GEMV_W4_BF16, _w4(B, zeros=None))[0] == (7, 1, 1)
     assert B.logical_grid(B.K_GEMV_W4_BF16, _w4(B, n=112, k=8, group=256))[0] == (7, 1, 1)
