@@ -44,12 +44,15 @@ struct Flash {
   static constexpr int L = PLACE / 1024 / WAVES;           // direct loads per wave and item
   static constexpr uint32_t RPL = 1024 / ROWB;             // tokens per load
   static constexpr unsigned LDS = PLACE * NS;
+  static constexpr uint32_t BEFORE = (L - 1) * 1024;       // (see ask)
   static constexpr int MK = ROWS == 32 ? 16 : 32;          // k of one MFMA
   static constexpr int QK = DIM / MK, PV = TOK / MK;
   static constexpr int TT = TOK / ROWS, DT = DIM / ROWS;   // blocks of tokens and of dims
   static constexpr int AN = ROWS == 32 ? 16 : 4;           // accumulators of a block
+  static constexpr int PAIRS = TT * AN / 2;                // of a lane's scores in a tile
   static_assert((DIM == 64 || DIM == 128) && (ROWS == 32 || ROWS == 16), "shapes that the maps below know");
   static_assert(L >= 1 && L * 1024 * WAVES == (int)PLACE && NS >= 3, "whole loads, two items on their way");
+  static_assert(BEFORE < 4096, "an immediate has 12 bits");
 
 #ifdef __HIP_DEVICE_COMPILE__
   typedef typename std::conditional<ROWS == 32, f32x16_t, f32x4_t>::type acc_t;
@@ -67,8 +70,7 @@ struct Flash {
   uint32_t k_at, v_at;                                     // a lane's place in K's and V's fragment reads
   bf16x8_t q[QK];
   acc_t acc[DT];
-  acc_t s[TT];                                             // scores, then p
-  float m, l;
+  float m, l, ref;                                         // ref: m, or 0 while a row has seen nothing
 
   // 16-byte chunk c of token t stands at chunk c xor swz(t): different for 16 neighbouring tokens (of
   // dim 64, whose rows are half as long, for every second one), and its high bits for four
@@ -103,17 +105,17 @@ struct Flash {
 #pragma unroll
     for (int d = 0; d < DT; ++d) acc[d] = acc_t{};
     m = -INFINITY;
-    l = 0.f;
+    l = ref = 0.f;
   }
   __device__ __forceinline__ Src source(const uint16_t *at, uint32_t tokens, uint32_t ld) const {
     Src r;
-    r.at = (const unsigned char *)at;
+    r.at = (const unsigned char *)at - BEFORE;
     r.left = tokens;
     r.ld = ld * 2;
 #pragma unroll
     for (int n = 0; n < L; ++n) {
       const uint32_t row = (wave * L + n) * RPL + lane / (ROWB / 16), c = lane % (ROWB / 16);
-      r.voff[n] = row * r.ld + ((c ^ swz(row)) << 4);
+      r.voff[n] = row * r.ld + ((c ^ swz(row)) << 4) + (BEFORE - n * 1024u);
     }
     return r;
   }
@@ -128,36 +130,44 @@ struct Flash {
   // the next item of a source to a place of the ring; past its end nothing is moved and zeros are left
   __device__ __forceinline__ void ask(Src &r, uint32_t place) const {
     // (Assembly: knowing of the loads, the compiler waits for all of them before any transposing read.  They
-    // have no destination in registers, sync() waits for them, and nothing else in these kernels uses m0.)
+    // have no destination in registers, sync() waits for them, and nothing else in these kernels uses m0.  The
+    // immediate separates a wave's loads in LDS; it moves the global address too, which is taken out of
+    // the lane's offset, and so that none is negative the buffer starts BEFORE bytes early.)
     const uint32_t n = r.left < (uint32_t)TOK ? r.left : (uint32_t)TOK;
     const uint64_t p = (uint64_t)(uintptr_t)r.at;
-    const u32x4_t b = {(uint32_t)p, (uint32_t)(p >> 32) & 0xFFFFu, n * r.ld, 0x00027000u};
-    uint32_t to = lds + place * PLACE + wave * (L * 1024u);
+    const u32x4_t b = {(uint32_t)p, (uint32_t)(p >> 32) & 0xFFFFu, n * r.ld + BEFORE, 0x00027000u};
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0" ::"s"(lds + place * PLACE + wave * (L * 1024u)) : "memory");
 #pragma unroll
     for (int j = 0; j < L; ++j)
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-                   ::"s"(to + j * 1024u), "v"(r.voff[j]), "s"(b) : "memory");
+      asm volatile("buffer_load_dwordx4 %0, %1, 0 offen offset:%2 lds" ::"v"(r.voff[j]), "s"(b), "n"(j * 1024) : "memory");
     r.at += (uint64_t)TOK * r.ld;
     r.left -= n;
   }
-  // item i is there for everyone, and everyone is done with item i - 1
-  __device__ __forceinline__ void sync() const {
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((NS - 2) * L) : "memory");
+  // all but the last LEFT loads of every wave are there, and every wave is done with what it has read
+  template <int LEFT>
+  static __device__ __forceinline__ void sync() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(LEFT) : "memory");
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
+  }
+  // (the compiler would wait for q in the loop, counting none of ask()'s loads)
+  __device__ __forceinline__ void wait_q() {
+#pragma unroll
+    for (int k = 0; k < QK; ++k) asm volatile("" : "+v"(q[k]));
+  }
+  // (what is computed from it is not kept beside what another loop has computed)
+  static __device__ __forceinline__ uint32_t opaque(uint32_t v) {
+    asm volatile("" : "+v"(v));
+    return v;
   }
 
   // which token of a tile element e of block t stands for, without the lane's own part
   static constexpr uint32_t token(int t, int e) { return ROWS == 32 ? 32 * t + 8 * (e / 4) + e % 4 : 16 * t + e; }
 
-  // scores of a tile and the softmax's step.  c: the scale times log2(e); lim: the lane's row may
-  // attend to tokens of the tile below it (MASK only).
+  // S^T of the tile whose K stands at `at`.  MASK: a lane's row attends to tokens of the tile below `lim` alone.
   template <bool MASK>
-  __device__ __forceinline__ void scores(uint32_t place, float c, int32_t lim) {
+  __device__ __forceinline__ void products(acc_t (&s)[TT], uint32_t at, uint32_t k_at, int32_t lim) const {
     typedef const __attribute__((address_space(3))) bf16x8_t *frag_t;
-    const uint32_t at = lds + place * PLACE;
-    uint32_t k_at = this->k_at;
-    if constexpr (MASK) asm volatile("" : "+v"(k_at));     // (its eight variants are not kept beside the other loop's)
 #pragma unroll
     for (int t = 0; t < TT; ++t) s[t] = acc_t{};
 #pragma unroll
@@ -172,17 +182,25 @@ struct Flash {
 #pragma unroll
         for (int e = 0; e < AN; ++e) s[t][e] = (int32_t)token(t, e) < left ? s[t][e] : -INFINITY;
     }
+  }
+  // a lane's largest score
+  static __device__ __forceinline__ float largest(const acc_t (&s)[TT]) {
     float top = s[0][0];
 #pragma unroll
     for (int t = 0; t < TT; ++t)
 #pragma unroll
       for (int e = 0; e < AN; ++e) top = fmaxf(top, s[t][e]);
-    top = over_row<MaxOp>(top) * c;
-    // A maximum that has grown by less than 2^8 is left as it is: p then stays below 2^8, which
-    // costs nothing in floating point, and acc is rarely rescaled.
+    return top;
+  }
+  // The running maximum follows that of a tile (c: the scale times log2(e)).  One that has grown by less than 2^8 is
+  // left as it is: p then stays below 2^8, which costs nothing in floating point, and acc is rarely rescaled (nor
+  // do the lanes of a row have to exchange theirs).
+  __device__ __forceinline__ void follow(float top, float c) {
+    top *= c;
     if (__builtin_amdgcn_ballot_w64(top > m + 8.f) != 0) {
-      const float now = fmaxf(m, top);
-      const float a = exp2(m - (now == -INFINITY ? 0.f : now));
+      const float now = fmaxf(m, over_row<MaxOp>(top));
+      ref = now == -INFINITY ? 0.f : now;
+      const float a = exp2(m - ref);
       m = now;
       l *= a;
 #pragma unroll
@@ -190,17 +208,20 @@ struct Flash {
 #pragma unroll
         for (int e = 0; e < AN; ++e) acc[d][e] *= a;
     }
-    const float ref = m == -INFINITY ? 0.f : m;
+  }
+  // scores to p; p in pairs as bf16, whose sum (of what the second product takes) goes to l
+  __device__ __forceinline__ void exponentials(const acc_t (&s)[TT], uint32_t (&p)[PAIRS], float c) {
+    float sum[2] = {0.f, 0.f};
 #pragma unroll
-    for (int t = 0; t < TT; ++t)
-#pragma unroll
-      for (int e = 0; e < AN; ++e) s[t][e] = exp2(__builtin_fmaf(s[t][e], c, -ref));
-    float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int t = 0; t < TT; ++t)
-#pragma unroll
-      for (int e = 0; e < AN; ++e) sum[e & 3] += s[t][e];
-    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    for (int i = 0; i < PAIRS; ++i) {
+      const int t = 2 * i / AN, e = 2 * i % AN;
+      p[i] = pack(exp2(__builtin_fmaf(s[t][e], c, -ref)), exp2(__builtin_fmaf(s[t][e + 1], c, -ref)));
+      sum[i & 1] = add_pair(p[i], sum[i & 1]);
+    }
+    l += sum[0] + sum[1];
+  }
+  static __device__ __forceinline__ float add_pair(uint32_t p, float to) {
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, p), __builtin_bit_cast(bf16x2_t, 0x3F803F80u), to, false);
   }
 
   static __device__ __forceinline__ uint32_t pack(float a, float b) {
@@ -208,18 +229,9 @@ struct Flash {
     const f32x2_t p = {a, b};
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(p, bf16x2_t));
   }
-  // p of MFMA step k as the second operand
-  __device__ __forceinline__ bf16x8_t weights(int k) const {
-    uint4 w;
-    if constexpr (ROWS == 32) {
-      const acc_t &p = s[k / 2];
-      const int o = 8 * (k & 1);
-      w = make_uint4(pack(p[o], p[o + 1]), pack(p[o + 2], p[o + 3]), pack(p[o + 4], p[o + 5]), pack(p[o + 6], p[o + 7]));
-    } else {
-      const acc_t &a = s[2 * k], &b = s[2 * k + 1];
-      w = make_uint4(pack(a[0], a[1]), pack(a[2], a[3]), pack(b[0], b[1]), pack(b[2], b[3]));
-    }
-    return __builtin_bit_cast(bf16x8_t, w);
+  // p of MFMA step k as the second operand: of 32 tokens' 16 pairs a lane has 8 (of 16 rows: 16 tokens' 4 in all)
+  static __device__ __forceinline__ bf16x8_t weights(const uint32_t (&p)[PAIRS], int k) {
+    return __builtin_bit_cast(bf16x8_t, make_uint4(p[4 * k], p[4 * k + 1], p[4 * k + 2], p[4 * k + 3]));
   }
   // V^T of dims [ROWS d, ROWS d + ROWS) for the tokens of MFMA step k, in the order of weights()
   static __device__ __forceinline__ uint4 values(uint32_t at, uint32_t v_at, int k, int d) {
@@ -234,20 +246,18 @@ struct Flash {
     }
     return make_uint4(h[0].x, h[0].y, h[1].x, h[1].y);
   }
-  __device__ __forceinline__ void add_values(uint32_t place, uint32_t v_at) {
-    const uint32_t at = lds + place * PLACE;
+  __device__ __forceinline__ void add_values(const uint32_t (&p)[PAIRS], uint32_t at, uint32_t v_at) {
 #pragma unroll
     for (int k = 0; k < PV; ++k) {
-      const bf16x8_t p = weights(k);
+      const bf16x8_t w = weights(p, k);
 #pragma unroll
-      for (int d = 0; d < DT; ++d) acc[d] = mma(__builtin_bit_cast(bf16x8_t, values(at, v_at, k, d)), p, acc[d]);
+      for (int d = 0; d < DT; ++d) acc[d] = mma(__builtin_bit_cast(bf16x8_t, values(at, v_at, k, d)), w, acc[d]);
     }
   }
   // The same where some rows must not see some of the tokens.  Their p is zero, but zero times an
   // infinity or NaN of V is NaN: a tile that holds any goes through the product with zeros in their
   // place, and is then looked through token by token, where a row takes what it sees.
-  __device__ __forceinline__ void add_values_masked(uint32_t place, int32_t lim) {
-    const uint32_t at = lds + place * PLACE;
+  __device__ __forceinline__ void add_values_masked(const uint32_t (&p)[PAIRS], uint32_t at, int32_t lim) {
     uint32_t v_at = this->v_at, lane = this->lane;
     asm volatile("" : "+v"(v_at), "+v"(lane));
     u16x2_t big = {0, 0};
@@ -262,22 +272,22 @@ struct Flash {
         __builtin_amdgcn_sched_barrier(0);
       }
     if (__builtin_expect(__builtin_amdgcn_ballot_w64(big.x >= 0x7F80 || big.y >= 0x7F80) == 0, 1)) {
-      add_values(place, v_at);
+      add_values(p, at, v_at);
       return;
     }
 #pragma unroll
     for (int k = 0; k < PV; ++k) {
-      const bf16x8_t p = weights(k);
+      const bf16x8_t w = weights(p, k);
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
         const uint4 v = values(at, v_at, k, d);
-        uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        uint32_t u[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          w[i] &= (w[i] & 0x7F80u) == 0x7F80u ? 0xFFFF0000u : 0xFFFFFFFFu;
-          w[i] &= (w[i] & 0x7F800000u) == 0x7F800000u ? 0xFFFFu : 0xFFFFFFFFu;
+          u[i] &= (u[i] & 0x7F80u) == 0x7F80u ? 0xFFFF0000u : 0xFFFFFFFFu;
+          u[i] &= (u[i] & 0x7F800000u) == 0x7F800000u ? 0xFFFFu : 0xFFFFFFFFu;
         }
-        acc[d] = mma(__builtin_bit_cast(bf16x8_t, make_uint4(w[0], w[1], w[2], w[3])), p, acc[d]);
+        acc[d] = mma(__builtin_bit_cast(bf16x8_t, make_uint4(u[0], u[1], u[2], u[3])), w, acc[d]);
         __builtin_amdgcn_sched_barrier(0);                 // (rare: in few registers rather than fast)
       }
     }
@@ -302,59 +312,177 @@ struct Flash {
     }
   }
 
+  // A tile's exponentials and its product with V beside the next tile's scores, in an order that is pinned: behind each
+  // MFMA one or two LDS reads (of what is needed four MFMAs later) and as many vector instructions as run while
+  // the matrix pipe is busy with it.  s: this tile's scores; next: the next tile's, whose largest is returned;
+  // `ask` (the next loads) is called behind the first MFMAs.
+  template <class Ask>
+  __device__ __forceinline__ float tile(acc_t (&next)[TT], const acc_t (&s)[TT], uint32_t k_place, uint32_t v_place, float c, Ask ask) {
+    static_assert(ROWS == 32 && TT == 2 && PV == 4, "32 scores of a lane, 16 for each half of the second product");
+    constexpr int NQ = QK * TT, NV = PV * DT, AHEAD = 4, EXPS = NQ + NV / 2;
+    typedef const __attribute__((address_space(3))) bf16x8_t *frag_t;
+    bf16x8_t kf[AHEAD];
+    uint4 vf[AHEAD];
+    uint32_t p[PAIRS];
+    float even = 0.f, sum[2] = {0.f, 0.f}, top = -INFINITY;
+    auto read_k = [&](int i) { kf[i % AHEAD] = *(frag_t)(k_place + (k_at ^ (i / TT * (MK * 2))) + i % TT * (ROWS * ROWB)); };
+    auto read_v = [&](int i) { vf[i % AHEAD] = values(v_place, v_at, i / DT, i % DT); };
+    auto exps = [&](int slot) {                            // 32 scores to p, over the first EXPS slots
+#pragma unroll
+      for (int i = slot * 32 / EXPS; i < (slot + 1) * 32 / EXPS; ++i) {
+        const float x = exp2(__builtin_fmaf(s[i / AN][i % AN], c, -ref));
+        if (i & 1) p[i / 2] = pack(even, x);
+        else even = x;
+      }
+    };
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) read_k(i);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) {
+      next[i % TT] = mma(kf[i % AHEAD], q[i / TT], i < TT ? acc_t{} : next[i % TT]);
+      if (i + AHEAD < NQ) read_k(i + AHEAD);
+      else read_v(i + AHEAD - NQ);
+      exps(i);
+      if (i == 1 || i == 3) ask(i / 2);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      acc[i % DT] = mma(__builtin_bit_cast(bf16x8_t, vf[i % AHEAD]), weights(p, i / DT), acc[i % DT]);
+      if (i + AHEAD < NV) read_v(i + AHEAD);
+      if (i < NV / 2) exps(NQ + i);
+      else {
+#pragma unroll
+        for (int n = (i - NV / 2) * (64 / NV); n < (i - NV / 2 + 1) * (64 / NV); ++n) {
+          top = fmaxf(top, next[n / AN][n % AN]);
+          if (n & 1) sum[n / 2 & 1] = add_pair(p[n / 2], sum[n / 2 & 1]);
+        }
+        asm volatile("" : "+v"(top), "+v"(sum[0]), "+v"(sum[1]));   // (here, not later)
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    l += sum[0] + sum[1];
+    return top;
+  }
+
   // Tokens [0, n) of K and V, `n` the same for all four waves; `mine` of them are seen by rows of this
   // wave (none if 0).  A row attends to tokens below its `lim`; full: below that every row does.
   // CAUSAL: there is data behind a row's last token (otherwise zeros).  `step(j)` is called behind
   // the barrier of each tile.
+  //
+  // Where reading K and V is what bounds it: one item of the ring after the other.
   template <bool CAUSAL, class Step>
-  __device__ __forceinline__ void run(Src ks, Src vs, uint32_t n, uint32_t mine, uint32_t full, int32_t lim, float c, Step step) {
+  __device__ __forceinline__ void run_lean(Src ks, Src vs, uint32_t n, uint32_t mine, uint32_t full, int32_t lim, float c, Step step) {
     __syncthreads();                                       // (LDS may still be read for the block before)
     const uint32_t tiles = (n + TOK - 1) / TOK, have = (mine + TOK - 1) / TOK, whole = full / TOK;
 #pragma unroll
     for (int i = 0; i < NS - 1; ++i) ask(i & 1 ? vs : ks, i);
-    // (q is waited for here: the compiler would do so in the loop, counting none of the loads above)
-#pragma unroll
-    for (int k = 0; k < QK; ++k) asm volatile("" : "+v"(q[k]));
+    wait_q();
+    acc_t s[TT];
+    uint32_t p[PAIRS];
     uint32_t place = 0;                                    // of item i; item i + NS - 1 goes to the place before it
     auto next = [&]() { place = place + 1 == NS ? 0 : place + 1; };
     auto before = [&]() { return place == 0 ? NS - 1 : place - 1; };
+    auto at = [&]() { return lds + place * PLACE; };
     constexpr bool V_FIRST = (NS - 1) & 1;                 // what item i + NS - 1 is, behind a K
     uint32_t j = 0;
     for (; j < whole && j < have; ++j) {
-      sync();
+      sync<(NS - 2) * L>();
       ask(V_FIRST ? vs : ks, before());
       step(j);
-      scores<false>(place, c, 0);
+      products<false>(s, at(), k_at, 0);
+      follow(largest(s), c);
+      exponentials(s, p, c);
       next();
-      sync();
+      sync<(NS - 2) * L>();
       ask(V_FIRST ? ks : vs, before());
-      add_values(place, v_at);
-      next();
-    }
-    for (; j < have; ++j) {
-      const int32_t below = lim - (int32_t)(j * TOK);
-      sync();
-      ask(V_FIRST ? vs : ks, before());
-      step(j);
-      scores<true>(place, c, below);
-      next();
-      sync();
-      ask(V_FIRST ? ks : vs, before());
-      if constexpr (CAUSAL) add_values_masked(place, below);
-      else add_values(place, v_at);
+      add_values(p, at(), v_at);
       next();
     }
     for (; j < tiles; ++j) {
-      sync();
+      const int32_t below = lim - (int32_t)(j * TOK);
+      sync<(NS - 2) * L>();
       ask(V_FIRST ? vs : ks, before());
       step(j);
+      if (j < have) {
+        products<true>(s, at(), opaque(k_at), below);
+        follow(largest(s), c);
+        exponentials(s, p, c);
+      }
       next();
-      sync();
+      sync<(NS - 2) * L>();
       ask(V_FIRST ? ks : vs, before());
+      if (j < have) {
+        if constexpr (CAUSAL) add_values_masked(p, at(), below);
+        else add_values(p, at(), v_at);
+      }
       next();
     }
     // what is still on its way is the zeros of items past the last one
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    l = over_row<AddOp>(l);
+  }
+
+  // Where the products are: the scores of the next tile are computed beside the exponentials of this one,
+  // which keeps the matrix pipe and the vector pipe busy at the same time, and there is one barrier a tile.  Behind
+  // tile j's, K of tile j + 1 and V of tile j are in LDS, and tile j - 1's V and tile j's K are done with:
+  // their places take those of tiles j + 1 and j + 2.
+  template <bool CAUSAL, class Step>
+  __device__ __forceinline__ void run(Src ks, Src vs, uint32_t n, uint32_t mine, uint32_t full, int32_t lim, float c, Step step) {
+    static_assert(NS == 4, "two tiles");
+    __syncthreads();                                       // (LDS may still be read for the block before)
+    const uint32_t tiles = (n + TOK - 1) / TOK, have = (mine + TOK - 1) / TOK;
+    const uint32_t whole = full / TOK < have ? full / TOK : have;
+    ask(ks, 0);
+    ask(ks, 2);
+    ask(vs, 1);
+    wait_q();
+    acc_t s[2][TT];
+    sync<2 * L>();
+    if (have) {
+      products<true>(s[0], lds, opaque(k_at), lim);
+      follow(largest(s[0]), c);
+    }
+    uint32_t j = 0;
+    auto both = [&](auto par) {                            // tile j, in the places of tiles with its parity
+      constexpr int P = decltype(par)::value;
+      sync<0>();
+      step(j);
+      follow(tile(s[1 - P], s[P], lds + (2 - 2 * P) * PLACE, lds + (1 + 2 * P) * PLACE, c,
+                         [&](int i) { i ? ask(vs, 3 - 2 * P) : ask(ks, 2 * P); }), c);
+      ++j;
+    };
+    while (j + 2 < whole) {
+      both(std::integral_constant<int, 0>());
+      both(std::integral_constant<int, 1>());
+    }
+    if (j + 1 < whole) {
+      both(std::integral_constant<int, 0>());
+#pragma unroll
+      for (int t = 0; t < TT; ++t) s[0][t] = s[1][t];
+    }
+    // the last tile that every row sees whole, and those that end at the rows' own
+    for (; j < tiles; ++j) {
+      const uint32_t par = j & 1;
+      const int32_t below = lim - (int32_t)(j * TOK);
+      sync<0>();
+      ask(ks, 2 * par);
+      ask(vs, 3 - 2 * par);
+      step(j);
+      if (j < have) {
+        uint32_t p[PAIRS];
+        exponentials(s[0], p, c);
+        const uint32_t at = lds + (1 + 2 * par) * PLACE;
+        if constexpr (CAUSAL) add_values_masked(p, at, below);
+        else add_values(p, at, opaque(v_at));
+        if (j + 1 < have) {
+          products<true>(s[0], lds + (2 - 2 * par) * PLACE, opaque(k_at), below - TOK);
+          follow(largest(s[0]), c);
+        }
+      }
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // (as above)
     l = over_row<AddOp>(l);
   }
 
@@ -416,23 +544,24 @@ struct PromptBodyT {
 #ifdef __HIP_DEVICE_COMPILE__
     const uint32_t head = block % a.heads, slot = block / a.heads;
     extern __shared__ __align__(1024) unsigned char tally_dyn_lds[];
-    // the sequence of this slot: the last one that starts at or before it, 64 candidates at a time
+    // the sequence of this slot: the last one that starts at or before it, 63 candidates at a time; the lane behind
+    // the last candidate has where that one ends
     const uint32_t ln = threadIdx.x & 63;
-    auto edge = [&](uint32_t s) {
-      const int32_t v = a.cu_seqlens[s];
-      return v < 0 ? 0u : (uint32_t)v < a.total ? (uint32_t)v : a.total;
-    };
-    uint32_t seq = 0;
+    uint32_t seq = 0, first, last;
     for (uint32_t n = a.n_seqs;;) {
-      const uint32_t step = (n + 63) / 64, s = ln * step;
-      const bool ok = s < n && edge(seq + s) / kPromptRows + seq + s <= slot;
+      const uint32_t step = (n + 62) / 63, s = ln * step < n ? ln * step : n;
+      const int32_t v = a.cu_seqlens[seq + s];
+      const uint32_t edge = v < 0 ? 0u : (uint32_t)v < a.total ? (uint32_t)v : a.total;
+      const bool ok = s < n && edge / kPromptRows + seq + s <= slot;
       const uint32_t c = (uint32_t)__popcll(__builtin_amdgcn_ballot_w64(ok)), i = c ? c - 1 : 0;
       seq += i * step;
-      if (step == 1) break;
+      if (step == 1) {
+        first = (uint32_t)__builtin_amdgcn_readlane((int)edge, (int)i);
+        last = (uint32_t)__builtin_amdgcn_readlane((int)edge, (int)i + 1);
+        break;
+      }
       n = n - i * step < step ? n - i * step : step;
     }
-    const uint32_t first = __builtin_amdgcn_readfirstlane(edge(seq));
-    const uint32_t last = __builtin_amdgcn_readfirstlane(edge(seq + 1));
     const uint32_t len = last > first ? last - first : 0u;
     const uint32_t at = slot - (first / kPromptRows + seq), blocks = (len + kPromptRows - 1) / kPromptRows;
     if (at >= blocks) return;                              // (the same for the whole workgroup; slots before the first sequence wrap)

@@ -83,9 +83,12 @@ __device__ __forceinline__ void prefix_part(const tally_attn_prefix_args &a, con
     if (exists) u = *reinterpret_cast<const uint4 *>(q + i * F::MK);
     f.q[i] = __builtin_bit_cast(bf16x8_t, u);
   }
-  if (n != 0)
-    f.template run<false>(f.source(k, n, ld), f.source(v, n, ld), n, mine < rows ? n : 0u, n, (int32_t)n,
-                          (a.scale > 0.f ? a.scale : F::DIM == 128 ? 0.08838834764831845f : 0.125f) * kLog2e, [](uint32_t) {});
+  const float c = (a.scale > 0.f ? a.scale : F::DIM == 128 ? 0.08838834764831845f : 0.125f) * kLog2e;
+  auto step = [](uint32_t) {};
+  if (n != 0) {
+    if constexpr (F::ROWS == 16) f.template run_lean<false>(f.source(k, n, ld), f.source(v, n, ld), n, mine < rows ? n : 0u, n, (int32_t)n, c, step);
+    else f.template run<false>(f.source(k, n, ld), f.source(v, n, ld), n, mine < rows ? n : 0u, n, (int32_t)n, c, step);
+  }
   if (!exists) return;
   const uint32_t parts = p.parts + p.own_parts;
   const uint64_t at = ((uint64_t)b * a.heads + head) * parts + part;

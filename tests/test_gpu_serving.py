@@ -195,7 +195,7 @@ def test_prompt_rows_do_not_see_what_is_hidden_from_them(env, where, poison, dim
             assert np.isnan(seen).all()
 
 
-@pytest.mark.parametrize("seqs", [63, 64, 65, 700, 5000])
+@pytest.mark.parametrize("seqs", [62, 63, 64, 65, 700, 3969, 3970, 5000])
 def test_prompt_many_sequences(env, seqs):
     """The search for a block's sequence, with one, two and three rounds of 64 candidates."""
     B, ctx, torch = env
