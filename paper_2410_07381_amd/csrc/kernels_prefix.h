@@ -45,7 +45,7 @@ inline PrefixPlan prefix_plan(uint32_t batch, uint32_t heads, uint32_t kv_heads,
   p.row_tiles = (uint32_t)up(p.rows, p.many ? kPrefixManyRows : kPrefixFewRows);
   p.own_tiles = (uint32_t)up(p.group, kPrefixFewRows);
   const uint64_t tokens = (uint64_t)kv_heads * p.row_tiles * prefix + (uint64_t)kv_heads * batch * p.own_tiles * own_cap;
-  uint64_t chunk = up(tokens, p.many ? 512 : 1024);
+  uint64_t chunk = up(tokens, p.many ? 512 : 1024);       // (workgroups that are on the GPU at once)
   if (chunk < kPrefixLeast) chunk = kPrefixLeast;
   auto parts = [&](uint32_t n, uint32_t &c, uint32_t &k) {
     const uint64_t least = up(n, kPrefixParts), w = chunk < least ? least : chunk < n ? chunk : n;
@@ -107,15 +107,25 @@ __device__ __forceinline__ void prefix_part(const tally_attn_prefix_args &a, con
 }
 
 template <int DIM, bool MANY>
+constexpr unsigned prefix_lds() { return MANY ? Flash<DIM, 32, 64, 4>::LDS : Flash<DIM, 16, 32, 3>::LDS; }
+
+template <int DIM, bool MANY>
 __global__ __launch_bounds__(256, MANY ? 2 : 4) void attn_prefix_partial(tally_attn_prefix_args a, PrefixPlan p, uint32_t urgent) {
   if (urgent) __builtin_amdgcn_s_setprio(3);
   extern __shared__ __align__(1024) unsigned char tally_dyn_lds[];
   typedef Flash<DIM, 16, 32, 3> Few;
   typedef Flash<DIM, 32, 64, 4> Many;
   typedef typename std::conditional<MANY, Many, Few>::type Shared;
+  // (beside 128-row workgroups, of which a compute unit has two, in the LDS that those take)
+  typedef typename std::conditional<MANY, Flash<DIM, 16, 32, 8>, Few>::type Own;
+  static_assert(Own::LDS <= prefix_lds<DIM, MANY>(), "one size for both");
   uint32_t i = blockIdx.x;
   if (i < p.prefix_groups) {
-    const uint32_t kv = i % a.kv_heads, rest = i / a.kv_heads, part = rest % p.parts, tile = rest / p.parts;
+    // the row tiles of one part of one K/V head next to one another on one die (every eighth workgroup is on
+    // the same one), so that all but the first find its K and V in that die's L2
+    const uint32_t units = a.kv_heads * p.parts, group = i / (8 * p.row_tiles), at8 = i % (8 * p.row_tiles);
+    const uint32_t side = units - 8 * group < 8 ? units - 8 * group : 8, tile = at8 / side, unit = 8 * group + at8 % side;
+    const uint32_t kv = unit % a.kv_heads, part = unit / a.kv_heads;
     const uint32_t LD = a.ld_prefix ? a.ld_prefix : a.kv_heads * DIM, t0 = part * p.chunk;
     const uint32_t n = a.prefix - t0 < p.chunk ? a.prefix - t0 : p.chunk;
     const uint32_t row0 = tile * Shared::BLOCK_ROWS, left = p.rows - row0;
@@ -130,31 +140,38 @@ __global__ __launch_bounds__(256, MANY ? 2 : 4) void attn_prefix_partial(tally_a
     const int32_t said = a.own_len[b];
     const uint32_t len = said < 0 ? 0u : (uint32_t)said < a.own_cap ? (uint32_t)said : a.own_cap;
     const uint32_t left = len > t0 ? len - t0 : 0u, n = __builtin_amdgcn_readfirstlane(left < p.own_chunk ? left : p.own_chunk);
-    const uint32_t row0 = tile * Few::BLOCK_ROWS, rows = p.group - row0;
+    const uint32_t row0 = tile * Own::BLOCK_ROWS, rows = p.group - row0;
     const uint64_t at = (uint64_t)b * (a.stride_own ? a.stride_own : (uint64_t)a.own_cap * LD) + (uint64_t)t0 * LD + kv * DIM;
-    prefix_part<Few>(a, p, tally_dyn_lds, a.Ko + at, a.Vo + at, LD, n, kv, b * p.group + row0,
-                     rows < (uint32_t)Few::BLOCK_ROWS ? rows : (uint32_t)Few::BLOCK_ROWS, p.parts + part);
+    prefix_part<Own>(a, p, tally_dyn_lds, a.Ko + at, a.Vo + at, LD, n, kv, b * p.group + row0,
+                     rows < (uint32_t)Own::BLOCK_ROWS ? rows : (uint32_t)Own::BLOCK_ROWS, p.parts + part);
   }
 }
 static_assert(Flash<128, 16, 32, 3>::LDS <= 31 * 1024, "room beside a paused 256 x 256 GEMM tile");
-template <int DIM, bool MANY>
-constexpr unsigned prefix_lds() { return MANY ? Flash<DIM, 32, 64, 4>::LDS : Flash<DIM, 16, 32, 3>::LDS; }
 
 // One row per workgroup: the parts' weights exp(m - max) first, then each wave a quarter of the
-// parts.  A part without tokens has l = 0 and its acc was not written.
+// parts, 16 bytes of a part's acc to a lane and eight loads at a time.  A part without tokens has l = 0 and its
+// acc was not written: what stands there is not added.
 template <int DIM>
 __global__ __launch_bounds__(256) void attn_prefix_combine(tally_attn_prefix_args a, PrefixPlan p, uint32_t urgent) {
 #ifdef __HIP_DEVICE_COMPILE__
   if (urgent) __builtin_amdgcn_s_setprio(3);
-  constexpr int PER = DIM / 64;
-  __shared__ float s_w[2 * kPrefixParts];
+  constexpr uint32_t LANES = DIM / 4, SIDE = 64 / LANES, ROUND = 4 * SIDE, U = 4;   // parts side by side in a wave, in all four
+  __shared__ float s_w[2 * kPrefixParts + ROUND * U];
   __shared__ float s_acc[4][DIM];
   const uint32_t head = blockIdx.x % a.heads, b = blockIdx.x / a.heads, parts = p.parts + p.own_parts;
   const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const uint64_t row = (uint64_t)b * a.heads + head;
   const float2 *ml = reinterpret_cast<const float2 *>(a.scratch) + row * parts;
   const float *rec = reinterpret_cast<const float *>(reinterpret_cast<const float2 *>(a.scratch) + (uint64_t)a.batch * a.heads * parts) +
-                     row * parts * DIM + lane * PER;
+                     row * parts * DIM + lane % LANES * 4;
+  const uint32_t mine = wave * SIDE + lane / LANES;
+  // (the first round's loads do not wait for the weights)
+  f32x4_t v[U];
+#pragma unroll
+  for (uint32_t u = 0; u < U; ++u) {
+    v[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    if (mine + u * ROUND < parts) v[u] = *reinterpret_cast<const f32x4_t *>(rec + (uint64_t)(mine + u * ROUND) * DIM);
+  }
   float2 own[2 * kPrefixParts / 64];
   float top = -INFINITY;
 #pragma unroll
@@ -170,25 +187,42 @@ __global__ __launch_bounds__(256) void attn_prefix_combine(tally_attn_prefix_arg
     const float w = own[i].y == 0.f ? 0.f : __builtin_amdgcn_exp2f(own[i].x - (top == -INFINITY ? 0.f : top));
     sum += own[i].y == 0.f ? 0.f : own[i].y * w;
     if (wave == 0) s_w[lane + 64 * i] = w;
-    // (l is no number only where scores were none: its maximum may still be -inf, and then w is 0)
   }
+  if (wave == 0 && lane < ROUND * U) s_w[2 * kPrefixParts + lane] = 0.f;
   sum = wave_sum(sum);
   __syncthreads();
-  float acc[PER] = {};
-  for (uint32_t i = wave; i < parts; i += 4) {
-    const float w = s_w[i];
-    if (w == 0.f) continue;
+  f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+  for (uint32_t i = mine;;) {
 #pragma unroll
-    for (int e = 0; e < PER; ++e) acc[e] = __builtin_fmaf(w, rec[(uint64_t)i * DIM + e], acc[e]);
+    for (uint32_t u = 0; u < U; ++u) {
+      const float w = s_w[i + u * ROUND];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] += w == 0.f ? 0.f : w * v[u][e];
+    }
+    i += ROUND * U;
+    if (i - mine >= parts) break;                          // (the same for every lane)
+#pragma unroll
+    for (uint32_t u = 0; u < U; ++u)
+      if (i + u * ROUND < parts) v[u] = *reinterpret_cast<const f32x4_t *>(rec + (uint64_t)(i + u * ROUND) * DIM);
   }
+  if constexpr (SIDE == 4) {
 #pragma unroll
-  for (int e = 0; e < PER; ++e) s_acc[wave][lane * PER + e] = acc[e];
+    for (int e = 0; e < 4; ++e) acc[e] = across_rows<AddOp>(acc[e]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float o = acc[e], w = o;
+      asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(o), "+v"(w));
+      acc[e] = o + w;
+    }
+  }
+  if (lane < LANES) *reinterpret_cast<f32x4_t *>(&s_acc[wave][lane * 4]) = acc;
   __syncthreads();
   if (threadIdx.x < DIM) {
     const uint32_t d = threadIdx.x;
-    const float v = (s_acc[0][d] + s_acc[1][d]) + (s_acc[2][d] + s_acc[3][d]);
+    const float o = (s_acc[0][d] + s_acc[1][d]) + (s_acc[2][d] + s_acc[3][d]);
     const uint32_t LDO = a.ld_out ? a.ld_out : a.heads * DIM;
-    a.out[(uint64_t)b * LDO + head * DIM + d] = f32_to_bf16(sum == 0.f ? 0.f : v / sum);
+    a.out[(uint64_t)b * LDO + head * DIM + d] = f32_to_bf16(sum == 0.f ? 0.f : o / sum);
   }
 #endif
 }
