@@ -34,6 +34,9 @@
 namespace tally {
 
 constexpr float kLog2e = 1.4426950408889634f;
+// The maximum of a row that has seen nothing: below any score, but a number, so that exp(s - m) is zero for a score
+// of -inf and exp(m - m_new) for any new maximum.
+constexpr float kNothing = -3e38f;
 
 template <int DIM_, int ROWS_, int TOK_, int NS_>
 struct Flash {
@@ -50,8 +53,9 @@ struct Flash {
   static constexpr int TT = TOK / ROWS, DT = DIM / ROWS;   // blocks of tokens and of dims
   static constexpr int AN = ROWS == 32 ? 16 : 4;           // accumulators of a block
   static constexpr int PAIRS = TT * AN / 2;                // of a lane's scores in a tile
+  static constexpr int AHEAD = 4;                          // fragments on their way from LDS
   static_assert((DIM == 64 || DIM == 128) && (ROWS == 32 || ROWS == 16), "shapes that the maps below know");
-  static_assert(L >= 1 && L * 1024 * WAVES == (int)PLACE && NS >= 3, "whole loads, two items on their way");
+  static_assert((L == 1 || L == 2 || L == 4) && L * 1024 * WAVES == (int)PLACE && NS >= 3, "whole loads, two items on their way");
   static_assert(BEFORE < 4096, "an immediate has 12 bits");
 
 #ifdef __HIP_DEVICE_COMPILE__
@@ -70,7 +74,7 @@ struct Flash {
   uint32_t k_at, v_at;                                     // a lane's place in K's and V's fragment reads
   bf16x8_t q[QK];
   acc_t acc[DT];
-  float m, l, ref;                                         // ref: m, or 0 while a row has seen nothing
+  float m, l;
 
   // 16-byte chunk c of token t stands at chunk c xor swz(t): different for 16 neighbouring tokens (of
   // dim 64, whose rows are half as long, for every second one), and its high bits for four
@@ -102,10 +106,13 @@ struct Flash {
     const uint32_t i = lane & 15, tok = 4 * part + (i >> 2);
     const uint32_t chunk = (ROWS == 32 ? (lane >> 4 & 1) * 2 : 0) + (i >> 1 & 1);
     v_at = tok * ROWB + ((chunk ^ swz(tok)) << 4) + (i & 1) * 8;
+    reset();
+  }
+  __device__ __forceinline__ void reset() {
 #pragma unroll
     for (int d = 0; d < DT; ++d) acc[d] = acc_t{};
-    m = -INFINITY;
-    l = ref = 0.f;
+    m = kNothing;
+    l = 0.f;
   }
   __device__ __forceinline__ Src source(const uint16_t *at, uint32_t tokens, uint32_t ld) const {
     Src r;
@@ -119,27 +126,29 @@ struct Flash {
     }
     return r;
   }
-  // rows of q: a lane's, of `rows` that exist (the others read as zeros)
-  __device__ __forceinline__ void read_q(const uint16_t *at, uint32_t rows, uint32_t ld) {
-    const buf_t b = make_buf(at, rows * ld * 2);
-#pragma unroll
-    for (int k = 0; k < QK; ++k)
-      q[k] = __builtin_bit_cast(bf16x8_t, buf_ld16(b, (lane % ROWS) * ld * 2 + (lane / ROWS) * 16, k * MK * 2));
-  }
-
   // the next item of a source to a place of the ring; past its end nothing is moved and zeros are left
   __device__ __forceinline__ void ask(Src &r, uint32_t place) const {
     // (Assembly: knowing of the loads, the compiler waits for all of them before any transposing read.  They
     // have no destination in registers, sync() waits for them, and nothing else in these kernels uses m0.  The
     // immediate separates a wave's loads in LDS; it moves the global address too, which is taken out of
-    // the lane's offset, and so that none is negative the buffer starts BEFORE bytes early.)
-    const uint32_t n = r.left < (uint32_t)TOK ? r.left : (uint32_t)TOK;
+    // the lane's offset, and so that none is negative the buffer starts BEFORE bytes early.  An SGPR that a vector
+    // instruction wrote (the buffer's words, where they had to be put away) may be read by a load five wait states
+    // later, which the compiler sees to for its own instructions alone: the block opens with them.)
+    const uint32_t n = r.left < (uint32_t)TOK ? r.left : (uint32_t)TOK, to = lds + place * PLACE + wave * (L * 1024u);
     const uint64_t p = (uint64_t)(uintptr_t)r.at;
     const u32x4_t b = {(uint32_t)p, (uint32_t)(p >> 32) & 0xFFFFu, n * r.ld + BEFORE, 0x00027000u};
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0" ::"s"(lds + place * PLACE + wave * (L * 1024u)) : "memory");
-#pragma unroll
-    for (int j = 0; j < L; ++j)
-      asm volatile("buffer_load_dwordx4 %0, %1, 0 offen offset:%2 lds" ::"v"(r.voff[j]), "s"(b), "n"(j * 1024) : "memory");
+#define LOAD_LDS(v, at) "buffer_load_dwordx4 " v ", %1, 0 offen offset:" at " lds"
+#define OPEN_LDS "s_mov_b32 m0, %0\n\ts_nop 4\n\t"
+    if constexpr (L == 1)
+      asm volatile(OPEN_LDS LOAD_LDS("%2", "0") ::"s"(to), "s"(b), "v"(r.voff[0]) : "memory");
+    else if constexpr (L == 2)
+      asm volatile(OPEN_LDS LOAD_LDS("%2", "0") "\n\t" LOAD_LDS("%3", "0x400") ::"s"(to), "s"(b), "v"(r.voff[0]), "v"(r.voff[1]) : "memory");
+    else
+      asm volatile(OPEN_LDS LOAD_LDS("%2", "0") "\n\t" LOAD_LDS("%3", "0x400") "\n\t" LOAD_LDS("%4", "0x800") "\n\t" LOAD_LDS("%5", "0xC00") ::"s"(to),
+                   "s"(b), "v"(r.voff[0]), "v"(r.voff[1]), "v"(r.voff[2]), "v"(r.voff[3])
+                   : "memory");
+#undef LOAD_LDS
+#undef OPEN_LDS
     r.at += (uint64_t)TOK * r.ld;
     r.left -= n;
   }
@@ -164,24 +173,33 @@ struct Flash {
   // which token of a tile element e of block t stands for, without the lane's own part
   static constexpr uint32_t token(int t, int e) { return ROWS == 32 ? 32 * t + 8 * (e / 4) + e % 4 : 16 * t + e; }
 
-  // S^T of the tile whose K stands at `at`.  MASK: a lane's row attends to tokens of the tile below `lim` alone.
-  template <bool MASK>
-  __device__ __forceinline__ void products(acc_t (&s)[TT], uint32_t at, uint32_t k_at, int32_t lim) const {
+  // fragment i of K, of the tile at `place`: block i % TT of tokens, MFMA step i / TT
+  __device__ __forceinline__ bf16x8_t key(uint32_t place, uint32_t k_at, int i) const {
     typedef const __attribute__((address_space(3))) bf16x8_t *frag_t;
+    return *(frag_t)(place + (k_at ^ (i / TT * (MK * 2))) + i % TT * (ROWS * ROWB));
+  }
+  // S^T of a tile; the fragments are read AHEAD MFMAs before they are needed
+  __device__ __forceinline__ void products(acc_t (&s)[TT], uint32_t place, uint32_t k_at) const {
+    constexpr int N = QK * TT;
+    bf16x8_t f[AHEAD];
 #pragma unroll
-    for (int t = 0; t < TT; ++t) s[t] = acc_t{};
+    for (int i = 0; i < AHEAD; ++i) f[i] = key(place, k_at, i);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int k = 0; k < QK; ++k)
-#pragma unroll
-      for (int t = 0; t < TT; ++t)
-        s[t] = mma(*(frag_t)(at + (k_at ^ (k * (MK * 2))) + t * (ROWS * ROWB)), q[k], s[t]);
-    if constexpr (MASK) {
-      const int32_t left = lim - 4 * (int32_t)(lane / ROWS);
-#pragma unroll
-      for (int t = 0; t < TT; ++t)
-#pragma unroll
-        for (int e = 0; e < AN; ++e) s[t][e] = (int32_t)token(t, e) < left ? s[t][e] : -INFINITY;
+    for (int i = 0; i < N; ++i) {
+      s[i % TT] = mma(f[i % AHEAD], q[i / TT], i < TT ? acc_t{} : s[i % TT]);
+      if (i + AHEAD < N) f[i % AHEAD] = key(place, k_at, i + AHEAD);
+      __builtin_amdgcn_sched_barrier(0);
     }
+  }
+  // a lane's row attends to tokens of the tile below `lim` alone
+  __device__ __forceinline__ void hide(acc_t (&s)[TT], int32_t lim) const {
+    int32_t left = lim - 4 * (int32_t)(lane / ROWS);
+    asm volatile("" : "+v"(left));                         // (computed here, where it is asked for)
+#pragma unroll
+    for (int t = 0; t < TT; ++t)
+#pragma unroll
+      for (int e = 0; e < AN; ++e) s[t][e] = (int32_t)token(t, e) < left ? s[t][e] : -INFINITY;
   }
   // a lane's largest score
   static __device__ __forceinline__ float largest(const acc_t (&s)[TT]) {
@@ -198,9 +216,7 @@ struct Flash {
   __device__ __forceinline__ void follow(float top, float c) {
     top *= c;
     if (__builtin_amdgcn_ballot_w64(top > m + 8.f) != 0) {
-      const float now = fmaxf(m, over_row<MaxOp>(top));
-      ref = now == -INFINITY ? 0.f : now;
-      const float a = exp2(m - ref);
+      const float now = fmaxf(m, over_row<MaxOp>(top)), a = exp2(m - now);
       m = now;
       l *= a;
 #pragma unroll
@@ -209,19 +225,9 @@ struct Flash {
         for (int e = 0; e < AN; ++e) acc[d][e] *= a;
     }
   }
-  // scores to p; p in pairs as bf16, whose sum (of what the second product takes) goes to l
-  __device__ __forceinline__ void exponentials(const acc_t (&s)[TT], uint32_t (&p)[PAIRS], float c) {
-    float sum[2] = {0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < PAIRS; ++i) {
-      const int t = 2 * i / AN, e = 2 * i % AN;
-      p[i] = pack(exp2(__builtin_fmaf(s[t][e], c, -ref)), exp2(__builtin_fmaf(s[t][e + 1], c, -ref)));
-      sum[i & 1] = add_pair(p[i], sum[i & 1]);
-    }
-    l += sum[0] + sum[1];
-  }
-  static __device__ __forceinline__ float add_pair(uint32_t p, float to) {
-    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, p), __builtin_bit_cast(bf16x2_t, 0x3F803F80u), to, false);
+  // to + times . p (two bf16 each)
+  static __device__ __forceinline__ float add_pair(uint32_t p, float to, uint32_t times = 0x3F803F80u) {
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, p), __builtin_bit_cast(bf16x2_t, times), to, false);
   }
 
   static __device__ __forceinline__ uint32_t pack(float a, float b) {
@@ -246,34 +252,43 @@ struct Flash {
     }
     return make_uint4(h[0].x, h[0].y, h[1].x, h[1].y);
   }
-  __device__ __forceinline__ void add_values(const uint32_t (&p)[PAIRS], uint32_t at, uint32_t v_at) {
+  // A tile's exponentials (p in pairs as bf16, whose sum, of what the product takes, goes to l) and its product with
+  // V, each step's beside the product of the one before.
+  __device__ __forceinline__ void finish(const acc_t (&s)[TT], uint32_t (&p)[PAIRS], uint32_t place, uint32_t v_at, float c) {
+    constexpr int N = PV * DT, EACH = 2 * PAIRS / PV;      // scores of a lane in an MFMA step
+    uint4 f[AHEAD];
+    float sum[2] = {0.f, 0.f};
+    auto exps = [&](int from, int to) {
 #pragma unroll
-    for (int k = 0; k < PV; ++k) {
-      const bf16x8_t w = weights(p, k);
-#pragma unroll
-      for (int d = 0; d < DT; ++d) acc[d] = mma(__builtin_bit_cast(bf16x8_t, values(at, v_at, k, d)), w, acc[d]);
-    }
-  }
-  // The same where some rows must not see some of the tokens.  Their p is zero, but zero times an
-  // infinity or NaN of V is NaN: a tile that holds any goes through the product with zeros in their
-  // place, and is then looked through token by token, where a row takes what it sees.
-  __device__ __forceinline__ void add_values_masked(const uint32_t (&p)[PAIRS], uint32_t at, int32_t lim) {
-    uint32_t v_at = this->v_at, lane = this->lane;
-    asm volatile("" : "+v"(v_at), "+v"(lane));
-    u16x2_t big = {0, 0};
-#pragma unroll
-    for (int k = 0; k < PV; ++k)
-#pragma unroll
-      for (int d = 0; d < DT; ++d) {
-        const uint4 v = values(at, v_at, k, d);
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) big = __builtin_elementwise_max(big, __builtin_bit_cast(u16x2_t, w[i] & 0x7FFF7FFFu));
-        __builtin_amdgcn_sched_barrier(0);
+      for (int i = from; i < to; i += 2) {
+        p[i / 2] = pack(exp2(__builtin_fmaf(s[i / AN][i % AN], c, -m)), exp2(__builtin_fmaf(s[i / AN][i % AN + 1], c, -m)));
+        sum[i / 2 & 1] = add_pair(p[i / 2], sum[i / 2 & 1]);
       }
-    if (__builtin_expect(__builtin_amdgcn_ballot_w64(big.x >= 0x7F80 || big.y >= 0x7F80) == 0, 1)) {
-      add_values(p, at, v_at);
-      return;
+    };
+#pragma unroll
+    for (int i = 0; i < AHEAD && i < N; ++i) f[i] = values(place, v_at, i / DT, i % DT);
+    exps(0, EACH);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int k = i / DT, d = i % DT;
+      acc[d] = mma(__builtin_bit_cast(bf16x8_t, f[i % AHEAD]), weights(p, k), acc[d]);
+      if (i + AHEAD < N) f[i % AHEAD] = values(place, v_at, (i + AHEAD) / DT, (i + AHEAD) % DT);
+      if (k + 1 < PV) exps((k + 1) * EACH + EACH * d / DT / 2 * 2, (k + 1) * EACH + EACH * (d + 1) / DT / 2 * 2);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    l += sum[0] + sum[1];
+  }
+  // The same where V has tokens that are no numbers and that not every row sees.  Their p is zero, but zero times an
+  // infinity or NaN is NaN: the product has zeros in their place, and the tile is then looked through
+  // token by token, where a row takes what it sees.  (Rare: in few registers rather than fast.)
+  __device__ __forceinline__ void finish_careful(const acc_t (&s)[TT], uint32_t (&p)[PAIRS], uint32_t at, uint32_t v_at, float c, int32_t lim) {
+    const uint32_t lane = opaque(this->lane);
+    asm volatile("" : "+v"(c));                            // (nothing in common with finish())
+#pragma unroll
+    for (int i = 0; i < 2 * PAIRS; i += 2) {
+      p[i / 2] = pack(exp2(__builtin_fmaf(s[i / AN][i % AN], c, -m)), exp2(__builtin_fmaf(s[i / AN][i % AN + 1], c, -m)));
+      l = add_pair(p[i / 2], l);
     }
 #pragma unroll
     for (int k = 0; k < PV; ++k) {
@@ -288,7 +303,7 @@ struct Flash {
           u[i] &= (u[i] & 0x7F800000u) == 0x7F800000u ? 0xFFFFu : 0xFFFFFFFFu;
         }
         acc[d] = mma(__builtin_bit_cast(bf16x8_t, make_uint4(u[0], u[1], u[2], u[3])), w, acc[d]);
-        __builtin_amdgcn_sched_barrier(0);                 // (rare: in few registers rather than fast)
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
     typedef const __attribute__((address_space(3))) uint2 *four_t;
@@ -312,36 +327,37 @@ struct Flash {
     }
   }
 
-  // A tile's exponentials and its product with V beside the next tile's scores, in an order that is pinned: behind each
-  // MFMA one or two LDS reads (of what is needed four MFMAs later) and as many vector instructions as run while
-  // the matrix pipe is busy with it.  s: this tile's scores; next: the next tile's, whose largest is returned;
-  // `ask` (the next loads) is called behind the first MFMAs.
-  template <class Ask>
-  __device__ __forceinline__ float tile(acc_t (&next)[TT], const acc_t (&s)[TT], uint32_t k_place, uint32_t v_place, float c, Ask ask) {
+  // Tile j: its exponentials and its product with V beside the scores of tile j + 1, in an order that is pinned:
+  // behind each MFMA one or two LDS reads (of what is needed AHEAD MFMAs later) and as many vector instructions
+  // as run while the matrix pipe is busy with it.  s: tile j's scores; next: the next one's, whose largest is
+  // returned (MASK: of those that a lane's row attends to, below `lim`); `ask` (the next loads) is called behind
+  // the first MFMAs.
+  template <bool MASK, class Ask>
+  __device__ __forceinline__ float tile(acc_t (&next)[TT], const acc_t (&s)[TT], uint32_t k_place, uint32_t v_place, uint32_t k_at,
+                                        uint32_t v_at, float c, int32_t lim, Ask ask) {
     static_assert(ROWS == 32 && TT == 2 && PV == 4, "32 scores of a lane, 16 for each half of the second product");
-    constexpr int NQ = QK * TT, NV = PV * DT, AHEAD = 4, EXPS = NQ + NV / 2;
-    typedef const __attribute__((address_space(3))) bf16x8_t *frag_t;
+    constexpr int NQ = QK * TT, NV = PV * DT, EXPS = NQ + NV / 2;
     bf16x8_t kf[AHEAD];
     uint4 vf[AHEAD];
     uint32_t p[PAIRS];
     float even = 0.f, sum[2] = {0.f, 0.f}, top = -INFINITY;
-    auto read_k = [&](int i) { kf[i % AHEAD] = *(frag_t)(k_place + (k_at ^ (i / TT * (MK * 2))) + i % TT * (ROWS * ROWB)); };
+    const int32_t left = lim - 4 * (int32_t)(lane / ROWS);
     auto read_v = [&](int i) { vf[i % AHEAD] = values(v_place, v_at, i / DT, i % DT); };
     auto exps = [&](int slot) {                            // 32 scores to p, over the first EXPS slots
 #pragma unroll
       for (int i = slot * 32 / EXPS; i < (slot + 1) * 32 / EXPS; ++i) {
-        const float x = exp2(__builtin_fmaf(s[i / AN][i % AN], c, -ref));
+        const float x = exp2(__builtin_fmaf(s[i / AN][i % AN], c, -m));
         if (i & 1) p[i / 2] = pack(even, x);
         else even = x;
       }
     };
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) read_k(i);
+    for (int i = 0; i < AHEAD; ++i) kf[i] = key(k_place, k_at, i);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
       next[i % TT] = mma(kf[i % AHEAD], q[i / TT], i < TT ? acc_t{} : next[i % TT]);
-      if (i + AHEAD < NQ) read_k(i + AHEAD);
+      if (i + AHEAD < NQ) kf[i % AHEAD] = key(k_place, k_at, i + AHEAD);
       else read_v(i + AHEAD - NQ);
       exps(i);
       if (i == 1 || i == 3) ask(i / 2);
@@ -355,6 +371,7 @@ struct Flash {
       else {
 #pragma unroll
         for (int n = (i - NV / 2) * (64 / NV); n < (i - NV / 2 + 1) * (64 / NV); ++n) {
+          if (MASK) next[n / AN][n % AN] = (int32_t)token(n / AN, n % AN) < left ? next[n / AN][n % AN] : -INFINITY;
           top = fmaxf(top, next[n / AN][n % AN]);
           if (n & 1) sum[n / 2 & 1] = add_pair(p[n / 2], sum[n / 2 & 1]);
         }
@@ -367,14 +384,15 @@ struct Flash {
   }
 
   // Tokens [0, n) of K and V, `n` the same for all four waves; `mine` of them are seen by rows of this
-  // wave (none if 0).  A row attends to tokens below its `lim`; full: below that every row does.
-  // CAUSAL: there is data behind a row's last token (otherwise zeros).  `step(j)` is called behind
-  // the barrier of each tile.
+  // wave (none if 0).  A wave's rows attend to tokens below `lim`, or (CAUSAL) the first to those and each
+  // further one to one more; full: below that every row does, and what is left of `mine` is one tile at most.  `step(j)` is called behind the barrier of each tile.  What is behind
+  // a row's last token has a weight of zero, and has to be numbers where it is not zeros, unless `careful`.
+  //
+  // LDS is nobody else's when they are called.  CAUSAL: the block's rows of q come from `qs`; otherwise q is there.
   //
   // Where reading K and V is what bounds it: one item of the ring after the other.
-  template <bool CAUSAL, class Step>
+  template <class Step>
   __device__ __forceinline__ void run_lean(Src ks, Src vs, uint32_t n, uint32_t mine, uint32_t full, int32_t lim, float c, Step step) {
-    __syncthreads();                                       // (LDS may still be read for the block before)
     const uint32_t tiles = (n + TOK - 1) / TOK, have = (mine + TOK - 1) / TOK, whole = full / TOK;
 #pragma unroll
     for (int i = 0; i < NS - 1; ++i) ask(i & 1 ? vs : ks, i);
@@ -384,39 +402,20 @@ struct Flash {
     uint32_t place = 0;                                    // of item i; item i + NS - 1 goes to the place before it
     auto next = [&]() { place = place + 1 == NS ? 0 : place + 1; };
     auto before = [&]() { return place == 0 ? NS - 1 : place - 1; };
-    auto at = [&]() { return lds + place * PLACE; };
     constexpr bool V_FIRST = (NS - 1) & 1;                 // what item i + NS - 1 is, behind a K
-    uint32_t j = 0;
-    for (; j < whole && j < have; ++j) {
-      sync<(NS - 2) * L>();
-      ask(V_FIRST ? vs : ks, before());
-      step(j);
-      products<false>(s, at(), k_at, 0);
-      follow(largest(s), c);
-      exponentials(s, p, c);
-      next();
-      sync<(NS - 2) * L>();
-      ask(V_FIRST ? ks : vs, before());
-      add_values(p, at(), v_at);
-      next();
-    }
-    for (; j < tiles; ++j) {
-      const int32_t below = lim - (int32_t)(j * TOK);
+    for (uint32_t j = 0; j < tiles; ++j) {
       sync<(NS - 2) * L>();
       ask(V_FIRST ? vs : ks, before());
       step(j);
       if (j < have) {
-        products<true>(s, at(), opaque(k_at), below);
+        products(s, lds + place * PLACE, k_at);
+        if (j >= whole) hide(s, lim - (int32_t)(j * TOK));
         follow(largest(s), c);
-        exponentials(s, p, c);
       }
       next();
       sync<(NS - 2) * L>();
       ask(V_FIRST ? ks : vs, before());
-      if (j < have) {
-        if constexpr (CAUSAL) add_values_masked(p, at(), below);
-        else add_values(p, at(), v_at);
-      }
+      if (j < have) finish(s, p, lds + place * PLACE, v_at, c);
       next();
     }
     // what is still on its way is the zeros of items past the last one
@@ -429,19 +428,32 @@ struct Flash {
   // tile j's, K of tile j + 1 and V of tile j are in LDS, and tile j - 1's V and tile j's K are done with:
   // their places take those of tiles j + 1 and j + 2.
   template <bool CAUSAL, class Step>
-  __device__ __forceinline__ void run(Src ks, Src vs, uint32_t n, uint32_t mine, uint32_t full, int32_t lim, float c, Step step) {
-    static_assert(NS == 4, "two tiles");
-    __syncthreads();                                       // (LDS may still be read for the block before)
+  __device__ __forceinline__ void run(Src qs, Src ks, Src vs, uint32_t n, uint32_t mine, uint32_t full, int32_t lim, float c,
+                                      Step step, bool careful = false) {
+    static_assert(NS == 4 && BLOCK_ROWS == 2 * TOK, "two tiles, and q as one");
     const uint32_t tiles = (n + TOK - 1) / TOK, have = (mine + TOK - 1) / TOK;
     const uint32_t whole = full / TOK < have ? full / TOK : have;
+    auto below = [&](uint32_t j) { return lim + (CAUSAL ? (int32_t)(opaque(lane) % ROWS) : 0) - (int32_t)(j * TOK); };   // in tile j
+    if constexpr (CAUSAL) {                                // q's rows come as tokens of K do, and are read as those are
+      ask(qs, 2);
+      ask(qs, 3);
+    }
     ask(ks, 0);
-    ask(ks, 2);
     ask(vs, 1);
-    wait_q();
     acc_t s[2][TT];
-    sync<2 * L>();
+    if constexpr (CAUSAL) {
+      sync<L>();
+#pragma unroll
+      for (int k = 0; k < QK; ++k) q[k] = key(lds + (2 + wave / TT) * PLACE, k_at + wave % TT * (ROWS * ROWB), k * TT);
+      sync<L>();
+    } else {
+      wait_q();
+      sync<L>();
+    }
+    ask(ks, 2);
     if (have) {
-      products<true>(s[0], lds, opaque(k_at), lim);
+      products(s[0], lds, opaque(k_at));
+      if (whole == 0) hide(s[0], below(0));
       follow(largest(s[0]), c);
     }
     uint32_t j = 0;
@@ -449,9 +461,13 @@ struct Flash {
       constexpr int P = decltype(par)::value;
       sync<0>();
       step(j);
-      follow(tile(s[1 - P], s[P], lds + (2 - 2 * P) * PLACE, lds + (1 + 2 * P) * PLACE, c,
+      follow(tile<false>(s[1 - P], s[P], lds + (2 - 2 * P) * PLACE, lds + (1 + 2 * P) * PLACE, k_at, v_at, c, 0,
                          [&](int i) { i ? ask(vs, 3 - 2 * P) : ask(ks, 2 * P); }), c);
       ++j;
+    };
+    auto keep = [&]() {
+#pragma unroll
+      for (int t = 0; t < TT; ++t) s[0][t] = s[1][t];
     };
     while (j + 2 < whole) {
       both(std::integral_constant<int, 0>());
@@ -459,47 +475,44 @@ struct Flash {
     }
     if (j + 1 < whole) {
       both(std::integral_constant<int, 0>());
-#pragma unroll
-      for (int t = 0; t < TT; ++t) s[0][t] = s[1][t];
+      keep();
     }
-    // the last tile that every row sees whole, and those that end at the rows' own
-    for (; j < tiles; ++j) {
-      const uint32_t par = j & 1;
-      const int32_t below = lim - (int32_t)(j * TOK);
+    auto asks = [&](int i) { i ? ask(vs, 3 - 2 * (j & 1)) : ask(ks, 2 * (j & 1)); };
+    if (j < whole && whole < have) {                       // the last that every row sees whole
       sync<0>();
-      ask(ks, 2 * par);
-      ask(vs, 3 - 2 * par);
       step(j);
-      if (j < have) {
-        uint32_t p[PAIRS];
-        exponentials(s[0], p, c);
-        const uint32_t at = lds + (1 + 2 * par) * PLACE;
-        if constexpr (CAUSAL) add_values_masked(p, at, below);
-        else add_values(p, at, opaque(v_at));
-        if (j + 1 < have) {
-          products<true>(s[0], lds + (2 - 2 * par) * PLACE, opaque(k_at), below - TOK);
-          follow(largest(s[0]), c);
-        }
+      follow(tile<true>(s[1], s[0], lds + (2 - 2 * (j & 1)) * PLACE, lds + (1 + 2 * (j & 1)) * PLACE, opaque(k_at), opaque(v_at), c,
+                        below(j + 1), asks), c);
+      keep();
+      ++j;
+    }
+    if (j < have) {                                        // the last one
+      sync<0>();
+      step(j);
+      uint32_t p[PAIRS];
+      const uint32_t at = lds + (1 + 2 * (j & 1)) * PLACE;
+      if (j + 1 < tiles) {
+        asks(0);
+        asks(1);
       }
+      if (CAUSAL && careful) finish_careful(s[0], p, at, opaque(v_at), c, below(j));
+      else finish(s[0], p, at, opaque(v_at), c);
+      ++j;
+    }
+    for (; j < tiles; ++j) {                               // those of the other waves alone
+      sync<0>();
+      asks(0);
+      asks(1);
+      step(j);
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // (as above)
     l = over_row<AddOp>(l);
   }
 
-  // eight neighbouring dims of the lane's row, as bf16: of dims 16 g .. 16 g + 16 of block d the lane holds
-  // the first eight or the last (lanes of 32 x 32 blocks); returns where they start
-  __device__ __forceinline__ uint32_t eight(int d, int g, float by, uint4 &out) const {
-    static_assert(ROWS == 32, "the swap is made for these");
+  // four neighbouring dims of the lane's row, times `by`, as bf16: those from ROWS d + 8 g + 4 (l / ROWS) on
+  __device__ __forceinline__ uint2 four(int d, int g, float by) const {
     const acc_t &a = acc[d];
-    const int e = 8 * g;
-    out.x = pack(a[e] * by, a[e + 1] * by);
-    out.y = pack(a[e + 2] * by, a[e + 3] * by);
-    out.z = pack(a[e + 4] * by, a[e + 5] * by);
-    out.w = pack(a[e + 6] * by, a[e + 7] * by);
-    // the upper half's first four against the lower half's last four
-    asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(out.x), "+v"(out.z));
-    asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(out.y), "+v"(out.w));
-    return d * 32 + g * 16 + (lane >> 5) * 8;
+    return make_uint2(pack(a[4 * g] * by, a[4 * g + 1] * by), pack(a[4 * g + 2] * by, a[4 * g + 3] * by));
   }
 #endif
 };
@@ -573,38 +586,64 @@ struct PromptBodyT {
     f.begin(tally_dyn_lds);
     const uint32_t wrow = row0 + f.wave * F::ROWS;         // this wave's first row
     const uint32_t rows = wrow < len ? (len - wrow < (uint32_t)F::ROWS ? len - wrow : (uint32_t)F::ROWS) : 0u;
-    const uint64_t qrow = (uint64_t)first + (rows ? wrow : 0u);
-    f.read_q(a.q + qrow * LDQ + head * DIM, rows, LDQ);
+    const uint64_t qrow = (uint64_t)first + wrow;
     const uint32_t n = len < row0 + kPromptRows ? len : row0 + kPromptRows;
     uint32_t left = ctl.ticks, look = 0;
     const bool looks = YIELD && ctl.ticks != 0 && f.wave == 0;
     const buf_t flag = make_buf(ctl.flag, 4);
     if (YIELD && ctl.look_first && looks) yield_while_preempted(ctl, left);
-    // the pause word is asked for behind a tile's loads and the answer acted on a tile later (as in the GEMM)
-    f.template run<true>(f.source(a.k + (uint64_t)first * LDK + kv * DIM, n, LDK), f.source(a.v + (uint64_t)first * LDV + kv * DIM, n, LDV),
-                         n, rows ? wrow + rows : 0u, rows ? wrow + 1 : 0u, (int32_t)(wrow + f.lane % F::ROWS + 1),
-                         (a.scale > 0.f ? a.scale : DIM == 128 ? 0.08838834764831845f : 0.125f) * kLog2e, [&](uint32_t j) {
-                           if constexpr (YIELD) {
-                             if (!looks) return;
-                             if (j != 0 && ((j - 1) & ctl.mask) == ctl.mask && __builtin_amdgcn_readfirstlane(look) == ctl.epoch)
-                               yield_while_preempted(ctl, left);
-                             if ((j & ctl.mask) == ctl.mask) look = __builtin_amdgcn_raw_buffer_load_b32(flag, 0, 0, 16);
-                           }
-                         });
-    const float by = 1.f / f.l;
-    uint16_t *o = a.out + (qrow + f.lane % F::ROWS) * LDO + head * DIM;
+    const float c = (a.scale > 0.f ? a.scale : DIM == 128 ? 0.08838834764831845f : 0.125f) * kLog2e;
+    constexpr int FOURS = F::DT * F::AN / 4;
+    uint2 v[FOURS];
+    __syncthreads();                                       // (LDS may still be read for the block before)
+    __shared__ uint32_t s_none;
+    if (threadIdx.x == 0) s_none = 0;
+    // Once as if all of K and V were numbers; if an output of the block is none, again with care.
+    for (bool careful = false;; careful = true) {
+      // the pause word is asked for behind a tile's loads and the answer acted on a tile later (as in the GEMM)
+      f.template run<true>(f.source(a.q + ((uint64_t)first + row0) * LDQ + head * DIM, n - row0, LDQ), f.source(a.k + (uint64_t)first * LDK + kv * DIM, n, LDK), f.source(a.v + (uint64_t)first * LDV + kv * DIM, n, LDV),
+                           n, rows ? wrow + rows : 0u, rows ? wrow + 1 : 0u, (int32_t)wrow + 1, c, [&](uint32_t j) {
+                             if constexpr (YIELD) {
+                               if (!looks) return;
+                               if (j != 0 && ((j - 1) & ctl.mask) == ctl.mask && __builtin_amdgcn_readfirstlane(look) == ctl.epoch)
+                                 yield_while_preempted(ctl, left);
+                               if ((j & ctl.mask) == ctl.mask) look = __builtin_amdgcn_raw_buffer_load_b32(flag, 0, 0, 16);
+                             }
+                           }, careful);
+      const float by = 1.f / f.l;
+      float none = 0.f;                                    // zero times the outputs: NaN if one is no number
 #pragma unroll
-    for (int d = 0; d < F::DT; ++d)
-#pragma unroll
-      for (int g = 0; g < 2; ++g) {
-        uint4 v;
-        const uint32_t dim = f.eight(d, g, by, v);
-        const u32x4_nt w = {v.x, v.y, v.z, v.w};
-        if (f.lane % F::ROWS < rows) {
-          if constexpr (NT) __builtin_nontemporal_store(w, reinterpret_cast<u32x4_nt *>(o + dim));
-          else *reinterpret_cast<u32x4_nt *>(o + dim) = w;
-        }
+      for (int i = 0; i < FOURS; ++i) {
+        v[i] = f.four(i / (F::AN / 4), i % (F::AN / 4), by);
+        none = F::add_pair(v[i].x, none, 0u);
+        none = F::add_pair(v[i].y, none, 0u);
       }
+      if (f.lane % F::ROWS < rows && none != none) s_none = 1;
+      __syncthreads();
+      if (careful || s_none == 0) break;
+      f.reset();
+    }
+    // The wave's rows go through a piece of LDS of its own, so that whole rows are written.  (Straight from the
+    // registers an instruction would write 16 bytes here and there, 32 rows of them: 128 tokens 8.2 us and so 7.7.)
+    typedef __attribute__((address_space(3))) uint2 *four_t;
+    typedef const __attribute__((address_space(3))) u32x4_nt *chunk_t;
+    const uint32_t lane = F::opaque(f.lane), row = lane % F::ROWS, mine = f.lds + f.wave * (F::ROWS * F::ROWB);
+    constexpr uint32_t CHUNKS = F::ROWB / 16, PER = 64 / CHUNKS;   // rows that an instruction writes
+    // (a row's chunks are xor-swizzled as in the ring)
+#pragma unroll
+    for (int i = 0; i < FOURS; ++i)
+      *(four_t)(mine + row * F::ROWB + ((i ^ F::swz(row)) << 4) + lane / F::ROWS * 8) = v[i];
+    asm volatile("" ::: "memory");                         // (written in one type and read in another)
+    uint16_t *o = a.out + (qrow + lane / CHUNKS) * LDO + head * DIM + lane % CHUNKS * 8;
+#pragma unroll
+    for (uint32_t i = 0; i < F::ROWS / PER; ++i) {
+      const uint32_t r = i * PER + lane / CHUNKS;
+      const u32x4_nt w = *(chunk_t)(mine + r * F::ROWB + ((lane % CHUNKS ^ F::swz(r)) << 4));
+      if (r < rows) {
+        if constexpr (NT) __builtin_nontemporal_store(w, reinterpret_cast<u32x4_nt *>(o + (uint64_t)(i * PER) * LDO));
+        else *reinterpret_cast<u32x4_nt *>(o + (uint64_t)(i * PER) * LDO) = w;
+      }
+    }
 #endif
   }
 };

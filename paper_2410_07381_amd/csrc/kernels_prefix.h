@@ -63,7 +63,7 @@ inline size_t prefix_scratch_bytes(uint32_t batch, uint32_t heads, uint32_t kv_h
   return (size_t)batch * heads * (p.parts + p.own_parts) * (dim + 2) * sizeof(float);
 }
 
-// One workgroup's part: tokens [0, n) of K and V at `k` and `v` for rows [row0, row0 + rows) of a K/V head,
+// One workgroup's part, the only one it has: tokens [0, n) of K and V at `k` and `v` for rows [row0, row0 + rows) of a K/V head,
 // row r being query head r % group of sequence r / group.
 template <class F>
 __device__ __forceinline__ void prefix_part(const tally_attn_prefix_args &a, const PrefixPlan &p, unsigned char *lds_at, const uint16_t *k,
@@ -86,8 +86,8 @@ __device__ __forceinline__ void prefix_part(const tally_attn_prefix_args &a, con
   const float c = (a.scale > 0.f ? a.scale : F::DIM == 128 ? 0.08838834764831845f : 0.125f) * kLog2e;
   auto step = [](uint32_t) {};
   if (n != 0) {
-    if constexpr (F::ROWS == 16) f.template run_lean<false>(f.source(k, n, ld), f.source(v, n, ld), n, mine < rows ? n : 0u, n, (int32_t)n, c, step);
-    else f.template run<false>(f.source(k, n, ld), f.source(v, n, ld), n, mine < rows ? n : 0u, n, (int32_t)n, c, step);
+    if constexpr (F::ROWS == 16) f.run_lean(f.source(k, n, ld), f.source(v, n, ld), n, mine < rows ? n : 0u, n, (int32_t)n, c, step);
+    else f.template run<false>(typename F::Src(), f.source(k, n, ld), f.source(v, n, ld), n, mine < rows ? n : 0u, n, (int32_t)n, c, step);
   }
   if (!exists) return;
   const uint32_t parts = p.parts + p.own_parts;
@@ -173,10 +173,10 @@ __global__ __launch_bounds__(256) void attn_prefix_combine(tally_attn_prefix_arg
     if (mine + u * ROUND < parts) v[u] = *reinterpret_cast<const f32x4_t *>(rec + (uint64_t)(mine + u * ROUND) * DIM);
   }
   float2 own[2 * kPrefixParts / 64];
-  float top = -INFINITY;
+  float top = kNothing;
 #pragma unroll
   for (uint32_t i = 0; i < 2 * kPrefixParts / 64; ++i) {
-    own[i] = make_float2(-INFINITY, 0.f);
+    own[i] = make_float2(kNothing, 0.f);
     if (lane + 64 * i < parts) own[i] = ml[lane + 64 * i];
     top = fmaxf(top, own[i].x);
   }
@@ -184,7 +184,7 @@ __global__ __launch_bounds__(256) void attn_prefix_combine(tally_attn_prefix_arg
   float sum = 0.f;
 #pragma unroll
   for (uint32_t i = 0; i < 2 * kPrefixParts / 64; ++i) {
-    const float w = own[i].y == 0.f ? 0.f : __builtin_amdgcn_exp2f(own[i].x - (top == -INFINITY ? 0.f : top));
+    const float w = own[i].y == 0.f ? 0.f : __builtin_amdgcn_exp2f(own[i].x - top);
     sum += own[i].y == 0.f ? 0.f : own[i].y * w;
     if (wave == 0) s_w[lane + 64 * i] = w;
   }
