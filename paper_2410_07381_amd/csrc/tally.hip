@@ -591,14 +591,14 @@ uint32_t prefix_choice(const void *args, uint32_t, uint64_t *groups) {
   memcpy(&a, args, sizeof(a));
   const PrefixPlan p = prefix_plan(a);
   *groups = (uint64_t)p.prefix_groups + p.own_groups;
-  return (a.dim == 64 ? 2 : 0) + p.many;
+  return (a.dim == 64 ? 3 : 0) + p.kind;
 }
-template <int DIM, bool MANY>
+template <int DIM, int KIND>
 hipError_t footprint_prefix(uint32_t *lds_bytes, uint32_t *waves, uint32_t *regs_per_lane) {
   hipFuncAttributes attr;
-  hipError_t e = hipFuncGetAttributes(&attr, (const void *)attn_prefix_partial<DIM, MANY>);
+  hipError_t e = hipFuncGetAttributes(&attr, (const void *)attn_prefix_partial<DIM, KIND>);
   if (e != hipSuccess) return e;
-  *lds_bytes = (uint32_t)attr.sharedSizeBytes + prefix_lds<DIM, MANY>();
+  *lds_bytes = (uint32_t)attr.sharedSizeBytes + prefix_lds<DIM, KIND>();
   *waves = 4;
   *regs_per_lane = ((uint32_t)attr.numRegs + 7u) & ~7u;
   return hipSuccess;
@@ -764,7 +764,8 @@ const KernelOps kOps[TALLY_K_COUNT] = {
     OPS_DIM(PromptBody, PromptNarrowBody, "attn_prompt_bf16", grid_prompt),
     {"attn_prefix_bf16", sizeof(tally_attn_prefix_args), false, grid_prefix, launch_native_prefix,
      nullptr, nullptr, nullptr, nullptr, nullptr, nullptr,
-     {footprint_prefix<128, false>, footprint_prefix<128, true>, footprint_prefix<64, false>, footprint_prefix<64, true>},
+     {footprint_prefix<128, 0>, footprint_prefix<128, 1>, footprint_prefix<128, 2>, footprint_prefix<64, 0>, footprint_prefix<64, 1>,
+      footprint_prefix<64, 2>},
      prefix_choice, nullptr, nullptr, nullptr, nullptr, false, false},
     {"gemv_w4_bf16", sizeof(tally_gemv_w4_args), true, grid_gemv_w4, launch_native_w4, launch_sliced_w4, launch_ptb_w4,
      nullptr, occupancy_w4, pause_fraction_t<GemvW4T<1, 1>>, footprint_w4, {W4_ALL(W4_FOOT)},

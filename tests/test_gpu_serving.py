@@ -299,9 +299,16 @@ PREFIX = [
     (3, 4, 2, 128, 33, 64, [64, 63, 32]), (5, 7, 1, 128, 127, 65, [65, 0, 31, 33, 64]), (4, 12, 12, 64, 300, 20, [3, 0, 20, 7]),
     # nothing to attend to, lengths outside the cache
     (3, 2, 2, 128, 0, 40, [0, 40, -3]), (3, 2, 1, 64, 10, 8, [99, -1, 8]), (2, 2, 2, 64, 0, 0, None),
-    # more than 64 rows to a K/V head (128-row workgroups), several tiles of them, more than 64 heads to one
+    # more than 64 rows to a K/V head, several workgroups' worth of them, more than 64 heads to one
     (40, 4, 2, 128, 200, 9, "even"), (70, 8, 4, 64, 129, 3, "even"), (300, 1, 1, 128, 64, 2, "even"), (3, 96, 1, 128, 70, 90, [90, 0, 45]),
     (2, 140, 2, 64, 65, 66, [66, 1]), (1, 70, 1, 128, 40, 0, None),
+    # everything of a sequence in one workgroup: a prefix that ends inside a tile and as many as a wave has, long ones of many sequences
+    (3, 8, 4, 128, 200, 300, [300, 0, 77]), (2, 16, 1, 128, 128, 128, [128, 1]), (4, 6, 2, 64, 97, 900, [900, 0, 1, 31]),
+    (128, 4, 2, 64, 0, 1100, "even"), (130, 2, 2, 128, 7, 600, "even"),
+    # in parts: 16 rows of the prefix, more than 16, more than 64
+    (1, 16, 1, 128, 4000, 0, None), (2, 16, 2, 64, 2500, 1300, [1300, 1299]), (6, 8, 2, 64, 1500, 100, "even"), (20, 8, 2, 128, 700, 600, "even"),
+    # many rows and a long prefix (128-row workgroups): several of them, one of few rows, more than 16 heads to a K/V head
+    (40, 16, 1, 64, 13200, 40, "even"), (33, 10, 2, 128, 25500, 70, "even"), (3, 96, 1, 128, 29200, 90, [90, 0, 45]),
 ]
 
 
