@@ -29,11 +29,11 @@ namespace tally {
 
 constexpr uint32_t kW4Rows = 16, kW4Block = 128, kW4Vectors = 16, kW4MaxGroup = 1u << 20;
 constexpr int kW4Waves = 8;
-constexpr uint32_t kW4Staged = 24 * 1024;                  // bytes of LDS for the vectors, where they go there
+constexpr uint32_t kW4Staged = 22 * 1024;                  // bytes of LDS for the vectors, where they go there
 constexpr uint32_t kW4LongK = 8192;                        // ... from this k on
 constexpr uint32_t kW4Piece = 1024;                        // bytes of a vector that one direct load brings
 
-// bytes from a vector to the next in LDS: whole pieces, and a step that spreads them over the banks
+// bytes from a vector to the next in LDS: whole pieces, and a step that spreads them over the banks (not behind the last)
 __host__ __device__ constexpr uint32_t w4_pitch(uint32_t k) { return (k * 2 + kW4Piece - 1) / kW4Piece * kW4Piece + 64; }
 
 // Rows of tiles that a workgroup takes.  It reads x once for all of them (from the L2s, 24 bytes a clock and compute
@@ -59,7 +59,7 @@ inline uint32_t w4_rows(uint32_t m, uint32_t n) {
 // are then asked for while it waits for none of x.  (us, straight from the L2s / so, 1 vector: 4096 x 11008, groups of
 // 64 with zero points, 9.1 / 7.8; of 128 7.5 / 6.4; 11008 x 11008 13.4 / 12.8; but 11008 x 1024 3.4 / 3.8.)
 inline bool w4_staged(const tally_gemv_w4_args &a) {
-  return a.k >= kW4LongK && (uint64_t)a.m * w4_pitch(a.k) <= kW4Staged && w4_rows(a.m, a.n) == 1;
+  return a.k >= kW4LongK && (uint64_t)a.m * w4_pitch(a.k) - 64 <= kW4Staged && w4_rows(a.m, a.n) == 1;
 }
 
 // One tile of 16 rows by 128 weights, as loaded.  SUB: MFMAs of a tile that share a scale (groups of 32, of
@@ -152,7 +152,7 @@ struct W4Base {
 template <int SUB>
 struct GemvW4StagedT : W4Base<1> {
   static constexpr int MIN_WAVES = 7;                      // 72 registers: two waves fit beside a paused GEMM tile
-  static constexpr unsigned DYN_LDS = kW4Staged - 2048;
+  static constexpr unsigned DYN_LDS = kW4Staged;
   static constexpr int DEEP = 2;
   static __device__ __forceinline__ void run(const Args &a, uint32_t bx, uint32_t, uint32_t) { run_t(a, bx); }
   static __device__ __forceinline__ void run_be(const Args &a, uint32_t bx, uint32_t, uint32_t) { run_t(a, bx); }

@@ -401,7 +401,9 @@ def _w4_ok(got_bits, x, codes, scales, zeros, group):
 
 W4 = [(1, 1, 8, 32, False), (1, 16, 128, 128, True), (2, 17, 120, 32, True), (3, 15, 136, 64, False), (16, 33, 1000, 32, True),
       (5, 100, 512, 64, True), (4, 50, 640, 256, False), (16, 64, 1288, 128, True), (7, 31, 2056, 64, False), (1, 300, 4096, 128, False),
-      (9, 48, 4104, 384, True), (16, 16, 72, 64, True), (1, 40, 11008, 64, True)]
+      (9, 48, 4104, 384, True), (16, 16, 72, 64, True), (1, 40, 11008, 64, True),
+      # vectors that just fit into LDS, and that just do not
+      (1, 33, 11264, 128, False), (1, 33, 11272, 32, True), (1, 20, 11776, 64, False), (1, 16, 12000, 128, True)]
 
 
 @pytest.mark.parametrize("form", ["hi", "be", "sliced", "ptb"])
