@@ -80,13 +80,15 @@ struct W4Tile {
           zeros(make_buf(a.zeros ? a.zeros + (uint64_t)rows * groups * 16 : nullptr, a.zeros ? groups * 16 : 0)),
           inverse(SUB == 4 ? (0x7FFFFFFFu + a.group / kW4Block) / (a.group / kW4Block) : 0u), has_zeros(a.zeros != nullptr) {}
   };
-  // (past the last block nothing is read, and zeros come back)
-  __device__ __forceinline__ void load(const From &f, uint32_t b, uint32_t lane) {
-    w = buf_ld16(f.w, lane * 16, b * 1024);
+  // (unless it is `there` nothing is read, and zeros come back: the lanes' offsets are past any buffer's end)
+  __device__ __forceinline__ void load(const From &f, uint32_t b, uint32_t lane, bool there = true) {
+    const uint32_t none = there ? 0u : 0x80000000u;
+    b = there ? b : 0u;
+    w = buf_ld16(f.w, lane * 16 | none, b * 1024);
     const uint32_t at = SUB == 4 ? __umulhi(2 * b, f.inverse) * 16 + (lane & 15)
                                  : b * (4 / SUB) * 16 + (SUB == 1 ? lane : (lane >> 5) * 16 + (lane & 15));
-    scale = __builtin_amdgcn_raw_buffer_load_b16(f.scales, at * 2, 0, 0);
-    zero = f.has_zeros ? __builtin_amdgcn_raw_buffer_load_b8(f.zeros, at, 0, 0) : 8u;
+    scale = __builtin_amdgcn_raw_buffer_load_b16(f.scales, at * 2 | none, 0, 0);
+    zero = f.has_zeros ? __builtin_amdgcn_raw_buffer_load_b8(f.zeros, at | none, 0, 0) : 8u;
   }
   // acc += this tile's rows times the vectors; x(i): the vectors' 32 elements for MFMA i
   template <class X>
@@ -190,7 +192,7 @@ struct GemvW4StagedT : W4Base<1> {
             typedef const __attribute__((address_space(3))) bf16x8_t *frag_t;
             return *(frag_t)(at + mine * (kW4Block * 2) + i * 64);
           });
-        t[j].load(from, mine + DEEP * kW4Waves, lane);
+        t[j].load(from, mine + DEEP * kW4Waves, lane, mine + DEEP * kW4Waves < blocks);
       }
     }
     store(a, acc, tile, wave, lane);
