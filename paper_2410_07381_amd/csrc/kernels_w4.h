@@ -204,7 +204,7 @@ struct GemvW4StagedT : W4Base<1> {
 template <int SUB, int ROWS>
 struct GemvW4T : W4Base<ROWS> {
   using Args = tally_gemv_w4_args;
-  static constexpr int MIN_WAVES = ROWS <= 2 ? 8 : ROWS == 3 ? 7 : 4;   // (up to 72 registers: two waves fit beside a paused GEMM tile)
+  static constexpr int MIN_WAVES = ROWS == 2 ? 8 : ROWS == 3 || ROWS == 1 ? 7 : 4;   // (up to 72 registers: two waves fit beside a paused GEMM tile)
   static constexpr unsigned DYN_LDS = 0;
   static __device__ __forceinline__ void run(const Args &a, uint32_t bx, uint32_t, uint32_t) { run_t(a, bx); }
   static __device__ __forceinline__ void run_be(const Args &a, uint32_t bx, uint32_t, uint32_t) { run_t(a, bx); }
@@ -222,22 +222,45 @@ struct GemvW4T : W4Base<ROWS> {
     f32x4_t acc[ROWS];
 #pragma unroll
     for (int o = 0; o < ROWS; ++o) acc[o] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    for (uint32_t b = wave; b < blocks; b += kW4Waves) {
-      W4Tile<SUB> t[ROWS];
-      uint4 xv[4];
+    struct Stage { W4Tile<SUB> t[ROWS]; uint4 xv[4]; };
+    auto load = [&](Stage &s, uint32_t b) {
 #pragma unroll
       for (int o = 0; o < ROWS; ++o) {
         const uint32_t tile = block * ROWS + o;
         const typename W4Tile<SUB>::From from(a, tile < tiles ? tile : tiles - 1, blocks, groups);
-        t[o].load(from, b, lane);
+        s.t[o].load(from, b, lane, b < blocks);
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const uint32_t k1 = b * kW4Block + i * 32;
-        xv[i] = buf_ld16(x, k1 + k0 < a.k ? xrow + k1 * 2 : 0x80000000u, 0);
+        s.xv[i] = buf_ld16(x, k1 + k0 < a.k ? xrow + k1 * 2 : 0x80000000u, 0);
       }
+    };
+    auto add = [&](const Stage &s) {
 #pragma unroll
-      for (int o = 0; o < ROWS; ++o) t[o].add(acc[o], lane, [&](int i) { return __builtin_bit_cast(bf16x8_t, xv[i]); });
+      for (int o = 0; o < ROWS; ++o) s.t[o].add(acc[o], lane, [&](int i) { return __builtin_bit_cast(bf16x8_t, s.xv[i]); });
+    };
+    if constexpr (ROWS == 1) {
+      Stage s[2];
+      uint32_t b = wave;
+      load(s[0], b);
+      while (b < blocks) {
+        load(s[1], b + kW4Waves);
+        __builtin_amdgcn_sched_barrier(0);
+        add(s[0]);
+        b += kW4Waves;
+        if (b >= blocks) break;
+        load(s[0], b + kW4Waves);
+        __builtin_amdgcn_sched_barrier(0);
+        add(s[1]);
+        b += kW4Waves;
+      }
+    } else {
+      for (uint32_t b = wave; b < blocks; b += kW4Waves) {
+        Stage s;
+        load(s, b);
+        add(s);
+      }
     }
     W4Base<ROWS>::store(a, acc, block, wave, lane);
 #endif
