@@ -16,6 +16,12 @@
 // The eight waves of a workgroup share the tiles of a row of tiles and join their sums in LDS.  Which wave takes
 // a tile and in what order sums are added depends on k alone, so a result's bits depend neither on the
 // number of vectors nor on the variant.
+//
+// Measured (us; the codes, scales and zero points read once at 5.1 TB/s in brackets, and an empty launch is 2.4): 1 vector,
+// 4096 x 4096 3.5 [1.7], 4096 x 11008 in groups of 64 with zero points 7.7 [4.8]; 16 vectors, 11008 x 4096 8.3 [4.6]; 5 vectors,
+// 50257 x 4096 in groups of 32 with zero points 30.8 [23.9].  With many vectors a short product is bound by reading x
+// from the L2s once per workgroup (16 vectors, 4096 x 16384: 19.7 [7.3]).  Beginning the rows of tiles at different columns, so that
+// not all ask for the same x at once, gave 9.9 for 10.9 with 8 vectors, 16384 x 4096, and 33.1 for 31.5 with 5, 50257 x 4096.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -55,9 +61,9 @@ inline uint32_t w4_rows(uint32_t m, uint32_t n) {
   }
   return best;
 }
-// x goes to LDS where it fits and a wave has many tiles to take one after the other: the loads of the next
-// are then asked for while it waits for none of x.  (us, straight from the L2s / so, 1 vector: 4096 x 11008, groups of
-// 64 with zero points, 9.1 / 7.8; of 128 7.5 / 6.4; 11008 x 11008 13.4 / 12.8; but 11008 x 1024 3.4 / 3.8.)
+// x goes to LDS where it fits and a wave has many tiles to take one after the other, so that nothing but codes is
+// on its way in the loop.  (us, straight from the L2s / so, 1 vector: 4096 x 11008, groups of
+// 64 with zero points, 9.1 / 8.3; 11008 x 11008 13.9 / 12.8; 1024 x 11008, groups of 32, 8.4 / 7.6; but 11008 x 1024 3.4 / 3.8.)
 inline bool w4_staged(const tally_gemv_w4_args &a) {
   return a.k >= kW4LongK && (uint64_t)a.m * w4_pitch(a.k) - 64 <= kW4Staged && w4_rows(a.m, a.n) == 1;
 }
@@ -200,7 +206,10 @@ struct GemvW4StagedT : W4Base<1> {
   }
 };
 
-// x as each wave needs it, from the L2s, together with the codes of one tile of each row.
+// x as each wave needs it, from the L2s, together with the codes of one tile of each row.  With one row there are
+// often no more workgroups than compute units, and a wave's loads for its next tile are sent before it works on
+// this one (4 vectors, 4096 x 11008, 9.3 us, without 12.3; 8 vectors, 2048 x 8192, 8.2 and 10.0; but one vector, 11008
+// x 4096, where three workgroups share a compute unit, 7.3 and 7.1); more rows have no registers for that.
 template <int SUB, int ROWS>
 struct GemvW4T : W4Base<ROWS> {
   using Args = tally_gemv_w4_args;
