@@ -19,6 +19,12 @@
 // passed, which also says that everyone is done with item i - 1, whose place takes item i + NS - 1.
 // A place holds its rows' 16-byte chunks xor-swizzled by the row, so that the 16 lanes that a
 // 128-bit read serves at once, and the 16 tokens of a transposing read, fall into different banks.
+//
+// What bounds long prompts is the matrix pipe, and the clock that it is left with: 32768 tokens, 8 heads of 128 on one
+// K/V head, take 1.92 ms, 1.15 PFLOP/s (8192^3 of the GEMM tile: 1.5), with the pipe busy for 65 % of the cycles at 1.55 GHz.
+// 8192 tokens, 32/8 heads, 505 us (1.09); 4096, 32 heads, 140 (0.98); 16384, 16 heads of 64, 580 (0.95).
+// Short ones are a chain of latencies: 128 tokens, 12 heads of 64, 5.4 us, of which an empty launch is 2.4; 512
+// tokens, 32/8 heads of 128, 13.6.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -39,7 +45,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNothing = -3e38f;
 
 template <int DIM_, int ROWS_, int TOK_, int NS_>
-struct Flash {
+struct OnePass {
   static constexpr int DIM = DIM_, ROWS = ROWS_, TOK = TOK_, NS = NS_, WAVES = 4;
   static constexpr int BLOCK_ROWS = ROWS * WAVES;
   static constexpr uint32_t ROWB = DIM * 2;                // bytes of a token's row
@@ -144,8 +150,8 @@ struct Flash {
     else if constexpr (L == 2)
       asm volatile(OPEN_LDS LOAD_LDS("%2", "0") "\n\t" LOAD_LDS("%3", "0x400") ::"s"(to), "s"(b), "v"(r.voff[0]), "v"(r.voff[1]) : "memory");
     else
-      asm volatile(OPEN_LDS LOAD_LDS("%2", "0") "\n\t" LOAD_LDS("%3", "0x400") "\n\t" LOAD_LDS("%4", "0x800") "\n\t" LOAD_LDS("%5", "0xC00") ::"s"(to),
-                   "s"(b), "v"(r.voff[0]), "v"(r.voff[1]), "v"(r.voff[2]), "v"(r.voff[3])
+      asm volatile(OPEN_LDS LOAD_LDS("%2", "0") "\n\t" LOAD_LDS("%3", "0x400") "\n\t" LOAD_LDS("%4", "0x800") "\n\t" LOAD_LDS("%5", "0xC00")
+                   ::"s"(to), "s"(b), "v"(r.voff[0]), "v"(r.voff[1]), "v"(r.voff[2]), "v"(r.voff[3])
                    : "memory");
 #undef LOAD_LDS
 #undef OPEN_LDS
@@ -385,8 +391,9 @@ struct Flash {
 
   // Tokens [0, n) of K and V, `n` the same for all four waves; `mine` of them are seen by rows of this
   // wave (none if 0).  A wave's rows attend to tokens below `lim`, or (CAUSAL) the first to those and each
-  // further one to one more; full: below that every row does, and what is left of `mine` is one tile at most.  `step(j)` is called behind the barrier of each tile.  What is behind
-  // a row's last token has a weight of zero, and has to be numbers where it is not zeros, unless `careful`.
+  // further one to one more; full: below that every row does, and what is left of `mine` is one tile at
+  // most.  `step(j)` is called behind the barrier of each tile.  What is behind a row's last token has a weight
+  // of zero, and has to be numbers where it is not zeros, unless `careful`.
   //
   // LDS is nobody else's when they are called.  CAUSAL: the block's rows of q come from `qs`; otherwise q is there.
   //
@@ -529,7 +536,7 @@ inline uint32_t prompt_slots(const tally_attn_prompt_args &a) { return a.total /
 template <int DIM>
 struct PromptBodyT {
   using Args = tally_attn_prompt_args;
-  typedef Flash<DIM, 32, 64, 4> F;
+  typedef OnePass<DIM, 32, 64, 4> F;
   static constexpr int THREADS = 256;
   static constexpr int MIN_WAVES = 2;
   static constexpr unsigned DYN_LDS = F::LDS;
@@ -601,8 +608,10 @@ struct PromptBodyT {
     // Once as if all of K and V were numbers; if an output of the block is none, again with care.
     for (bool careful = false;; careful = true) {
       // the pause word is asked for behind a tile's loads and the answer acted on a tile later (as in the GEMM)
-      f.template run<true>(f.source(a.q + ((uint64_t)first + row0) * LDQ + head * DIM, n - row0, LDQ), f.source(a.k + (uint64_t)first * LDK + kv * DIM, n, LDK), f.source(a.v + (uint64_t)first * LDV + kv * DIM, n, LDV),
-                           n, rows ? wrow + rows : 0u, rows ? wrow + 1 : 0u, (int32_t)wrow + 1, c, [&](uint32_t j) {
+      f.template run<true>(f.source(a.q + ((uint64_t)first + row0) * LDQ + head * DIM, n - row0, LDQ),
+                           f.source(a.k + (uint64_t)first * LDK + kv * DIM, n, LDK),
+                           f.source(a.v + (uint64_t)first * LDV + kv * DIM, n, LDV), n, rows ? wrow + rows : 0u,
+                           rows ? wrow + 1 : 0u, (int32_t)wrow + 1, c, [&](uint32_t j) {
                              if constexpr (YIELD) {
                                if (!looks) return;
                                if (j != 0 && ((j - 1) & ctl.mask) == ctl.mask && __builtin_amdgcn_readfirstlane(look) == ctl.epoch)

@@ -22,7 +22,7 @@
 #include <string.h>
 
 #include "../../include/tally.h"
-#include "kernels_flash.h"
+#include "kernels_onepass.h"
 #include "kernels_stream.h"
 #include "launch_forms.h"
 
@@ -151,7 +151,7 @@ template <int DIM>
 __device__ __forceinline__ void lone_part(const tally_attn_prefix_args &a, const PrefixPlan &p, unsigned char *lds_at, const Span &one,
                                           const Span &two, uint32_t kv, uint32_t row0, uint32_t rows, uint32_t part) {
 #ifdef __HIP_DEVICE_COMPILE__
-  typedef Flash<DIM, 16, 32, 3> F;
+  typedef OnePass<DIM, 16, 32, 3> F;
   typedef typename F::s16x4_t s16x4_t;
   constexpr uint32_t PIECE = 4096, CHUNKS = DIM / 8;        // of LDS, for tokens of a wave; 16-byte chunks of a token
   constexpr int TOK = PIECE / F::ROWB, TURNS = 32 / TOK, BLOCKS = TOK / 16, LOADS = 4;   // of a piece
@@ -304,7 +304,7 @@ __device__ __forceinline__ void lone_part(const tally_attn_prefix_args &a, const
 
 template <int DIM, int KIND>
 constexpr unsigned prefix_lds() {
-  constexpr unsigned lone = 4 * 4096 + 16 * DIM * 2, shared = KIND == 2 ? Flash<DIM, 32, 64, 4>::LDS : KIND == 1 ? Flash<DIM, 16, 32, 3>::LDS : 0;
+  constexpr unsigned lone = 4 * 4096 + 16 * DIM * 2, shared = KIND == 2 ? OnePass<DIM, 32, 64, 4>::LDS : KIND == 1 ? OnePass<DIM, 16, 32, 3>::LDS : 0;
   return lone > shared ? lone : shared;
 }
 
@@ -312,10 +312,10 @@ template <int DIM, int KIND>
 __global__ __launch_bounds__(256, KIND == 2 ? 2 : 4) void attn_prefix_partial(tally_attn_prefix_args a, PrefixPlan p, uint32_t urgent) {
   if (urgent) __builtin_amdgcn_s_setprio(3);
   extern __shared__ __align__(1024) unsigned char tally_dyn_lds[];
-  typedef Flash<DIM, 16, 32, 3> Few;
-  typedef typename std::conditional<KIND == 2, Flash<DIM, 32, 64, 4>, Few>::type Shared;
+  typedef OnePass<DIM, 16, 32, 3> Few;
+  typedef typename std::conditional<KIND == 2, OnePass<DIM, 32, 64, 4>, Few>::type Shared;
   // (beside 128-row workgroups, of which a compute unit has two, in the LDS that those take)
-  typedef typename std::conditional<KIND == 2, Flash<DIM, 16, 32, 8>, Few>::type Own;
+  typedef typename std::conditional<KIND == 2, OnePass<DIM, 16, 32, 8>, Few>::type Own;
   static_assert(KIND == 0 || Own::LDS <= prefix_lds<DIM, KIND>(), "one size for both");
   uint32_t i = blockIdx.x;
   const uint32_t LDP = a.ld_prefix ? a.ld_prefix : a.kv_heads * DIM;
@@ -364,7 +364,7 @@ __global__ __launch_bounds__(256, KIND == 2 ? 2 : 4) void attn_prefix_partial(ta
   }
   lone_part<DIM>(a, p, tally_dyn_lds, one, two, kv, row0, rows, part);
 }
-static_assert(Flash<128, 16, 32, 3>::LDS + 1024 <= 31 * 1024, "room beside a paused 256 x 256 GEMM tile");
+static_assert(OnePass<128, 16, 32, 3>::LDS + 1024 <= 31 * 1024, "room beside a paused 256 x 256 GEMM tile");
 
 // One row per workgroup: the parts' weights exp(m - max) first, then each wave a quarter of the
 // parts, 16 bytes of a part's acc to a lane and eight loads at a time.  A part without tokens has l = 0 and its

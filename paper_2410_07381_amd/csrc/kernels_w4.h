@@ -177,7 +177,7 @@ struct GemvW4StagedT : W4Base<1> {
       const uint32_t v = i / pieces, c = i % pieces;
       const uint64_t p = (uint64_t)(uintptr_t)(a.x + (uint64_t)v * LDX);
       const u32x4_t b = {(uint32_t)p, (uint32_t)(p >> 32) & 0xFFFFu, a.k * 2, 0x00027000u};
-      // (as in Flash::ask, the waits too: what is past the vector's end is left as zeros)
+      // (as in OnePass::ask, the waits too: what is past the vector's end is left as zeros)
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                    ::"s"(lds + v * pitch + c * kW4Piece), "v"(lane * 16 + c * kW4Piece), "s"(b) : "memory");
     }

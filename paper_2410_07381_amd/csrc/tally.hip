@@ -22,7 +22,7 @@
 #include "admission.h"
 #include "gemm_cover.h"
 #include "kernels_attn.h"
-#include "kernels_flash.h"
+#include "kernels_onepass.h"
 #include "kernels_gemm.h"
 #include "kernels_prefix.h"
 #include "kernels_stream.h"
