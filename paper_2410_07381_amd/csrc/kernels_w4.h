@@ -118,11 +118,12 @@ struct W4Tile {
 #pragma unroll
         for (int j = 0; j < 4; ++j) q[j] = (word[i] >> (4 * j) & mask) | base;
         off = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xv, less, off, 0, 0, 0);
+        if (SUB == 1) part = off;
         part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xv, __builtin_bit_cast(bf16x8_t, make_uint4(q[0], q[1], q[2], q[3])), part, 0, 0, 0);
       }
       const float s = bf16_hi(u);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[e] = __builtin_fmaf(s, part[e] + off[e], acc[e]);
+      for (int e = 0; e < 4; ++e) acc[e] = __builtin_fmaf(s, SUB == 1 ? part[e] : part[e] + off[e], acc[e]);
     }
   }
 #endif
