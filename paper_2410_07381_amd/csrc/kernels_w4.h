@@ -19,7 +19,7 @@
 //
 // Measured (us; the codes, scales and zero points read once at 5.1 TB/s in brackets, and an empty launch is 2.4): 1 vector,
 // 4096 x 4096 3.5 [1.7], 4096 x 11008 in groups of 64 with zero points 7.7 [4.8]; 16 vectors, 11008 x 4096 8.3 [4.6]; 5 vectors,
-// 50257 x 4096 in groups of 32 with zero points 30.8 [23.9].  With many vectors a short product is bound by reading x
+// 50257 x 4096 in groups of 32 with zero points 30.0 [23.9].  With many vectors a short product is bound by reading x
 // from the L2s once per workgroup (16 vectors, 4096 x 16384: 19.7 [7.3]).  Beginning the rows of tiles at different columns, so that
 // not all ask for the same x at once, gave 9.9 for 10.9 with 8 vectors, 16384 x 4096, and 33.1 for 31.5 with 5, 50257 x 4096.
 #pragma once
@@ -110,7 +110,7 @@ struct W4Tile {
       const uint32_t u = SUB == 4 ? both : (uint32_t)__builtin_amdgcn_ds_bpermute((g * 16 + (lane & 15)) * 4, (int)both);
       const uint32_t cc = __builtin_amdgcn_perm(u, u, 0x01000100u);
       const bf16x8_t less = __builtin_bit_cast(bf16x8_t, make_uint4(cc, cc, cc, cc));
-      f32x4_t part = {0.f, 0.f, 0.f, 0.f}, off = {0.f, 0.f, 0.f, 0.f};   // (two chains: an MFMA waits for the one before)
+      f32x4_t part = {0.f, 0.f, 0.f, 0.f}, off = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int i = g; i < g + SUB; ++i) {
         const bf16x8_t xv = x(i);
@@ -118,6 +118,8 @@ struct W4Tile {
 #pragma unroll
         for (int j = 0; j < 4; ++j) q[j] = (word[i] >> (4 * j) & mask) | base;
         off = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xv, less, off, 0, 0, 0);
+        // (of 64 and more two chains, as an MFMA waits for the one before: 16 vectors, 11008 x 4096, 8.6 us, in one 9.1;
+        // of 32 one, which is short and saves additions: 5 vectors, 50257 x 4096, 30.3, in two 31.4)
         if (SUB == 1) part = off;
         part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(xv, __builtin_bit_cast(bf16x8_t, make_uint4(q[0], q[1], q[2], q[3])), part, 0, 0, 0);
       }
