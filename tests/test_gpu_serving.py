@@ -375,6 +375,87 @@ def test_prefix_strides_and_caches_beyond_32_bits(env):
     assert (got[:, heads:] == SENTINEL).all()
 
 
+# batch, heads, kv_heads, dim, prefix, own_cap: all of a sequence in a workgroup, and in parts of 16, 64 and 128 rows of the prefix
+WAYS = [(3, 4, 2, 64, 150, 200), (2, 16, 2, 128, 2200, 700), (3, 16, 2, 64, 2200, 700), (40, 96, 6, 128, 2200, 40)]
+
+
+@pytest.mark.parametrize("batch,heads,kv,dim,prefix,cap", WAYS)
+def test_prefix_large_scores(env, batch, heads, kv, dim, prefix, cap):
+    """A maximum that keeps rising, in the prefix and beyond it in a sequence's own tokens, to about e^10 times the
+    first weights.  (sum |q k| stays below 13: scores are off by 130 x 13 x 2^-24 < 2^-13.2, and numerator and
+    denominator by as much of M each, below 2^-12 together.)"""
+    B, ctx, torch = env
+    rng = np.random.default_rng(batch)
+    base = rng.standard_normal(dim)
+    base *= (dim / (base @ base)) ** 0.5
+    near = lambda shape, times: TI.to_bf16_bits((times * base + 0.3 * rng.standard_normal(shape)).astype(np.float32))
+    ramp = lambda n, lo, hi: np.linspace(lo, hi, n)[:, None, None]
+    q, K, Ko = near((batch, heads, dim), 1.0), near((prefix, kv, dim), ramp(prefix, 0.1, 1.0)), near((batch, cap, kv, dim), ramp(cap, 1.0, 1.6))
+    V, Vo = _bits(rng, (prefix, kv, dim)), _bits(rng, (batch, cap, kv, dim))
+    lens = [cap - 3 * b if b % 4 else 0 for b in range(batch)]
+    scale = 6.0 / dim
+    out = torch.zeros((batch, heads, dim), dtype=torch.int16, device="cuda")
+    kern = B.attn_prefix_bf16(*(_dev(torch, t) for t in (q, K, V, Ko, Vo)), torch.tensor([max(n, 0) for n in lens], dtype=torch.int32, device="cuda"),
+                              out, _scratch(B, torch, batch, heads, kv, dim, prefix, cap), scale=scale)
+    torch.cuda.synchronize()
+    _run(ctx, torch, kern, "hi")
+    want, mass = OS.attn_prefix(*(obf16.decode(t) for t in (q, K, V, Ko, Vo)), lens, scale)
+    _attn_ok(_host(out), want, mass)
+
+
+@pytest.mark.parametrize("batch,heads,kv,dim,prefix,cap", WAYS[1:])
+def test_prefix_tokens_as_far_apart_as_they_may_be(env, batch, heads, kv, dim, prefix, cap):
+    """2^20 elements between the prefix's tokens: more than 2^32 bytes in all, in each way of cutting a call up."""
+    B, ctx, torch = env
+    q, K, V, Ko, Vo = _prefix(batch + dim, batch, heads, kv, dim, prefix, cap)
+    lens = [(7 * b) % (cap + 1) for b in range(batch)]
+    far = torch.empty((prefix, 1 << 20), dtype=torch.int16, device="cuda")
+    K1, V1 = (far[:, at:at + kv * dim].unflatten(1, (kv, dim)) for at in (0, kv * dim))
+    K1.copy_(_dev(torch, K))
+    V1.copy_(_dev(torch, V))
+    out = torch.zeros((batch, heads, dim), dtype=torch.int16, device="cuda")
+    kern = B.attn_prefix_bf16(_dev(torch, q), K1, V1, _dev(torch, Ko), _dev(torch, Vo), torch.tensor(lens, dtype=torch.int32, device="cuda"),
+                              out, _scratch(B, torch, batch, heads, kv, dim, prefix, cap))
+    torch.cuda.synchronize()
+    _run(ctx, torch, kern, "hi")
+    got = _host(out)
+    del far, K1, V1, kern
+    want, mass = OS.attn_prefix(*(obf16.decode(t) for t in (q, K, V, Ko, Vo)), lens)
+    _attn_ok(got, want, mass)
+
+
+@pytest.mark.parametrize("batch,heads,kv,dim,prefix,cap", WAYS)
+def test_prefix_captured_twice_with_scratch_of_its_own(env, batch, heads, kv, dim, prefix, cap):
+    """Two graphs of the same call, replayed in turn and with eager calls between them; lengths change in place."""
+    B, ctx, torch = env
+    g = torch.Generator(device="cuda").manual_seed(6)
+    t = lambda *s: torch.randn(s, generator=g, device="cuda").to(torch.bfloat16)
+    q, K, V, Ko, Vo = t(batch, heads, dim), t(prefix, kv, dim), t(prefix, kv, dim), t(batch, cap, kv, dim), t(batch, cap, kv, dim)
+    lens = torch.full((batch,), cap, dtype=torch.int32, device="cuda")
+    outs = [torch.zeros_like(q) for _ in range(3)]
+    calls = [B.attn_prefix_bf16(q, K, V, Ko, Vo, lens, o, _scratch(B, torch, batch, heads, kv, dim, prefix, cap)) for o in outs]
+    torch.cuda.synchronize()
+    graphs = []
+    for kern in calls[:2]:
+        ctx.launch_native(kern, hi=True)
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=ctx._streams[0]):
+            ctx.launch_native(kern, hi=True)
+    for turn in range(4):
+        lens.copy_((torch.arange(batch, device="cuda") * (5 + turn) + turn) % (cap + 1))
+        q.copy_(torch.randn(q.shape, generator=g, device="cuda"))
+        torch.cuda.synchronize()
+        graphs[0].replay()
+        torch.cuda.synchronize()
+        ctx.launch_native(calls[2], hi=True)
+        torch.cuda.synchronize()
+        graphs[1].replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(o.view(torch.int16), outs[2].view(torch.int16)) for o in outs[:2]), turn
+        assert outs[2].float().abs().sum() > 0
+
+
 def test_prefix_is_not_transformable(env):
     B, ctx, torch = env
     z = torch.zeros((1, 1, 64), dtype=torch.int16, device="cuda")
