@@ -49,6 +49,9 @@ constexpr uint32_t kPrefixLeast = 128;                     // tokens of a part
 //
 // Parts: as many workgroups as one round on the GPU takes.  Kind 0 is better off with one per compute
 // unit, whose parts are longer (16 sequences of up to 3001, 4 heads: 14.1, with 512 of them 15.8, with 1024 16.9).
+// Where four waves share tokens (kind 1) a part is a longer chain than where each has its own: with mostly the latter,
+// parts of the prefix are shorter by a fourth (32 behind 4096 with up to 512, 8 heads: 18.8 against 19.7; 48 behind 2000 with
+// up to 300, heads of 64: 10.3 and 11.4; but 32 behind 4000 with up to 100, heads of 64: 12.7 and 12.0).
 struct PrefixPlan {
   uint32_t group, rows;                                    // query heads per K/V head; rows of one K/V head
   uint32_t kind;                                           // rows of a workgroup: 0: 16, 1: 64, 2: 128 of the prefix
@@ -69,15 +72,18 @@ inline PrefixPlan prefix_plan(uint32_t batch, uint32_t heads, uint32_t kv_heads,
   p.whole = 0;
   p.row_tiles = (uint32_t)up(p.rows, p.kind == 2 ? kPrefixManyRows : kPrefixFewRows);
   p.own_tiles = (uint32_t)up(p.group, kPrefixFewRows);
-  const uint64_t tokens = (uint64_t)kv_heads * p.row_tiles * prefix + (uint64_t)kv_heads * batch * p.own_tiles * own_cap;
-  uint64_t chunk = up(tokens, p.kind == 0 ? 256 : 512);
+  const uint64_t shared = (uint64_t)kv_heads * p.row_tiles * prefix, own = (uint64_t)kv_heads * batch * p.own_tiles * own_cap;
+  uint64_t chunk = up(shared + own, p.kind == 0 ? 256 : 512);
   if (chunk < kPrefixLeast) chunk = kPrefixLeast;
   auto parts = [&](uint32_t n, uint32_t &c, uint32_t &k) {
     const uint64_t least = up(n, kPrefixParts), w = chunk < least ? least : chunk < n ? chunk : n;
     c = (uint32_t)(up(w ? w : 1, 64) * 64);
     k = (uint32_t)up(n, c);
   };
+  const uint64_t own_chunk = chunk;
+  if (p.kind == 1 && own >= 2 * shared && chunk * 3 / 4 >= kPrefixLeast) chunk = chunk * 3 / 4;
   parts(prefix, p.chunk, p.parts);
+  chunk = own_chunk;
   parts(own_cap, p.own_chunk, p.own_parts);
   p.prefix_groups = kv_heads * p.row_tiles * p.parts;
   p.own_groups = kv_heads * batch * p.own_tiles * p.own_parts;
