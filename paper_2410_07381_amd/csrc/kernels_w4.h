@@ -45,18 +45,19 @@ __host__ __device__ constexpr uint32_t w4_pitch(uint32_t k) { return (k * 2 + kW
 // Rows of tiles that a workgroup takes.  It reads x once for all of them (from the L2s, 24 bytes a clock and compute
 // unit where all of them read the same): with many vectors that is more than the codes, so fewer workgroups
 // with more rows each are faster, as long as each of the 256 compute units has the same number of them.  Cost of
-// a workgroup: its rows, and a quarter of a row per vector; of equals the one with more rows.  More than 2 (3, 4)
-// rows did not pay with 4 or 5 (8, 16) vectors, and with 1 or 2 vectors only large products gain from a second.
-// us by rows, k = 4096, groups of 128: 1 vector, n = 11008 6.7 7.1 7.2, 50256 25.4 20.6 21.4; 4 vectors, 11008 8.3 7.5
-// 7.3 8.3, 16384 10.0 8.1 9.8 9.1; 16 vectors, 4096 5.9 6.7 7.4 8.3, 11008 13.8 11.0 8.0 8.8, 16384 17.5 11.1 12.6
-// 9.5, 50256 52.4 32.6 28.1 26.9.
+// a workgroup: its rows, and a quarter of a row per vector, and four rows' long way if there is nothing beside it; of
+// equals the one with more rows.  More than 2 (3, 4) rows did not pay with 4 or 5 (8, 16) vectors, and
+// with 1 or 2 vectors only large products gain from a second.
+// us by rows, groups of 128, k = 4096: 1 vector, n = 11008 7.2 8.0 7.6, 32000 14.8 14.5 14.7; 4 vectors, 11008 8.7 7.8
+// 7.8 9.8, 16384 10.7 8.5 10.3 11.2; 16 vectors, 4096 6.1 6.9 7.4 9.8, 11008 14.5 11.0 8.5 11.0, 16384 18.6 11.4 13.1
+// 12.6, 32000 34.6 19.5 18.0 16.1.
 inline uint32_t w4_rows(uint32_t m, uint32_t n) {
   const uint32_t tiles = (n + kW4Rows - 1) / kW4Rows, most = m <= 6 ? 2 : m <= 10 ? 3 : 4;
   if (m <= 2) return tiles > 1024 ? 2 : 1;
   uint32_t best = 1;
   uint64_t least = ~0ull;
   for (uint32_t r = 1; r <= most; ++r) {
-    const uint64_t groups = (tiles + r - 1) / r, cost = (groups + 255) / 256 * (4 * r + m);
+    const uint64_t groups = (tiles + r - 1) / r, cost = (groups + 255) / 256 * (4 * r + m) + (r == 4 && groups <= 256 ? 17 : 0);
     if (cost <= least) { least = cost; best = r; }
   }
   return best;
@@ -216,7 +217,7 @@ struct GemvW4StagedT : W4Base<1> {
 template <int SUB, int ROWS>
 struct GemvW4T : W4Base<ROWS> {
   using Args = tally_gemv_w4_args;
-  static constexpr int MIN_WAVES = ROWS == 2 ? 8 : ROWS == 3 || ROWS == 1 ? 7 : 4;   // (up to 72 registers: two waves fit beside a paused GEMM tile)
+  static constexpr int MIN_WAVES = ROWS <= 3 ? 7 : 4;   // (up to 72 registers: two waves fit beside a paused GEMM tile)
   static constexpr unsigned DYN_LDS = 0;
   static __device__ __forceinline__ void run(const Args &a, uint32_t bx, uint32_t, uint32_t) { run_t(a, bx); }
   static __device__ __forceinline__ void run_be(const Args &a, uint32_t bx, uint32_t, uint32_t) { run_t(a, bx); }

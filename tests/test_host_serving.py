@@ -93,7 +93,7 @@ def test_w4_refusals(B, bad):
 
 
 @pytest.mark.parametrize("m,n,rows", [(1, 1, 1), (1, 16384, 1), (2, 16385, 2), (4, 4096, 1), (4, 11008, 2), (8, 11008, 3), (8, 16384, 2),
-                                      (16, 4096, 1), (16, 11008, 3), (16, 16384, 4), (16, 50256, 4), (5, 50257, 2)])
+                                      (16, 4096, 1), (16, 11008, 3), (16, 16384, 2), (16, 32000, 4), (16, 50256, 4), (5, 50257, 2)])
 def test_w4_rows_of_tiles_by_vectors_and_rows(B, m, n, rows):
     """The rule's measured best: workgroups of as many rows as keep x from being read again and again, with the
     same number of workgroups on every compute unit."""
