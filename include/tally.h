@@ -133,9 +133,9 @@ typedef struct {
  * infinities included).  The values of cu_seqlens are read by the kernel: entries outside [0, total] count
  * as its ends, a sequence whose end lies before its start as empty; nothing outside the
  * tensors is touched.
- * Logical grid: heads x (total / 128 + n_seqs) blocks in one dimension, below 2^24; block heads x b + h owns up
- * to 128 rows of head h of one sequence s, which has the slots b from cu_seqlens[s] / 128 + s on that its
- * rows fill, last rows first. */
+ * Logical grid: heads x (total / 128 + n_seqs) blocks in one dimension, below 2^24; block heads x b + p owns up
+ * to 128 rows of one head (p, or with a multiple of eight heads p % 8 x heads / 8 + p / 8) of one sequence s, which
+ * has the slots b from cu_seqlens[s] / 128 + s on that its rows fill, last rows first. */
 typedef struct {
   const uint16_t *q; const uint16_t *k; const uint16_t *v; uint16_t *out;
   const int32_t *cu_seqlens;

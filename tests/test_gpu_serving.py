@@ -88,6 +88,8 @@ CASES = [
     # packed: empty sequences, single tokens, starts away from any tile, rows before and behind them
     ([0, 1, 1, 2, 66, 66, 193], 193, 4, 2, 128), ([5, 5, 20, 148, 150], 160, 3, 1, 64),
     ([0, 127, 128, 129, 257, 258], 300, 2, 2, 128), ([100, 229], 400, 1, 1, 128),
+    # as many heads as dies, and more
+    ([0, 300, 301, 450], 450, 8, 2, 64), ([0, 130, 500], 500, 16, 4, 128), ([3, 140], 150, 24, 24, 64),
 ]
 
 
