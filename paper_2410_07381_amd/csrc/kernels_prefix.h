@@ -102,6 +102,10 @@ inline size_t prefix_scratch_bytes(uint32_t batch, uint32_t heads, uint32_t kv_h
   return (size_t)batch * heads * (p.parts + p.own_parts) * (dim + 2) * sizeof(float);
 }
 
+// What stands for the sum of a part without tokens (a sum is never negative; that of tokens whose weights are all
+// zero in 32 bits is zero, and such a part's acc counts: zero times an infinity or NaN of V is NaN).
+constexpr float kNoTokens = -1.f;
+
 // Tokens of K and V, `ld` elements between them.
 struct Span { const uint16_t *k, *v; uint32_t ld, n; };
 
@@ -135,7 +139,7 @@ __device__ __forceinline__ void prefix_part(const tally_attn_prefix_args &a, con
   const uint32_t parts = p.parts + p.own_parts;
   const uint64_t at = ((uint64_t)b * a.heads + head) * parts + part;
   float2 *ml = reinterpret_cast<float2 *>(a.scratch);
-  if (f.lane < F::ROWS) ml[at] = make_float2(f.m, f.l);
+  if (f.lane < F::ROWS) ml[at] = make_float2(f.m, n != 0 ? f.l : kNoTokens);
   float *acc = reinterpret_cast<float *>(ml + (uint64_t)a.batch * a.heads * parts) + at * F::DIM + f.lane / F::ROWS * 4;
   if (n != 0) {
 #pragma unroll
@@ -300,7 +304,7 @@ __device__ __forceinline__ void lone_part(const tally_attn_prefix_args &a, const
   const uint32_t parts = p.parts + p.own_parts;
   const uint64_t to = ((uint64_t)out_b * a.heads + head) * parts + part;
   float2 *ml = reinterpret_cast<float2 *>(a.scratch);
-  if (piece == 0) ml[to] = make_float2(top, sum);
+  if (piece == 0) ml[to] = make_float2(top, tiles != 0 ? sum : kNoTokens);
   if (tiles == 0) return;
   float *acc = reinterpret_cast<float *>(ml + (uint64_t)a.batch * a.heads * parts) + to * DIM + piece * 4;
 #pragma unroll
@@ -373,8 +377,8 @@ __global__ __launch_bounds__(256, KIND == 2 ? 2 : 4) void attn_prefix_partial(ta
 static_assert(OnePass<128, 16, 32, 3>::LDS + 1024 <= 31 * 1024, "room beside a paused 256 x 256 GEMM tile");
 
 // One row per workgroup: the parts' weights exp(m - max) first, then each wave a quarter of the
-// parts, 16 bytes of a part's acc to a lane and eight loads at a time.  A part without tokens has l = 0 and its
-// acc was not written: what stands there is not added.
+// parts, 16 bytes of a part's acc to a lane and eight loads at a time.  A part without tokens says so in place of its
+// sum and its acc was not written: what stands there is not added (its weight is kNoTokens too, below any other).
 template <int DIM>
 __global__ __launch_bounds__(256) void attn_prefix_combine(tally_attn_prefix_args a, PrefixPlan p, uint32_t urgent) {
 #ifdef __HIP_DEVICE_COMPILE__
@@ -400,7 +404,7 @@ __global__ __launch_bounds__(256) void attn_prefix_combine(tally_attn_prefix_arg
   float top = kNothing;
 #pragma unroll
   for (uint32_t i = 0; i < 2 * kPrefixParts / 64; ++i) {
-    own[i] = make_float2(kNothing, 0.f);
+    own[i] = make_float2(kNothing, kNoTokens);
     if (lane + 64 * i < parts) own[i] = ml[lane + 64 * i];
     top = fmaxf(top, own[i].x);
   }
@@ -408,11 +412,12 @@ __global__ __launch_bounds__(256) void attn_prefix_combine(tally_attn_prefix_arg
   float sum = 0.f;
 #pragma unroll
   for (uint32_t i = 0; i < 2 * kPrefixParts / 64; ++i) {
-    const float w = own[i].y == 0.f ? 0.f : __builtin_amdgcn_exp2f(own[i].x - top);
-    sum += own[i].y == 0.f ? 0.f : own[i].y * w;
+    const bool none = own[i].y < 0.f;
+    const float w = none ? kNoTokens : __builtin_amdgcn_exp2f(own[i].x - top);
+    sum += none ? 0.f : own[i].y * w;
     if (wave == 0) s_w[lane + 64 * i] = w;
   }
-  if (wave == 0 && lane < ROUND * U) s_w[2 * kPrefixParts + lane] = 0.f;
+  if (wave == 0 && lane < ROUND * U) s_w[2 * kPrefixParts + lane] = kNoTokens;
   sum = wave_sum(sum);
   __syncthreads();
   f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
@@ -421,7 +426,7 @@ __global__ __launch_bounds__(256) void attn_prefix_combine(tally_attn_prefix_arg
     for (uint32_t u = 0; u < U; ++u) {
       const float w = s_w[i + u * ROUND];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[e] += w == 0.f ? 0.f : w * v[u][e];
+      for (int e = 0; e < 4; ++e) acc[e] += w < 0.f ? 0.f : w * v[u][e];
     }
     i += ROUND * U;
     if (i - mine >= parts) break;                          // (the same for every lane)

@@ -458,6 +458,48 @@ def test_prefix_captured_twice_with_scratch_of_its_own(env, batch, heads, kv, di
         assert outs[2].float().abs().sum() > 0
 
 
+@pytest.mark.parametrize("poison", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("low", ["prefix", "own"])
+@pytest.mark.parametrize("batch,heads,kv,dim,prefix,cap", WAYS)
+def test_prefix_what_a_token_holds_is_seen_whatever_its_weight(env, batch, heads, kv, dim, prefix, cap, low, poison):
+    """V of one token is no number, in a stretch of tokens (the first half of the prefix, or a sequence's own) whose
+    scores lie 300 below the others': its weight is zero in 32 bits, and zero times it is not zero.
+    (Scores of magnitude S are off by (dim + 2) S 2^-24, and p by as much of itself, in numerator and denominator.)"""
+    B, ctx, torch = env
+    rng = np.random.default_rng(batch + dim)
+    base = rng.standard_normal(dim)
+    base *= (dim / (base @ base)) ** 0.5
+    near = lambda shape, times: (times * base + 0.1 * rng.standard_normal(shape)).astype(np.float32)
+    q, K, Ko = near((batch, heads, dim), 1.0), near((prefix, kv, dim), 1.0), near((batch, cap, kv, dim), 1.0)
+    V, Vo = _bits(rng, (prefix, kv, dim)), _bits(rng, (batch, cap, kv, dim))
+    lens = [cap - b % 4 for b in range(batch)]
+    hit = rng.integers(0, prefix // 2), rng.integers(0, min(lens))
+    bad = TI.to_bf16_bits(np.float32([poison]))[0]
+    clean = V.copy(), Vo.copy()
+    if low == "prefix":
+        K[:prefix // 2] *= -1
+        V[hit[0], kv - 1, 5:9] = bad
+    else:
+        Ko *= -1
+        Vo[batch - 1, hit[1], kv - 1, 5:9] = bad
+    q, K, Ko = (TI.to_bf16_bits(t) for t in (q, K, Ko))
+    scale = 150.0 / dim
+    out = torch.zeros((batch, heads, dim), dtype=torch.int16, device="cuda")
+    kern = B.attn_prefix_bf16(*(_dev(torch, t) for t in (q, K, V, Ko, Vo)), torch.tensor(lens, dtype=torch.int32, device="cuda"),
+                              out, _scratch(B, torch, batch, heads, kv, dim, prefix, cap), scale=scale)
+    torch.cuda.synchronize()
+    _run(ctx, torch, kern, "hi")
+    qd, Kd, Kod = (obf16.decode(t) for t in (q, K, Ko))
+    want, mass = OS.attn_prefix(qd, Kd, obf16.decode(clean[0]), Kod, obf16.decode(clean[1]), lens, scale)
+    hits = np.zeros(want.shape, bool)
+    hits[0 if low == "prefix" else batch - 1:, heads - heads // kv:, 5:9] = True
+    got = obf16.decode(_host(out))
+    assert not np.isfinite(got[hits]).any()
+    S = scale * np.sqrt((qd ** 2).sum(-1).max() * max((Kd ** 2).sum(-1).max(), (Kod ** 2).sum(-1).max()))
+    bound = 2.0 ** -8 * np.abs(want) + (2.0 ** -8 + 2.0 ** -12 + 2 * (dim + 2) * S * 2.0 ** -24) * mass
+    assert (np.abs(got - want) <= bound)[~hits].all()
+
+
 def test_prefix_is_not_transformable(env):
     B, ctx, torch = env
     z = torch.zeros((1, 1, 64), dtype=torch.int16, device="cuda")
