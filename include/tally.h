@@ -147,7 +147,8 @@ typedef struct {
 /* Single-token attention of a batch behind a shared prefix: query head h of sequence b attends to the
  * prefix's tokens and to the first own_len[b] of its own,
  *   out[b][h] = sum_t p_t v_t / sum_t p_t,  p_t = exp(scale q[b][h] . k_t),
- * with k_t and v_t those of K/V head h / (heads / kv_heads).  Zeros where there is no token at all.
+ * with k_t and v_t those of K/V head h / (heads / kv_heads).  Zeros where there is no token at all (where
+ * there are, and all scores are -inf, NaN).
  * q, out: batch x heads x dim; K, V: prefix x kv_heads x dim; Ko, Vo: batch x own_cap x kv_heads x dim; all
  * bf16.  heads a multiple of kv_heads, dim 64 or 128.  prefix or own_cap may be 0 (their pointers
  * are then not looked at; own_len neither without own_cap).  own_len: batch int32 in DEVICE memory; values

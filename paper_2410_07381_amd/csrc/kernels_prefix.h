@@ -293,7 +293,7 @@ __device__ __forceinline__ void lone_part(const tally_attn_prefix_args &a, const
   for (int i = 0; i < 4; ++i) sum += s_ml[i][r].y * F::exp2(s_ml[i][r].x - top);
   const uint32_t out_b = (row0 + r) / p.group, head = kv * p.group + (row0 + r) % p.group;
   if (p.whole) {
-    const float over = sum == 0.f ? 0.f : 1.f / sum;
+    const float over = tiles == 0 ? 0.f : 1.f / sum;        // (scores of -inf throughout: NaN, as in a prompt)
     uint16_t *out = a.out + (uint64_t)out_b * (a.ld_out ? a.ld_out : a.heads * DIM) + head * DIM + piece * 4;
 #pragma unroll
     for (int h = 0; h < 2; ++h)
@@ -410,15 +410,18 @@ __global__ __launch_bounds__(256) void attn_prefix_combine(tally_attn_prefix_arg
   }
   top = wave_max(top);
   float sum = 0.f;
+  bool any = false;
 #pragma unroll
   for (uint32_t i = 0; i < 2 * kPrefixParts / 64; ++i) {
     const bool none = own[i].y < 0.f;
+    any |= !none;
     const float w = none ? kNoTokens : __builtin_amdgcn_exp2f(own[i].x - top);
     sum += none ? 0.f : own[i].y * w;
     if (wave == 0) s_w[lane + 64 * i] = w;
   }
   if (wave == 0 && lane < ROUND * U) s_w[2 * kPrefixParts + lane] = kNoTokens;
   sum = wave_sum(sum);
+  any = __builtin_amdgcn_ballot_w64(any) != 0;             // (the same for every wave)
   __syncthreads();
   f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
   for (uint32_t i = mine;;) {
@@ -451,7 +454,7 @@ __global__ __launch_bounds__(256) void attn_prefix_combine(tally_attn_prefix_arg
     const uint32_t d = threadIdx.x;
     const float o = (s_acc[0][d] + s_acc[1][d]) + (s_acc[2][d] + s_acc[3][d]);
     const uint32_t LDO = a.ld_out ? a.ld_out : a.heads * DIM;
-    a.out[(uint64_t)b * LDO + head * DIM + d] = f32_to_bf16(sum == 0.f ? 0.f : o / sum);
+    a.out[(uint64_t)b * LDO + head * DIM + d] = f32_to_bf16(any ? o / sum : 0.f);
   }
 #endif
 }

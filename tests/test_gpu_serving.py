@@ -500,6 +500,24 @@ def test_prefix_what_a_token_holds_is_seen_whatever_its_weight(env, batch, heads
     assert (np.abs(got - want) <= bound)[~hits].all()
 
 
+@pytest.mark.parametrize("batch,heads,kv,dim,prefix,cap", WAYS + [(2, 16, 2, 128, 0, 3000), (2, 4, 2, 64, 0, 60)])
+def test_prefix_without_a_token_gives_zeros_and_without_a_finite_score_none(env, batch, heads, kv, dim, prefix, cap):
+    """Scores of -inf throughout have no softmax: NaN, as in a prompt.  Zeros stand where there is no token."""
+    B, ctx, torch = env
+    q, K, V, Ko, Vo = _prefix(batch, batch, heads, kv, dim, prefix, cap)
+    q = q & np.uint16(0x7FFF) | np.uint16(0x3C00)          # (positive, so that no product is +inf)
+    K[:], Ko[:] = 0xFF80, 0xFF80
+    lens = [0 if b % 2 else cap for b in range(batch)]
+    out = torch.full((batch, heads, dim), SENTINEL, dtype=torch.int16, device="cuda")
+    kern = B.attn_prefix_bf16(*(_dev(torch, t) for t in (q, K, V, Ko, Vo)), torch.tensor(lens, dtype=torch.int32, device="cuda"),
+                              out, _scratch(B, torch, batch, heads, kv, dim, prefix, cap))
+    torch.cuda.synchronize()
+    _run(ctx, torch, kern, "hi")
+    got = obf16.decode(_host(out))
+    for b, n in enumerate(lens):
+        assert np.isnan(got[b]).all() if prefix + n else (got[b] == 0).all(), b
+
+
 def test_prefix_is_not_transformable(env):
     B, ctx, torch = env
     z = torch.zeros((1, 1, 64), dtype=torch.int16, device="cuda")
