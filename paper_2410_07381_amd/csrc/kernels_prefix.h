@@ -97,9 +97,14 @@ inline PrefixPlan prefix_plan(uint32_t batch, uint32_t heads, uint32_t kv_heads,
   }
   return p;
 }
+// Scratch: (max, sum) of each row's parts, and behind them, from a multiple of 16 bytes on, each part's acc.
+__host__ __device__ inline uint64_t prefix_records(uint32_t batch, uint32_t heads, const PrefixPlan &p) {
+  return (uint64_t)batch * heads * (p.parts + p.own_parts);
+}
+__host__ __device__ inline uint64_t prefix_acc_at(uint64_t records) { return (records * 2 + 3) / 4 * 4; }   // in floats
 inline size_t prefix_scratch_bytes(uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t dim, uint32_t prefix, uint32_t own_cap) {
-  const PrefixPlan p = prefix_plan(batch, heads, kv_heads, dim, prefix, own_cap);
-  return (size_t)batch * heads * (p.parts + p.own_parts) * (dim + 2) * sizeof(float);
+  const uint64_t n = prefix_records(batch, heads, prefix_plan(batch, heads, kv_heads, dim, prefix, own_cap));
+  return (size_t)(prefix_acc_at(n) + n * dim) * sizeof(float);
 }
 
 // What stands for the sum of a part without tokens (a sum is never negative; that of tokens whose weights are all
@@ -140,7 +145,7 @@ __device__ __forceinline__ void prefix_part(const tally_attn_prefix_args &a, con
   const uint64_t at = ((uint64_t)b * a.heads + head) * parts + part;
   float2 *ml = reinterpret_cast<float2 *>(a.scratch);
   if (f.lane < F::ROWS) ml[at] = make_float2(f.m, n != 0 ? f.l : kNoTokens);
-  float *acc = reinterpret_cast<float *>(ml + (uint64_t)a.batch * a.heads * parts) + at * F::DIM + f.lane / F::ROWS * 4;
+  float *acc = static_cast<float *>(a.scratch) + prefix_acc_at(prefix_records(a.batch, a.heads, p)) + at * F::DIM + f.lane / F::ROWS * 4;
   if (n != 0) {
 #pragma unroll
     for (int d = 0; d < F::DT; ++d)
@@ -306,7 +311,7 @@ __device__ __forceinline__ void lone_part(const tally_attn_prefix_args &a, const
   float2 *ml = reinterpret_cast<float2 *>(a.scratch);
   if (piece == 0) ml[to] = make_float2(top, tiles != 0 ? sum : kNoTokens);
   if (tiles == 0) return;
-  float *acc = reinterpret_cast<float *>(ml + (uint64_t)a.batch * a.heads * parts) + to * DIM + piece * 4;
+  float *acc = static_cast<float *>(a.scratch) + prefix_acc_at(prefix_records(a.batch, a.heads, p)) + to * DIM + piece * 4;
 #pragma unroll
   for (int h = 0; h < 2; ++h) *reinterpret_cast<f32x4_t *>(acc + h * (DIM / 2)) = o[h];
 #endif
@@ -390,8 +395,7 @@ __global__ __launch_bounds__(256) void attn_prefix_combine(tally_attn_prefix_arg
   const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const uint64_t row = (uint64_t)b * a.heads + head;
   const float2 *ml = reinterpret_cast<const float2 *>(a.scratch) + row * parts;
-  const float *rec = reinterpret_cast<const float *>(reinterpret_cast<const float2 *>(a.scratch) + (uint64_t)a.batch * a.heads * parts) +
-                     row * parts * DIM + lane % LANES * 4;
+  const float *rec = static_cast<const float *>(a.scratch) + prefix_acc_at(prefix_records(a.batch, a.heads, p)) + row * parts * DIM + lane % LANES * 4;
   const uint32_t mine = wave * SIDE + lane / LANES;
   // (the first round's loads do not wait for the weights)
   f32x4_t v[U];

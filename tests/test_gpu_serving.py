@@ -518,6 +518,24 @@ def test_prefix_without_a_token_gives_zeros_and_without_a_finite_score_none(env,
         assert np.isnan(got[b]).all() if prefix + n else (got[b] == 0).all(), b
 
 
+@pytest.mark.parametrize("batch,heads,kv,dim,prefix,cap,lens", [(1, 7, 1, 128, 4000, 64, [64]), (1, 1, 1, 64, 4480, 0, [0]),
+                                                                (1, 35, 5, 64, 1100, 700, [699])])
+def test_prefix_with_an_odd_number_of_partial_results(env, batch, heads, kv, dim, prefix, cap, lens):
+    """The weighted sums in scratch begin at a multiple of 16 bytes, and end where the scratch does."""
+    B, ctx, torch = env
+    q, K, V, Ko, Vo = _prefix(heads + prefix, batch, heads, kv, dim, prefix, cap)
+    n = B.attn_prefix_scratch_bytes(batch, heads, kv, dim, prefix, cap)
+    assert n % 16 == 0 and (n // (dim * 4 + 8)) % 2 == 1   # (an odd number of records of dim floats and two)
+    room = torch.full((n + 64,), 0x7F, dtype=torch.uint8, device="cuda")
+    out = torch.zeros((batch, heads, dim), dtype=torch.int16, device="cuda")
+    kern = B.attn_prefix_bf16(*(_dev(torch, t) for t in (q, K, V, Ko, Vo)), torch.tensor(lens, dtype=torch.int32, device="cuda"), out, room)
+    torch.cuda.synchronize()
+    _run(ctx, torch, kern, "hi")
+    want, mass = OS.attn_prefix(*(obf16.decode(t) for t in (q, K, V, Ko, Vo)), lens)
+    _attn_ok(_host(out), want, mass)
+    assert (room[n:] == 0x7F).all()
+
+
 def test_prefix_is_not_transformable(env):
     B, ctx, torch = env
     z = torch.zeros((1, 1, 64), dtype=torch.int16, device="cuda")

@@ -82,6 +82,14 @@ def test_prefix_without_a_part_does_not_look_at_its_pointers(B):
         assert B.attn_prefix_scratch_bytes(*refused) == 0
 
 
+@pytest.mark.parametrize("batch,heads,kv,dim,prefix,cap,records", [(1, 7, 1, 128, 4000, 64, 231), (1, 1, 1, 64, 300, 0, 3),
+                                                                   (3, 5, 5, 64, 2000, 0, 240), (1, 7, 1, 128, 3968, 128, 224)])
+def test_prefix_scratch_keeps_the_weighted_sums_aligned(B, batch, heads, kv, dim, prefix, cap, records):
+    """A record of (max, sum) for each row's parts, then from a multiple of 16 bytes on, with odd numbers of them too,
+    the parts' weighted sums, which are read and written 16 bytes at a time."""
+    assert B.attn_prefix_scratch_bytes(batch, heads, kv, dim, prefix, cap) == -(-records * 8 // 16) * 16 + records * dim * 4
+
+
 @pytest.mark.parametrize("bad", [
     dict(x=None), dict(W=None), dict(scales=None), dict(y=None), dict(x=P + 8), dict(W=P + 4), dict(m=0), dict(m=17),
     dict(n=0), dict(k=0), dict(k=252), dict(group=0), dict(group=16), dict(group=96), dict(group=192), dict(ld_x=248),
