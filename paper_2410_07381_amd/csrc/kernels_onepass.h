@@ -36,6 +36,7 @@
 #include "kernels_gemm.h"
 #include "kernels_stream.h"
 #include "launch_forms.h"
+#include "turnaround.h"
 
 namespace tally {
 
@@ -525,10 +526,6 @@ struct OnePass {
 };
 
 // ---- a whole prompt ---------------------------------------------------------------------
-constexpr uint32_t kPromptRows = 128;                      // rows of a logical block
-
-inline uint32_t prompt_slots(const tally_attn_prompt_args &a) { return a.total / kPromptRows + a.n_seqs; }
-
 // Logical block heads x slot + nth: 128 rows of one sequence for one query head.  (With a multiple of eight heads those that
 // share a K/V head are dealt to one die, every eighth block's, as far as they are neighbours: one sequence of 700
 // tokens, 32/8 heads, 15.0 us, in the heads' own order 15.6; long ones the same.)  Where sequences begin is
@@ -545,13 +542,8 @@ struct PromptBodyT {
   static constexpr bool END_BARRIER = false;               // (a block opens with a barrier)
   static constexpr bool YIELDS = true;
   static constexpr bool RANGE = false;
-  static_assert(F::BLOCK_ROWS == (int)kPromptRows, "rows of a block");
-  // share of the longest block between two looks at the pause word, `every` tiles apart, and the
-  // tile after, in which the answer is acted on
-  static double pause_fraction(const Args &a, uint32_t every) {
-    const uint32_t tiles = (a.total + F::TOK - 1) / F::TOK;
-    return tiles > every + 1 ? (double)(every + 1) / tiles : 1.0;
-  }
+  static_assert(F::BLOCK_ROWS == (int)kPromptRows && F::TOK == (int)kPromptTile, "rows of a block, tokens of a tile");
+  static double pause_fraction(const Args &a, uint32_t every) { return prompt_pause_share(a, every); }
   static __device__ __forceinline__ void run(const Args &a, uint32_t bx, uint32_t, uint32_t) {
     run_impl<false, false>(a, bx, YieldCtl{nullptr, 0, 0, 15, false});
   }

@@ -28,6 +28,7 @@
 #include "kernels_stream.h"
 #include "kernels_w4.h"
 #include "launch_forms.h"
+#include "turnaround.h"
 
 using namespace tally;
 
@@ -1879,9 +1880,7 @@ int tally_stream_report(tally_ctx *ctx, int *be_delays_hi, uint32_t *set_aside) 
 // ------------------------------------------------------------------ configuration choice
 double tally_ptb_turnaround_ms(double kernel_latency_ms, uint32_t worker_blocks, uint32_t chunk,
                                uint64_t total_blocks) {
-  if (total_blocks == 0) return 0.0;
-  return kernel_latency_ms * (double)worker_blocks * (double)(chunk ? chunk : 1) /
-         (double)total_blocks;
+  return eq1_turnaround_ms(kernel_latency_ms, worker_blocks, chunk, total_blocks);
 }
 
 int tally_select_config(const tally_config *c, uint32_t n, double threshold_ms) {
@@ -1922,13 +1921,11 @@ void fill_turnaround(tally_ctx *ctx, const KernelOps *ops, const void *args, uin
   if (c->kind == 0) {
     uint32_t whole = 0;
     const uint32_t parts = segment_parts(ops, total, total, c->param, c->chunk ? c->chunk : 1, &whole);
-    // a body that pauses inside its blocks hands the execution units over after a share
-    // of ONE block, whatever the chunk: Eq. 1 with chunk 1, times that share
     const double share = ctx->yield_ticks ? ops->pause_fraction(args, ctx->yield_every, parts, whole) : 1.0;
     if (parts > 1 && !whole)   // one part per worker, all of them at once: a part lasts as long as the kernel
       c->turnaround_ms = (float)(c->latency_ms * share);
     else
-      c->turnaround_ms = (float)(tally_ptb_turnaround_ms(c->latency_ms, c->param, share < 1.0 || !c->chunk ? 1 : c->chunk, total) * share);
+      c->turnaround_ms = (float)workers_turnaround_ms(c->latency_ms, c->param, c->chunk, total, share);
   } else {
     // one slice's time, times the number of slices that may be enqueued at once
     uint64_t slices = (total + c->param - 1) / c->param;

@@ -158,3 +158,61 @@ def test_the_binding_checks_shapes_and_strides(B):
                  (x[:1].expand(2, 256), W, s, y)):
         with pytest.raises(AssertionError):
             B.gemv_w4_bf16(*args)
+
+
+@pytest.fixture(scope="module")
+def estimate(tmp_path_factory):
+    """The turnaround estimate of prompts as workers: for every (latency us, workers, chunk, looks every, heads, total, n_seqs)."""
+    import os
+    import subprocess
+    src = tmp_path_factory.mktemp("turnaround") / "turnaround.cpp"
+    src.write_text(r"""
+#include <cstdio>
+#include "turnaround.h"
+using namespace tally;
+int main() {
+  tally_attn_prompt_args a{};
+  double us;
+  uint32_t workers, chunk, every;
+  while (scanf("%lf %u %u %u %u %u %u", &us, &workers, &chunk, &every, &a.heads, &a.total, &a.n_seqs) == 7)
+    printf("%.9g\n", 1e3 * workers_turnaround_ms(us * 1e-3, workers, chunk, (uint64_t)a.heads * prompt_slots(a), prompt_pause_share(a, every)));
+  return 0;
+}
+""")
+    exe = src.with_suffix("")
+    csrc = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2410_07381_amd", "csrc")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-I", csrc, str(src), "-o", str(exe)], check=True, timeout=60)
+    return lambda *c: float(subprocess.run([str(exe)], input=" ".join(map(str, c)), capture_output=True, text=True, check=True).stdout)
+
+
+def _tiles(lens):
+    """Tiles of the blocks of one head."""
+    return [-(-min(r + 128, n) // 64) for n in lens for r in range(0, n, 128)]
+
+
+@pytest.mark.parametrize("every", [1, 4, 16])
+@pytest.mark.parametrize("total", [1, 64, 128, 129, 1000, 4097, 32768])
+def test_prompt_turnaround_of_one_sequence_is_that_of_the_tiles_between_two_looks(estimate, total, every):
+    """A worker hands over `every` + 1 tiles after the request, or at its block's end; a tile's time is the kernel's over
+    the tiles that each worker has."""
+    heads, workers = 8, 256
+    tiles = _tiles([total])
+    tile_us = 1000.0 * workers / (heads * sum(tiles))
+    slots = total // 128 + 1
+    want = min(every + 1, sum(tiles) / slots) * tile_us
+    assert estimate(1000.0, workers, 1, every, heads, total, 1) == pytest.approx(want, rel=1e-6)
+    chunk = 16 if want == sum(tiles) / slots * tile_us else 1   # (that stop between blocks alone: all of a fetch)
+    assert estimate(1000.0, workers, 16, every, heads, total, 1) == pytest.approx(chunk * want, rel=1e-6)
+
+
+@pytest.mark.parametrize("lens", [[int(4096 ** (i / 23) + 0.5) for i in range(24)], [256] * 64, [3000, 1], [8192] * 4])
+def test_prompt_turnaround_of_several_sequences_is_not_that_of_one_of_all_tokens(estimate, lens):
+    """Which blocks pause at all depends on lengths that the host does not know: the estimate is Eq. 1's, no shorter than
+    the time of an average slot, whatever the number of blocks a fetch brings."""
+    heads, workers, every = 32, 512, 4
+    tiles = _tiles(lens)
+    tile_us = 1000.0 * workers / (heads * sum(tiles))
+    slots = sum(lens) // 128 + len(lens)
+    for chunk in (1, 4):
+        got = estimate(1000.0, workers, chunk, every, heads, sum(lens), len(lens))
+        assert got == pytest.approx(chunk * sum(tiles) / slots * tile_us, rel=1e-6)
