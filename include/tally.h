@@ -433,7 +433,9 @@ int tally_select_config(const tally_config *cands, uint32_t n, double threshold_
 /* Measure every candidate configuration of a kernel on the best-effort stream (`runs`
  * timed executions each, after one warm-up; the kernel really runs, so its outputs are
  * written `runs`+1 times per candidate), fill latency and turnaround, choose under
- * threshold_ms and cache the choice per (kernel, grid, block).  cands: in/out array.
+ * threshold_ms and cache the choice per (kernel, grid, block), for prompts and 4-bit products also
+ * per sizes (m, n, k, group and whether there are zero points; total, n_seqs, heads, kv_heads, dim): their grids
+ * are the same for very different work.  cands: in/out array.
  * Turnaround of a persistent-worker candidate is Eq. 1; for a kernel whose workers pause
  * inside their blocks while preempted (and with the pause enabled, see
  * tally_set_yield_bound_us) it is the time of ONE block times the share of a block
@@ -443,7 +445,7 @@ int tally_select_config(const tally_config *cands, uint32_t n, double threshold_
  * the kernel's. */
 int tally_profile(tally_ctx *ctx, const tally_kernel_desc *desc, tally_config *cands, uint32_t n,
                   uint32_t runs, double threshold_ms, uint32_t *chosen);
-/* lookup_launch_config() of Figure 4: the fixed choice for (kernel, grid, block);
+/* lookup_launch_config() of Figure 4: the fixed choice for (kernel, grid, block) as above;
  * TALLY_ERR_BAD_STATE while none is fixed. */
 int tally_lookup_config(tally_ctx *ctx, const tally_kernel_desc *desc, tally_config *out);
 

@@ -7,6 +7,7 @@
 #include <stdint.h>
 #include <string.h>
 
+#include <array>
 #include <atomic>
 #include <chrono>
 #include <condition_variable>
@@ -61,6 +62,8 @@ static_assert(kMaxShared + kRingCount == kMaxNative && (uint32_t)GemmCover::kRin
   static_assert(GemmRingT<ra, rb, r>::MIN_WAVES == ring_per_cu(ra, rb, r), "as many as the launch bounds say");
 GEMM_RINGS(GEMM_RING_CHECK)
 
+typedef std::array<uint32_t, 5> CallSizes;
+
 struct KernelOps {
   const char *name;
   size_t args_size;
@@ -94,6 +97,8 @@ struct KernelOps {
   bool together;
   // the original form's kernel depends on what else is on the GPU
   bool chooses;
+  // what a block's time depends on and the grid does not say (null: nothing that keeps measurements apart)
+  CallSizes (*sizes)(const void *args);
 };
 
 template <class Body>
@@ -614,6 +619,16 @@ uint32_t w4_range(const void *args) {
   return (a.group == 32 ? 0 : a.group == 64 ? 5 : 10) + (w4_staged(a) ? 4 : w4_rows(a.m, a.n) - 1);
 }
 uint32_t w4_choice(const void *args, uint32_t, uint64_t *) { return w4_range(args); }
+CallSizes w4_sizes(const void *args) {
+  tally_gemv_w4_args a;
+  memcpy(&a, args, sizeof(a));
+  return {a.m, a.n, a.k, a.group, a.zeros != nullptr};
+}
+CallSizes prompt_sizes(const void *args) {
+  tally_attn_prompt_args a;
+  memcpy(&a, args, sizeof(a));
+  return {a.total, a.n_seqs, a.heads, a.kv_heads, a.dim};
+}
 hipError_t launch_native_w4(hipStream_t s, const void *args, tally_dim3 g, uint32_t how) {
 #define W4_CASE(i, ...) case i: return launch_native_t<__VA_ARGS__>(s, args, g, how);
   switch (w4_range(args)) { W4_ALL(W4_CASE) }
@@ -734,12 +749,12 @@ struct TakesTogether<Body, std::enable_if_t<Body::TOGETHER>> : std::true_type {}
                        GEMM_WAVE_TILES(false) GEMM_RINGS(GEMM_RING_FOOT_F)},                                                           \
    gemm_native_choice<Body::TILE_N>, gemm_sliced_choice<slices>, GemmParts<Body>::parts, nullptr, nullptr, false, true}
 
-#define OPS_DIM(Wide, Narrow, nm, gridfn)                                                                 \
+#define OPS_DIM(Wide, Narrow, nm, gridfn, sizes)                                                          \
   {nm, sizeof(Wide::Args), true, gridfn, launch_native_dim_t<Wide, Narrow>,                               \
    launch_sliced_dim_t<Wide, Narrow>, launch_ptb_dim_t<Wide, Narrow>, init_dim_t<Wide, Narrow>,           \
    occupancy_t<Wide>, pause_fraction_t<Wide>, footprint_t<Wide>,                                          \
    {footprint_native_t<Wide>, footprint_native_t<Narrow>}, dim_choice<Wide, Narrow>, dim_range<Wide, Narrow>, \
-   nullptr, nullptr, nullptr, false, false}
+   nullptr, nullptr, nullptr, false, false, sizes}
 
 #define W4_FOOT(i, ...) footprint_native_t<__VA_ARGS__>,
 const KernelOps kOps[TALLY_K_COUNT] = {
@@ -762,7 +777,7 @@ const KernelOps kOps[TALLY_K_COUNT] = {
      gemm_sliced_choice<GemmCover::k32>, nullptr, block_bytes<GemmSmallBody>, GemmSmallBody::team_bytes,
      false, true},
     OPS_GEMM(GemmN128Body, "gemm_bf16_n128", grid_gemm_n128, GemmCover::k256x128),
-    OPS_DIM(PromptBody, PromptNarrowBody, "attn_prompt_bf16", grid_prompt),
+    OPS_DIM(PromptBody, PromptNarrowBody, "attn_prompt_bf16", grid_prompt, prompt_sizes),
     {"attn_prefix_bf16", sizeof(tally_attn_prefix_args), false, grid_prefix, launch_native_prefix,
      nullptr, nullptr, nullptr, nullptr, nullptr, nullptr,
      {footprint_prefix<128, 0>, footprint_prefix<128, 1>, footprint_prefix<128, 2>, footprint_prefix<64, 0>, footprint_prefix<64, 1>,
@@ -770,7 +785,7 @@ const KernelOps kOps[TALLY_K_COUNT] = {
      prefix_choice, nullptr, nullptr, nullptr, nullptr, false, false},
     {"gemv_w4_bf16", sizeof(tally_gemv_w4_args), true, grid_gemv_w4, launch_native_w4, launch_sliced_w4, launch_ptb_w4,
      nullptr, occupancy_w4, pause_fraction_t<GemvW4T<1, 1>>, footprint_w4, {W4_ALL(W4_FOOT)},
-     w4_choice, w4_range, nullptr, nullptr, nullptr, false, false},
+     w4_choice, w4_range, nullptr, nullptr, nullptr, false, false, w4_sizes},
 };
 
 constexpr size_t kMaxArgs = 128;
@@ -788,7 +803,7 @@ enum JobKind { KIND_PTB = 0, KIND_SLICED = 1, KIND_NATIVE = 2 };
 // One kernel's profiling record.  Measurements are sums over real executions of the kernel
 // (each invocation measures one candidate once); the configuration is fixed when every
 // candidate has `runs` samples.
-typedef std::tuple<uint32_t, uint32_t, uint32_t, uint32_t, uint32_t> ProfileKey;
+typedef std::tuple<uint32_t, uint32_t, uint32_t, uint32_t, uint32_t, CallSizes> ProfileKey;
 struct ProfileEntry {
   std::vector<tally_config> cands;
   std::vector<double> sum_ms;
@@ -858,7 +873,7 @@ struct tally_ctx {
   std::atomic<uint32_t> native_asked;  // of them, how many lie before the last marker of native_done()
   int device;
   int live_jobs;
-  // profile-guided configuration (Section 4.2): per (kernel, grid, block) the candidate
+  // profile-guided configuration (Section 4.2): per (kernel, grid, block; see CallSizes) the candidate
   // table with its measurements, and the choice once every candidate has been measured
   std::mutex profile_mu;
   std::map<ProfileKey, ProfileEntry> profiles;
@@ -1912,7 +1927,10 @@ int tally_select_config(const tally_config *c, uint32_t n, double threshold_ms) 
 namespace {
 
 ProfileKey profile_key(const tally_kernel_desc *d) {
-  return std::make_tuple(d->kernel_id, d->grid.x, d->grid.y, d->grid.z, d->block.x);
+  // (a question about a descriptor that no launch would take has no entry, and nothing of it is read)
+  const KernelOps *ops = d->kernel_id < TALLY_K_COUNT ? &kOps[d->kernel_id] : nullptr;
+  const bool read = ops && ops->sizes && d->args && d->args_size == ops->args_size;
+  return std::make_tuple(d->kernel_id, d->grid.x, d->grid.y, d->grid.z, d->block.x, read ? ops->sizes(d->args) : CallSizes{});
 }
 
 // Turnaround estimate of one measured candidate (Section 4.2).

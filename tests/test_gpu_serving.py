@@ -748,6 +748,34 @@ def test_two_calls_at_once_on_two_streams(env):
             assert all(torch.equal(a.view(torch.int16), b.view(torch.int16)) for a, b in zip(results, w))
 
 
+def test_measurements_of_calls_with_equal_grids_are_kept_apart(env):
+    """The grid of a 4-bit product has n alone, a prompt's only heads, tokens and sequences: the profiler's records
+    and choices are per sizes, and one call's are not another's."""
+    B, ctx, torch = env
+    z = lambda *s: torch.zeros(s, dtype=torch.int16, device="cuda")
+    def product(m, k, group, zeros):
+        W = torch.zeros((4, -(-k // 128), 64, 4), dtype=torch.int32, device="cuda")
+        zp = torch.zeros((4, -(-k // group), 16), dtype=torch.uint8, device="cuda") if zeros else None
+        return B.gemv_w4_bf16(z(m, k), W, z(4, -(-k // group), 16), z(m, 64), zeros=zp, group=group)
+    def prompt(total, heads, kv, dim, seqs):
+        cu = torch.tensor([total * i // seqs for i in range(seqs + 1)], dtype=torch.int32, device="cuda")
+        return B.attn_prompt_bf16(z(total, heads, dim), z(total, kv, dim), z(total, kv, dim), z(total, heads, dim), cu)
+    calls = [[product(*c) for c in ((1, 256, 64, False), (2, 256, 64, False), (1, 1024, 64, False), (1, 256, 32, False), (1, 256, 64, True))],
+             [prompt(*c) for c in ((300, 4, 4, 64, 2), (300, 4, 4, 128, 2), (300, 4, 2, 64, 2), (280, 4, 4, 64, 2), (200, 4, 4, 64, 3), (300, 2, 2, 64, 6))]]
+    ctx.profile_reset()
+    torch.cuda.synchronize()
+    for same in calls:
+        for i, kern in enumerate(same):
+            assert kern.desc.grid.x == same[0].desc.grid.x
+            for later in same[i:]:
+                assert ctx.profile_table(later) == ([], -1)
+                assert ctx.lookup_config(later) is None
+            ctx.profile(kern, [(B.CFG_PTB, 4, 1), (B.CFG_SLICED, 1 + i, 1)], runs=1)
+            assert all(len(ctx.profile_table(k)[0]) == 2 for k in same[:i + 1])
+        assert [ctx.profile_table(k)[0][1]["param"] for k in same] == [1 + i for i in range(len(same))]
+    ctx.profile_reset()
+
+
 def test_footprints_leave_room_for_a_paused_product(env):
     """The 4-bit products fit beside a paused 256 x 256 GEMM tile (their eight waves are compiled for 72 registers
     except with four rows of tiles), and what the prompt's workers occupy is known to the admission rules."""
