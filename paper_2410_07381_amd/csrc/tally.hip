@@ -1648,7 +1648,9 @@ int tally_kernel_footprint(tally_ctx *ctx, uint32_t kernel_id, int form, uint32_
     return TALLY_ERR_INVALID_ARG;
   if (form == 0 && !kOps[kernel_id].transformable) return TALLY_ERR_UNSUPPORTED;
   uint32_t most[3] = {0, 0, 0};
-  for (uint32_t f = 0; f < (form == 0 ? 1u : kMaxShared); ++f)
+  // (an operator that does not look at what else is there takes any of its kernels beside others)
+  const uint32_t kernels = form == 0 ? 1u : kOps[kernel_id].chooses ? kMaxShared : kMaxNative;
+  for (uint32_t f = 0; f < kernels; ++f)
     for (int i = 0; i < 3; ++i) {
       const uint32_t v = form == 0 ? ctx->foot_worker[kernel_id][i] : ctx->foot_native[kernel_id][f][i];
       if (v > most[i]) most[i] = v;
