@@ -624,6 +624,81 @@ def test_gemv_w4_rows_do_not_depend_on_the_number_of_vectors(env):
     assert all((o == outs[-1][:len(o)]).all() for o in outs)
 
 
+# m, n, rows of tiles of a workgroup, k, group, zeros: every kernel with more than one row, the last workgroup with all of
+# its rows and without one, two or three of them, its last row with all of its 16 rows of weights and without some
+W4_ROWS = [
+    (1, 16401, 2, 72, 32, True), (2, 16400, 2, 296, 64, False), (1, 16390, 2, 264, 128, True), (4, 4117, 2, 1160, 128, False),
+    (3, 4100, 2, 136, 64, True), (6, 4112, 2, 2200, 32, False),
+    (8, 8213, 3, 1288, 32, True), (16, 8230, 3, 200, 64, False), (10, 8208, 3, 296, 128, True), (7, 8240, 3, 1160, 256, False), (8, 16405, 3, 128, 64, True),
+    (16, 24600, 4, 72, 64, True), (13, 24580, 4, 264, 32, False), (16, 24624, 4, 1160, 128, True), (11, 24640, 4, 136, 384, False),
+]
+
+
+@pytest.mark.parametrize("m,n,rows,k,group,zeros", W4_ROWS)
+def test_gemv_w4_with_several_rows_of_tiles(env, m, n, rows, k, group, zeros):
+    """In every form; what stands for rows and columns that do not exist is garbage, and y's neighbours stay."""
+    B, ctx, torch = env
+    rng = np.random.default_rng(n + k)
+    x, codes, scales, z = _w4(rng, m, n, k, group, zeros)
+    junk = torch.from_numpy(rng.integers(0, 16, (-(-n // 16) * 16, -(-k // 128) * 128)))
+    junk[:n, :k] = torch.from_numpy(codes)
+    W, s = B.pack_w4(junk).cuda(), B.pack_w4_groups(torch.from_numpy(scales.view(np.int16)))
+    if n % 16:
+        s[-1, :, n % 16:] = 0x7FC0
+    zp = B.pack_w4_groups(torch.from_numpy(z)).cuda() if zeros else None
+    xd, s = _dev(torch, x), s.cuda()
+    want, mass = OS.gemv_w4(obf16.decode(x), codes, obf16.decode(scales), z, group)
+    bound = 2.0 ** -8 * np.abs(want) + (2 * k + 300) * 2.0 ** -24 * mass
+    outs = []
+    for form in ("hi", "be", "sliced", "ptb"):
+        y = torch.full((m + 1, n), SENTINEL, dtype=torch.int16, device="cuda")
+        kern = B.gemv_w4_bf16(xd, W, s, y[:m], zeros=zp, group=group)
+        assert kern.grid == (-(-n // (16 * rows)), 1, 1)
+        torch.cuda.synchronize()
+        _run(ctx, torch, kern, form)
+        outs.append(_host(y))
+        err = np.abs(obf16.decode(outs[-1][:m]) - want)
+        assert (err <= bound).all(), f"{form}: worst {(err / bound).max():.2f} bounds"
+        assert (outs[-1][m] == SENTINEL).all(), form
+    assert all((o == outs[0]).all() for o in outs)
+
+
+@pytest.mark.parametrize("group,zeros", [(32, True), (64, False), (128, True), (384, False)])
+@pytest.mark.parametrize("n,k,kernels", [(24596, 520, {(1, 2), (4, 2), (8, 3), (16, 4)}), (8210, 1000, {(1, 1), (3, 1), (4, 2), (10, 3)}),
+                                         (16410, 9000, {(1, 2), (4, 2), (16, 3)})])
+def test_gemv_w4_bits_do_not_depend_on_the_kernel(env, n, k, kernels, group, zeros):
+    """Every row's bits are the same with one to sixteen vectors, one to four rows of tiles, and (one vector, k = 9000, few
+    rows) with x in LDS."""
+    B, ctx, torch = env
+    g = torch.Generator(device="cuda").manual_seed(n)
+    tiles, groups = -(-n // 16), -(-k // group)
+    W = torch.randint(-(1 << 31), 1 << 31, (tiles, -(-k // 128), 64, 4), generator=g, device="cuda", dtype=torch.int64).to(torch.int32)
+    s = torch.rand((tiles, groups, 16), generator=g, device="cuda").to(torch.bfloat16)
+    zp = torch.randint(0, 17, (tiles, groups, 16), generator=g, device="cuda", dtype=torch.uint8) if zeros else None
+    x = torch.randn((16, k), generator=g, device="cuda").to(torch.bfloat16)
+    outs = []
+    for m, rows in sorted(kernels):
+        y = torch.zeros((m, n), dtype=torch.bfloat16, device="cuda")
+        kern = B.gemv_w4_bf16(x[:m], W, s, y, zeros=zp, group=group)
+        assert kern.grid[0] == -(-tiles // rows)
+        torch.cuda.synchronize()
+        ctx.launch_native(kern, hi=True)
+        outs.append(y)
+    for rows in (16, 100, 4096):                           # (one row of tiles each; with one vector of 9000, x is in LDS)
+        y = torch.zeros((1, rows), dtype=torch.bfloat16, device="cuda")
+        part = -(-rows // 16)
+        kern = B.gemv_w4_bf16(x[:1], W[:part], s[:part], y, zeros=zp[:part] if zeros else None, group=group)
+        assert kern.grid[0] == part
+        torch.cuda.synchronize()
+        ctx.launch_native(kern, hi=True)
+        outs.append(y)
+    torch.cuda.synchronize()
+    whole = outs[len(kernels) - 1].view(torch.int16)
+    assert whole.shape[0] >= 10 and torch.isfinite(outs[len(kernels) - 1].float()).all()
+    for o in outs:
+        assert torch.equal(o.view(torch.int16), whole[:o.shape[0], :o.shape[1]]), o.shape
+
+
 # ---------------------------------------------------------------- as a program uses them
 def _decode_step(B, torch, g, batch, heads, kv, dim, prefix_kv, cap):
     """A batch's decode step behind a prefix: attention, then two 4-bit products of its output."""
