@@ -35,12 +35,9 @@ namespace tally {
 
 constexpr uint32_t kW4Rows = 16, kW4Block = 128, kW4Vectors = 16, kW4MaxGroup = 1u << 20;
 constexpr int kW4Waves = 8;
-constexpr uint32_t kW4Staged = 22 * 1024;                  // bytes of LDS for the vectors, where they go there
+constexpr uint32_t kW4Staged = 22 * 1024;                  // bytes of LDS for x, where it goes there
 constexpr uint32_t kW4LongK = 8192;                        // ... from this k on
-constexpr uint32_t kW4Piece = 1024;                        // bytes of a vector that one direct load brings
-
-// bytes from a vector to the next in LDS: whole pieces, and a step that spreads them over the banks (not behind the last)
-__host__ __device__ constexpr uint32_t w4_pitch(uint32_t k) { return (k * 2 + kW4Piece - 1) / kW4Piece * kW4Piece + 64; }
+constexpr uint32_t kW4Piece = 1024;                        // bytes of x that one direct load brings
 
 // Rows of tiles that a workgroup takes.  It reads x once for all of them (from the L2s, 24 bytes a clock and compute
 // unit where all of them read the same): with many vectors that is more than the codes, so fewer workgroups
@@ -62,11 +59,12 @@ inline uint32_t w4_rows(uint32_t m, uint32_t n) {
   }
   return best;
 }
-// x goes to LDS where it fits and a wave has many tiles to take one after the other, so that nothing but codes is
-// on its way in the loop.  (us, straight from the L2s / so, 1 vector: 4096 x 11008, groups of
+// One vector goes to LDS where it fits (two from kW4LongK on do not) and a wave has many tiles to take one after the
+// other, so that nothing but codes is on its way in the loop.  (us, straight from the L2s / so: 4096 x 11008, groups of
 // 64 with zero points, 9.1 / 8.3; 11008 x 11008 13.9 / 12.8; 1024 x 11008, groups of 32, 8.4 / 7.6; but 11008 x 1024 3.4 / 3.8.)
+static_assert(2 * kW4LongK * 2 > kW4Staged, "room for one vector alone");
 inline bool w4_staged(const tally_gemv_w4_args &a) {
-  return a.k >= kW4LongK && (uint64_t)a.m * w4_pitch(a.k) - 64 <= kW4Staged && w4_rows(a.m, a.n) == 1;
+  return a.m == 1 && a.k >= kW4LongK && a.k * 2 <= kW4Staged && w4_rows(a.m, a.n) == 1;
 }
 
 // One tile of 16 rows by 128 weights, as loaded.  SUB: MFMAs of a tile that share a scale (groups of 32, of
@@ -160,7 +158,7 @@ struct W4Base {
   }
 };
 
-// x in LDS, straight from memory; behind its loads each wave keeps two tiles of codes on their way.
+// One vector in LDS, straight from memory; behind its loads each wave keeps two tiles of codes on their way.
 template <int SUB>
 struct GemvW4StagedT : W4Base<1> {
   static constexpr int MIN_WAVES = 7;                      // 72 registers: two waves fit beside a paused GEMM tile
@@ -175,15 +173,13 @@ struct GemvW4StagedT : W4Base<1> {
     asm volatile("" : "+v"(lane));
     const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t blocks = (a.k + kW4Block - 1) / kW4Block, groups = (a.k + a.group - 1) / a.group;
-    const uint32_t LDX = a.ld_x ? a.ld_x : a.k, pitch = w4_pitch(a.k), pieces = (a.k * 2 + kW4Piece - 1) / kW4Piece;
     const uint32_t lds = (uint32_t)(uintptr_t)(lptr_t)tally_dyn_lds;
-    for (uint32_t i = wave; i < a.m * pieces; i += kW4Waves) {
-      const uint32_t v = i / pieces, c = i % pieces;
-      const uint64_t p = (uint64_t)(uintptr_t)(a.x + (uint64_t)v * LDX);
-      const u32x4_t b = {(uint32_t)p, (uint32_t)(p >> 32) & 0xFFFFu, a.k * 2, 0x00027000u};
+    const uint64_t p = (uint64_t)(uintptr_t)a.x;
+    const u32x4_t x = {(uint32_t)p, (uint32_t)(p >> 32) & 0xFFFFu, a.k * 2, 0x00027000u};
+    for (uint32_t at = wave * kW4Piece; at < a.k * 2; at += kW4Waves * kW4Piece) {
       // (as in OnePass::ask, the waits too: what is past the vector's end is left as zeros)
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-                   ::"s"(lds + v * pitch + c * kW4Piece), "v"(lane * 16 + c * kW4Piece), "s"(b) : "memory");
+                   ::"s"(lds + at), "v"(lane * 16 + at), "s"(x) : "memory");
     }
     const typename W4Tile<SUB>::From from(a, tile, blocks, groups);
     W4Tile<SUB> t[DEEP];
@@ -191,7 +187,7 @@ struct GemvW4StagedT : W4Base<1> {
     for (int j = 0; j < DEEP; ++j) t[j].load(from, wave + j * kW4Waves, lane);
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * DEEP) : "memory");   // (at least so many loads are behind those of x)
     __syncthreads();
-    const uint32_t col = lane & 15, at = lds + (col < a.m ? col : 0u) * pitch + (lane >> 4) * 16;
+    const uint32_t at = lds + (lane >> 4) * 16;            // (the same for all 16 rows of an MFMA, of which one counts)
     f32x4_t acc[1] = {{0.f, 0.f, 0.f, 0.f}};
     for (uint32_t b = wave; b < blocks; b += DEEP * kW4Waves) {
 #pragma unroll
