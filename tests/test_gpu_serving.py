@@ -142,6 +142,31 @@ def test_prompt_scale_and_large_scores(env, scale):
     _attn_ok(_host(out), want, mass)
 
 
+@pytest.mark.parametrize("dim,scale,reach", [(64, 1.5, 3.0), (128, 0.8, 6.0), (64, 20.0, 3.0)])
+def test_prompt_scores_of_hundreds_and_thousands(env, dim, scale, reach):
+    """A maximum that keeps rising over scores of magnitude S, up to some thousands.  A score's products and sums are off by
+    (dim + 2) S 2^-24, p by as much of itself, and so are numerator and denominator, each by that much of M."""
+    B, ctx, torch = env
+    total = 520
+    rng = np.random.default_rng(dim)
+    ramp = np.linspace(0.05, reach, total)[:, None, None]
+    q, v = _bits(rng, (total, 4, dim)), _bits(rng, (total, 2, dim))
+    k = TI.to_bf16_bits((rng.standard_normal((total, 2, dim)) * ramp).astype(np.float32))
+    out = torch.zeros((total, 4, dim), dtype=torch.int16, device="cuda")
+    cu = torch.tensor([0, 200, total], dtype=torch.int32, device="cuda")
+    kern = B.attn_prompt_bf16(_dev(torch, q), _dev(torch, k), _dev(torch, v), out, cu, scale=scale)
+    torch.cuda.synchronize()
+    _run(ctx, torch, kern, "hi")
+    qd, kd = obf16.decode(q), obf16.decode(k)
+    want, mass = OS.attn_prompt(qd, kd, obf16.decode(v), [0, 200, total], scale)
+    S = scale * np.abs(qd).sum(-1).max() * np.abs(kd).max()   # (at least sum |q k| of any pair)
+    S = min(S, scale * np.sqrt((qd ** 2).sum(-1).max() * (kd ** 2).sum(-1).max()))
+    bound = 2.0 ** -8 * np.abs(want) + (2.0 ** -8 + 2.0 ** -12 + 2 * (dim + 2) * S * 2.0 ** -24) * mass
+    assert S > 100
+    err = np.abs(obf16.decode(_host(out)) - want)
+    assert (err <= bound).all(), (err / bound).max()
+
+
 def test_prompt_strided_views_of_one_buffer(env):
     """q, k and v of a fused projection's padded output, out a view with padding of its own."""
     B, ctx, torch = env
@@ -281,6 +306,94 @@ def test_prompt_workers_pause_inside_a_block_and_go_on(env):
     job.free()
     torch.cuda.synchronize()
     assert torch.equal(a.view(torch.int16), b.view(torch.int16))
+
+
+@pytest.mark.parametrize("dim,every,chunk", [(128, 4, 1), (64, 1, 1), (128, 16, 4), (64, 64, 2)])
+def test_prompt_workers_that_are_asked_to_pause_wait_inside_their_blocks(env, dim, every, chunk):
+    """A request that is held for 4 ms, several times a block's time and more than the whole kernel's, keeps the workers where
+    they are (they would have left otherwise); withdrawn, they finish their blocks and leave, and go on when resumed.  The bits
+    are those of the original form, with every block executed once."""
+    import time
+    B, ctx, torch = env
+    total = 16384
+    g = torch.Generator(device="cuda").manual_seed(dim + every)
+    q, k, v = (torch.randn((total, 16, dim), generator=g, device="cuda").to(torch.bfloat16) for _ in range(3))
+    cu = torch.tensor([0, total], dtype=torch.int32, device="cuda")
+    want, out = torch.zeros_like(q), torch.zeros_like(q)
+    torch.cuda.synchronize()
+    ctx.launch_native(B.attn_prompt_bf16(q, k, v, want, cu))
+    torch.cuda.synchronize()
+    kern = B.attn_prompt_bf16(q, k, v, out, cu)
+    ctx.set_yield_bound_us(100000)
+    ctx.set_yield_every(every)
+    try:
+        spans = []
+        for pauses in (0, 0, 2):
+            out.zero_()
+            torch.cuda.synchronize()
+            t0 = time.perf_counter()
+            job = ctx.launch_ptb(kern, 256, chunk=chunk, coverage=True)
+            stops = 0
+            for _ in range(pauses):
+                while time.perf_counter() < t0 + 0.2 * spans[-1]:
+                    pass
+                job.preempt(pause=True)
+                time.sleep(0.004)
+                job.pump()
+                assert job.progress()[2] == B.JOB_RUNNING
+                job.end_pause()
+                if job.wait() == B.JOB_STOPPED:
+                    stops += 1
+                    t0 = time.perf_counter()
+                    job.resume()
+            assert job.wait() == B.JOB_COMPLETE
+            if pauses:
+                assert stops >= 1
+            else:
+                spans.append(time.perf_counter() - t0)
+            assert (job.coverage()["count"] == 1).all()
+            job.free()
+            torch.cuda.synchronize()
+            assert torch.equal(out.view(torch.int16), want.view(torch.int16))
+        assert 0.0003 < spans[-1] < 0.003                  # (otherwise the pauses prove nothing)
+    finally:
+        ctx.set_yield_bound_us(1000)
+        ctx.set_yield_every(4)
+
+
+def test_prompt_blocks_too_short_to_pause_inside_pause_before_the_next_of_their_fetch(env):
+    """Blocks of two and four tiles with looks 16 tiles apart: of the 64 blocks of a fetch the next one waits."""
+    import time
+    B, ctx, torch = env
+    seqs, total = 800, 160000
+    g = torch.Generator(device="cuda").manual_seed(5)
+    q, k, v = (torch.randn((total, 2, 64), generator=g, device="cuda").to(torch.bfloat16) for _ in range(3))
+    cu = torch.arange(seqs + 1, dtype=torch.int32, device="cuda") * 200
+    want, out = torch.zeros_like(q), torch.zeros_like(q)
+    torch.cuda.synchronize()
+    ctx.launch_native(B.attn_prompt_bf16(q, k, v, want, cu))
+    torch.cuda.synchronize()
+    kern = B.attn_prompt_bf16(q, k, v, out, cu)
+    ctx.set_yield_bound_us(100000)
+    ctx.set_yield_every(16)
+    try:
+        job = ctx.launch_ptb(kern, 2, chunk=64, coverage=True)
+        time.sleep(0.0005)
+        job.preempt(pause=True)
+        time.sleep(0.01)
+        job.pump()
+        assert job.progress()[2] == B.JOB_RUNNING
+        job.end_pause()
+        assert job.wait() == B.JOB_STOPPED and 0 < job.progress()[0] < kern.total_blocks
+        job.resume()
+        assert job.wait() == B.JOB_COMPLETE
+        assert (job.coverage()["count"] == 1).all()
+        job.free()
+    finally:
+        ctx.set_yield_bound_us(1000)
+        ctx.set_yield_every(4)
+    torch.cuda.synchronize()
+    assert torch.equal(out.view(torch.int16), want.view(torch.int16))
 
 
 # ---------------------------------------------------------------- behind a shared prefix

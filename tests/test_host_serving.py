@@ -216,3 +216,27 @@ def test_prompt_turnaround_of_several_sequences_is_not_that_of_one_of_all_tokens
     for chunk in (1, 4):
         got = estimate(1000.0, workers, chunk, every, heads, sum(lens), len(lens))
         assert got == pytest.approx(chunk * sum(tiles) / slots * tile_us, rel=1e-6)
+
+
+def test_registers_leave_the_room_that_the_kernels_count_on(B, tmp_path):
+    """From the library's own notes, kernel by kernel: 4-bit products of one to three rows of tiles have 72 registers at most in
+    every form (two of their eight waves fit beside a paused 256 x 256 tile's), those of four 96; attention behind a prefix in
+    parts of 16 and 64 rows 128; prompts 256."""
+    import re
+    from test_host_logic import _device_code
+    notes = _device_code(B, tmp_path)("llvm-readelf", "--notes")
+    found = {}
+    for kernel in notes.split("- .agpr_count:")[1:]:
+        name, regs = re.search(r"\.name:\s+(_Z\S+)", kernel), re.search(r"\.vgpr_count:\s+(\d+)", kernel)
+        found[name.group(1)] = int(regs.group(1)) + int(kernel.split()[0])
+    w4 = {(m.group(1), int(m.group(2)), int(m.group(3))): r for n, r in found.items()
+          if (m := re.search(r"(native|sliced|ptb)_kernelINS_7GemvW4TILi(\d)ELi(\d)E", n))}
+    assert len(w4) == 36
+    assert all(r <= (96 if rows == 4 else 72) for (_, _, rows), r in w4.items()), w4
+    staged = {n: r for n, r in found.items() if "GemvW4StagedT" in n}
+    assert len(staged) == 9 and max(staged.values()) <= 72
+    behind = {(int(m.group(1)), int(m.group(2))): r for n, r in found.items()
+              if (m := re.search(r"attn_prefix_partialILi(\d+)ELi(\d)E", n))}
+    assert len(behind) == 6 and all(r <= (256 if kind == 2 else 128) for (_, kind), r in behind.items()), behind
+    prompts = {n: r for n, r in found.items() if "PromptBodyT" in n}
+    assert len(prompts) == 6 and max(prompts.values()) <= 256
