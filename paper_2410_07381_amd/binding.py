@@ -377,6 +377,17 @@ def _rows(t, dim=None):
     return row
 
 
+def _is_bf16(*tensors):
+    """bf16, or any 16 bits that hold one; fp16, which would be taken for one, is none."""
+    import torch
+    return all(t.element_size() == 2 and t.dtype != torch.float16 for t in tensors)
+
+
+def _is_int32(t):
+    import torch
+    return t.dtype == torch.int32 and t.dim() == 1 and t.is_contiguous()
+
+
 def attn_prompt_bf16(q, k, v, out, cu_seqlens, scale=None):
     """Causal attention over prompts packed one behind the other: q, out [total, heads, dim]; k, v
     [total, kv_heads, dim]; 16-bit storage tensors that may be views with padded tokens (one
@@ -385,8 +396,8 @@ def attn_prompt_bf16(q, k, v, out, cu_seqlens, scale=None):
     total, heads, dim = q.shape
     kv_heads = k.shape[1]
     assert out.shape == q.shape and k.shape == v.shape == (total, kv_heads, dim)
-    assert all(t.element_size() == 2 for t in (q, k, v, out))
-    assert cu_seqlens.dim() == 1 and cu_seqlens.element_size() == 4 and cu_seqlens.is_contiguous() and cu_seqlens.numel() >= 2
+    assert _is_bf16(q, k, v, out)
+    assert _is_int32(cu_seqlens) and cu_seqlens.numel() >= 2
     args = AttnPromptArgs(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), cu_seqlens.data_ptr(),
                           total, cu_seqlens.numel() - 1, heads, kv_heads, dim,
                           _rows(q, dim), _rows(k, dim), _rows(v, dim), _rows(out, dim), _scale(scale))
@@ -405,15 +416,15 @@ def attn_prefix_bf16(q, K, V, Ko, Vo, own_len, out, scratch, scale=None):
     if held(K, 0):
         prefix, ld_prefix = K.shape[0], _rows(K, dim)
         assert V.shape == K.shape == (prefix, kv_heads, dim) and _rows(V, dim) == ld_prefix
-        assert K.element_size() == V.element_size() == 2
+        assert _is_bf16(K, V)
     if held(Ko, 1):
         own_cap, ld_own = Ko.shape[1], _rows(Ko, dim)
         assert Vo.shape == Ko.shape == (batch, own_cap, kv_heads, dim) and _rows(Vo, dim) == ld_own
-        assert Ko.element_size() == Vo.element_size() == 2
-        assert own_len.shape == (batch,) and own_len.element_size() == 4 and own_len.is_contiguous()
+        assert _is_bf16(Ko, Vo)
+        assert _is_int32(own_len) and own_len.numel() == batch
         stride = Ko.stride(0) if batch > 1 else 0
         assert batch == 1 or (stride == Vo.stride(0) and stride > 0)
-    assert out.shape == q.shape and q.element_size() == out.element_size() == 2
+    assert out.shape == q.shape and _is_bf16(q, out)
     assert scratch.is_contiguous() and (scratch.numel() * scratch.element_size() >=
                                         attn_prefix_scratch_bytes(batch, heads, kv_heads, dim, prefix, own_cap))
     ptr = lambda t, n: t.data_ptr() if n else None
@@ -440,8 +451,9 @@ def gemv_w4_bf16(x, W, scales, y, zeros=None, group=128):
     """y = x (codes - zeros)^T with a scale per row and group: x [m, k], y [m, n], m <= 16, 16-bit storage
     tensors whose rows may be padded; W, scales and zeros as pack_w4() and pack_w4_groups() lay them out."""
     (m, k), n = x.shape, y.shape[1]
+    assert group > 0
     tiles, blocks, groups = -(-n // 16), -(-k // 128), -(-k // group)
-    assert y.shape[0] == m and x.element_size() == y.element_size() == scales.element_size() == 2
+    assert y.shape[0] == m and _is_bf16(x, y, scales)
     assert W.shape == (tiles, blocks, 64, 4) and W.element_size() == 4 and W.is_contiguous()
     assert scales.shape == (tiles, groups, 16) and scales.is_contiguous()
     assert zeros is None or (zeros.shape == scales.shape and zeros.element_size() == 1 and zeros.is_contiguous())
@@ -455,6 +467,8 @@ def pack_w4(codes):
     [ceil(n / 16), ceil(k / 128), 64, 4] of 16 rows by 128 columns, filled up with zeros."""
     import torch
     n, k = codes.shape
+    # (a code of more bits would change its neighbours)
+    assert not codes.is_floating_point() and (codes.numel() == 0 or (int(codes.min()) >= 0 and int(codes.max()) <= 15))
     tiles, blocks = -(-n // 16), -(-k // 128)
     full = torch.zeros((tiles * 16, blocks * 128), dtype=torch.int64, device=codes.device)
     full[:n, :k] = codes
@@ -465,9 +479,10 @@ def pack_w4(codes):
 
 
 def pack_w4_groups(t):
-    """Scales or zero points [n, groups] as gemv_w4_bf16 reads them: [ceil(n / 16), groups, 16]."""
+    """Scales or zero points (bytes 0 .. 128) [n, groups] as gemv_w4_bf16 reads them: [ceil(n / 16), groups, 16]."""
     import torch
     n, groups = t.shape
+    assert t.element_size() != 1 or t.numel() == 0 or (int(t.min()) >= 0 and int(t.max()) <= 128)
     full = torch.zeros((-(-n // 16) * 16, groups), dtype=t.dtype, device=t.device)
     full[:n] = t
     return full.view(-1, 16, groups).transpose(1, 2).contiguous()

@@ -240,3 +240,32 @@ def test_registers_leave_the_room_that_the_kernels_count_on(B, tmp_path):
     assert len(behind) == 6 and all(r <= (256 if kind == 2 else 128) for (_, kind), r in behind.items()), behind
     prompts = {n: r for n, r in found.items() if "PromptBodyT" in n}
     assert len(prompts) == 6 and max(prompts.values()) <= 256
+
+
+def test_the_binding_refuses_types_that_would_be_taken_for_others(B):
+    """fp16 for bf16, floats or 64 bits for lengths, codes of more than four bits, zero points above 128, groups of none."""
+    import torch
+    z = lambda *s, dtype=torch.bfloat16: torch.zeros(s, dtype=dtype)
+    half = lambda t: t.to(torch.float16)
+    cu, q, lens = torch.tensor([0, 5], dtype=torch.int32), z(5, 2, 64), torch.zeros(3, dtype=torch.int32)
+    q3, own = z(3, 2, 64), z(3, 7, 2, 64)
+    room = torch.zeros(B.attn_prefix_scratch_bytes(3, 2, 2, 64, 5, 7), dtype=torch.uint8)
+    x, y, W, s = z(2, 256), z(2, 20), B.pack_w4(torch.zeros(20, 256, dtype=torch.uint8)), z(2, 2, 16)
+    calls = [(B.attn_prompt_bf16, (q, q, q, z(5, 2, 64), cu), range(4), 4), (B.attn_prefix_bf16, (q3, q, q, own, own, lens, z(3, 2, 64), room), (0, 1, 2, 3, 4, 6), 5),
+             (B.gemv_w4_bf16, (x, W, s, y), (0, 2, 3), None)]
+    for call, args, values, lengths in calls:
+        call(*args)
+        call(*(a.view(torch.int16) if i in values else a for i, a in enumerate(args)))
+        bad = [(i, half(args[i])) for i in values] + ([(lengths, args[lengths].float()), (lengths, args[lengths].long())] if lengths else [])
+        for i, other in bad:
+            with pytest.raises(AssertionError):
+                call(*args[:i], other, *args[i + 1:])
+    with pytest.raises(AssertionError):
+        B.gemv_w4_bf16(x, W, s, y, group=0)
+    for codes in (torch.tensor([[16] * 8]), torch.tensor([[-1] * 8]), torch.ones(1, 8)):
+        with pytest.raises(AssertionError):
+            B.pack_w4(codes)
+    assert B.pack_w4(torch.full((1, 8), 15)).shape == (1, 1, 64, 4)
+    assert B.pack_w4_groups(torch.full((3, 2), 128, dtype=torch.uint8)).max() == 128
+    with pytest.raises(AssertionError):
+        B.pack_w4_groups(torch.full((3, 2), 129, dtype=torch.uint8))
