@@ -133,6 +133,10 @@ typedef struct {
  * infinities included).  The values of cu_seqlens are read by the kernel: entries outside [0, total] count
  * as its ends, a sequence whose end lies before its start as empty; nothing outside the
  * tensors is touched.
+ * Arithmetic: scores, maxima and sums in fp32; each p_ij is rounded to bf16 before it multiplies v, and the sum is of
+ * the rounded ones; the output is rounded once more.  Together at most 2^-8 of sum p |v| / sum p and 2^-8 of the output,
+ * beside fp32's own.  What a row sees may be as large as scores (scale q . k) of 2^24 and v of 2^96; an output
+ * that a NaN or infinity reaches in the formula is one or the other.
  * Logical grid: heads x (total / 128 + n_seqs) blocks in one dimension, below 2^24; block heads x b + p owns up
  * to 128 rows of one head (p, or with a multiple of eight heads p % 8 x heads / 8 + p / 8) of one sequence s, which
  * has the slots b from cu_seqlens[s] / 128 + s on that its rows fill, last rows first. */
@@ -154,7 +158,8 @@ typedef struct {
  * are then not looked at; own_len neither without own_cap).  own_len: batch int32 in DEVICE memory; values
  * outside [0, own_cap] count as its ends.  What lies in the caches behind own_len is not read.
  * ld_*: elements between sequences (q, out) or tokens (prefix, own), multiples of 8, at most 2^20, 0: dense;
- * stride_own: elements between the sequences' caches, a multiple of 8, 0: dense.  scale as above.
+ * stride_own: elements between the sequences' caches, a multiple of 8, 0: dense.  scale and arithmetic as
+ * above (TALLY_K_ATTN_DECODE_BF16 keeps p in fp32).
  * scratch: caller-owned device memory of tally_attn_prefix_scratch_bytes() bytes, 16-byte aligned; two calls
  * that may overlap need one each.  batch * heads at most 2^20, prefix and own_cap at most 2^28. */
 typedef struct {
@@ -169,14 +174,15 @@ typedef struct {
 /* y[v][r] = sum_k x[v][k] (code[r][k] - zero[r][k / group]) scale[r][k / group], v < m <= 16, r < n.
  * x: m x k, y: m x n, scales: bf16; codes 0 .. 15; zeros: bytes 0 .. 128, or NULL for 8 everywhere.
  * n at most 2^26, k a multiple of 8 and at most 2^24; group 32, 64 or a multiple of 128 up to 2^20; the last group
- * may be short.  x finite
- * (an infinity gives NaN).  Sums are held in fp32 and rounded once.
+ * may be short.  x below 2^112 in magnitude (an infinity gives NaN).  Sums are held in fp32 and rounded once; the codes
+ * enter them as 128 + code, and -(128 + zero) takes that out again, so fp32's rounding is of terms up to
+ * (256 + code + zero) |x| scale.
  * Layout of the weights, with N = ceil(n / 16), B = ceil(k / 128), G = ceil(k / group):
  *   W: N x B tiles of 64 x 4 words; word i of entry 16 q + r of tile (t, b) holds the codes of row 16 t + r,
  *      columns c = 128 b + 32 i + 8 q up to c + 7: c + 2 j in bits 4 j and c + 2 j + 1 in bits 16 + 4 j;
  *   scales, zeros: N x G x 16, entry (t, g, r) for row 16 t + r.
- * What stands for rows and columns that do not exist does not matter.  x and W 16-byte aligned, ld_x (elements
- * between vectors, a multiple of 8) and ld_y 0: dense, at most 2^24.
+ * What stands for rows and columns that do not exist does not matter.  x and W 16-byte aligned; ld_x and ld_y: elements
+ * between vectors, 0: dense, ld_x a multiple of 8 and at most 2^24.
  * Logical grid: blocks of 16, 32, 48 or 64 rows, by m and n (tally_logical_grid). */
 typedef struct {
   const uint16_t *x; const uint32_t *W; const uint16_t *scales; const uint8_t *zeros; uint16_t *y;

@@ -649,6 +649,37 @@ def test_prefix_with_an_odd_number_of_partial_results(env, batch, heads, kv, dim
     assert (room[n:] == 0x7F).all()
 
 
+@pytest.mark.parametrize("dim", [64, 128])
+def test_attention_takes_scores_of_2_24_and_values_of_2_96(env, dim):
+    """Scores of 2^17, 2 x 2^17 ... 2^24, each the largest so far: its token's weight is one, all others' zero, and the output
+    is its V, to the bit (a product with p and a division by the same p, off by 2^-23 in all before the last rounding)."""
+    B, ctx, torch = env
+    n = 128
+    rng = np.random.default_rng(dim)
+    k = np.zeros((n, 1, dim), np.float32)
+    k[:, 0, 5] = (1 + np.arange(n)) * 2.0 ** 17            # (8 bits each)
+    q = np.zeros((n, 2, dim), np.float32)
+    q[:, :, 5] = 1.0
+    v = TI.to_bf16_bits((np.sign(rng.standard_normal((n, 1, dim))) * 2.0 ** rng.uniform(90, 96, (n, 1, dim))).astype(np.float32))
+    q, k = TI.to_bf16_bits(q), TI.to_bf16_bits(k)
+    out = torch.zeros((n, 2, dim), dtype=torch.int16, device="cuda")
+    qd, kd, vd = (_dev(torch, t) for t in (q, k, v))
+    prompt = B.attn_prompt_bf16(qd, kd, vd, out, torch.tensor([0, n], dtype=torch.int32, device="cuda"), scale=1.0)
+    torch.cuda.synchronize()
+    _run(ctx, torch, prompt, "hi")
+    assert (_host(out) == v).all()
+    for prefix, cap in ((n, 0), (0, n), (50, n - 50)):
+        lens = torch.tensor([cap, 0][:2 if prefix else 1], dtype=torch.int32, device="cuda")
+        batch = lens.numel()
+        one = torch.zeros((batch, 2, dim), dtype=torch.int16, device="cuda")
+        own = [t[prefix:].unsqueeze(0).repeat(batch, 1, 1, 1) for t in (kd, vd)]
+        step = B.attn_prefix_bf16(qd[:batch], kd[:prefix], vd[:prefix], *own, lens, one, _scratch(B, torch, batch, 2, 1, dim, prefix, cap), scale=1.0)
+        torch.cuda.synchronize()
+        _run(ctx, torch, step, "hi")
+        got = _host(one)
+        assert (got[0] == v[-1]).all() and (batch == 1 or (got[1] == v[prefix - 1]).all())
+
+
 def test_prefix_is_not_transformable(env):
     B, ctx, torch = env
     z = torch.zeros((1, 1, 64), dtype=torch.int16, device="cuda")
@@ -720,6 +751,22 @@ def test_gemv_w4_strides_and_neighbours(env):
     _w4_ok(got[1:1 + m, 2:2 + n], x, codes, scales, z, group)
     assert (got[0] == SENTINEL).all() and (got[1 + m:] == SENTINEL).all()
     assert (got[1:1 + m, :2] == SENTINEL).all() and (got[1:1 + m, 2 + n:] == SENTINEL).all()
+
+
+@pytest.mark.parametrize("m,k,group", [(1, 8200, 128), (3, 520, 32), (16, 1000, 64), (5, 640, 256)])
+def test_gemv_w4_takes_vectors_of_2_112(env, m, k, group):
+    """x as large as the header allows, scales as small: nothing overflows on the way."""
+    B, ctx, torch = env
+    n = 50
+    x, codes, scales, z = _w4(np.random.default_rng(k), m, n, k, group, True)
+    x = TI.to_bf16_bits((np.clip(obf16.decode(x), -3.9, 3.9) * 2.0 ** 110).astype(np.float32))
+    scales = TI.to_bf16_bits((obf16.decode(scales) * 2.0 ** -112).astype(np.float32))
+    y = torch.zeros((m, n), dtype=torch.int16, device="cuda")
+    kern = B.gemv_w4_bf16(_dev(torch, x), B.pack_w4(torch.from_numpy(codes)).cuda(), B.pack_w4_groups(torch.from_numpy(scales.view(np.int16))).cuda(),
+                          y, zeros=B.pack_w4_groups(torch.from_numpy(z)).cuda(), group=group)
+    torch.cuda.synchronize()
+    _run(ctx, torch, kern, "hi")
+    _w4_ok(_host(y), x, codes, scales, z, group)
 
 
 def test_gemv_w4_rows_do_not_depend_on_the_number_of_vectors(env):
