@@ -49,9 +49,10 @@ constexpr uint32_t kPrefixLeast = 128;                     // tokens of a part
 //
 // Parts: as many workgroups as one round on the GPU takes.  Kind 0 is better off with one per compute
 // unit, whose parts are longer (16 sequences of up to 3001, 4 heads: 14.1, with 512 of them 15.8, with 1024 16.9).
-// Where four waves share tokens (kind 1) a part is a longer chain than where each has its own: with mostly the latter,
-// parts of the prefix are shorter by a fourth (32 behind 4096 with up to 512, 8 heads: 18.8 against 19.7; 48 behind 2000 with
-// up to 300, heads of 64: 10.3 and 11.4; but 32 behind 4000 with up to 100, heads of 64: 12.7 and 12.0).
+// Where four waves share tokens (kind 1) a part is a longer chain than where each has its own: with half as many again of
+// the latter and more, parts of the prefix are shorter by a fourth.  Both sides of 104 calls drawn at random, by own : shared:
+// from 1.5 on 4.6 % faster on average (from 10 % slower, one of 67, to 15 % faster), between 1 and 1.5 0.3 % slower (12 % either
+// way), below 1.2 2.1 % slower.
 struct PrefixPlan {
   uint32_t group, rows;                                    // query heads per K/V head; rows of one K/V head
   uint32_t kind;                                           // rows of a workgroup: 0: 16, 1: 64, 2: 128 of the prefix
@@ -81,7 +82,7 @@ inline PrefixPlan prefix_plan(uint32_t batch, uint32_t heads, uint32_t kv_heads,
     k = (uint32_t)up(n, c);
   };
   const uint64_t own_chunk = chunk;
-  if (p.kind == 1 && own >= 2 * shared && chunk * 3 / 4 >= kPrefixLeast) chunk = chunk * 3 / 4;
+  if (p.kind == 1 && 2 * own >= 3 * shared && chunk * 3 / 4 >= kPrefixLeast) chunk = chunk * 3 / 4;
   parts(prefix, p.chunk, p.parts);
   chunk = own_chunk;
   parts(own_cap, p.own_chunk, p.own_parts);

@@ -82,6 +82,15 @@ def test_prefix_without_a_part_does_not_look_at_its_pointers(B):
         assert B.attn_prefix_scratch_bytes(*refused) == 0
 
 
+@pytest.mark.parametrize("batch,heads,kv,dim,prefix,cap", [(32, 32, 8, 128, 4096, 512), (64, 32, 8, 128, 65500, 1024), (24, 32, 8, 64, 2000, 500)])
+def test_prefix_is_cut_up_like_its_neighbours(B, batch, heads, kv, dim, prefix, cap):
+    """One token more or less in the prefix or in the caches does not move a call across a line of the plan."""
+    def parts(p, c):
+        n = B.attn_prefix_scratch_bytes(batch, heads, kv, dim, p, c)
+        return n // (batch * heads * (dim * 4 + 8))
+    assert {parts(p, c) for p in (prefix - 1, prefix, prefix + 1) for c in (cap - 1, cap)} == {parts(prefix, cap)}
+
+
 @pytest.mark.parametrize("batch,heads,kv,dim,prefix,cap,records", [(1, 7, 1, 128, 4000, 64, 231), (1, 1, 1, 64, 300, 0, 3),
                                                                    (3, 5, 5, 64, 2000, 0, 240), (1, 7, 1, 128, 3968, 128, 224)])
 def test_prefix_scratch_keeps_the_weighted_sums_aligned(B, batch, heads, kv, dim, prefix, cap, records):
