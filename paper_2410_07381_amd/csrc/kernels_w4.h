@@ -42,19 +42,26 @@ constexpr uint32_t kW4Piece = 1024;                        // bytes of x that on
 // Rows of tiles that a workgroup takes.  It reads x once for all of them (from the L2s, 24 bytes a clock and compute
 // unit where all of them read the same): with many vectors that is more than the codes, so fewer workgroups
 // with more rows each are faster, as long as each of the 256 compute units has the same number of them.  Cost of
-// a workgroup: its rows, and a quarter of a row per vector, and four rows' long way if there is nothing beside it; of
-// equals the one with more rows.  More than 2 (3, 4) rows did not pay with 4 or 5 (8, 16) vectors, and
-// with 1 or 2 vectors only large products gain from a second.
-// us by rows, groups of 128, k = 4096: 1 vector, n = 11008 7.2 8.0 7.6, 32000 14.8 14.5 14.7; 4 vectors, 11008 8.7 7.8
-// 7.8 9.8, 16384 10.7 8.5 10.3 11.2; 16 vectors, 4096 6.1 6.9 7.4 9.8, 11008 14.5 11.0 8.5 11.0, 16384 18.6 11.4 13.1
-// 12.6, 32000 34.6 19.5 18.0 16.1.
+// a workgroup: its rows, and a quarter of a row per vector; of equals the one with more rows.  Four rows are left out where
+// that is one workgroup per compute unit at most, with nothing beside its long way (800 to 1024 tiles, 13 to 16 vectors, two
+// rows and four: k = 2048, groups of 32, 6.5 to 7.2 and 7.2 to 9.1; 4096, of 64, 10.8 to 12.3 and 13.1 to 14.0; 1024 the
+// same; 4096, of 128, 9.4 to 10.7 and 9.4 to 10.3).
+// us by rows, groups of 128, k = 4096, 256 / 688 / 1024 / 2000 tiles:
+//    1 vector   3.7 4.7 5.9 7.5 /  7.0  7.4 6.2  8.5 /  8.7  7.7  9.5  8.9 / 15.1 14.2 14.7 15.5
+//    4 vectors  4.1 4.8 6.0 7.7 /  8.3  7.4 6.2  9.3 / 10.6  7.4  9.4  8.9 / 18.7 14.3 14.6 15.6
+//    8 vectors  4.7 5.2 6.0 8.0 / 10.1  8.0 6.3  8.9 / 12.9  8.1  9.9  9.2 / 23.7 15.2 15.0 15.3
+//   16 vectors  6.1 6.4 7.2 8.5 / 14.2 10.8 7.4 10.3 / 18.2 10.7 12.5 10.3 / 34.0 19.0 17.7 15.7
+// k and the groups are not asked for.  Over 254 random calls (n to 65536, k to 11585, all groups) the choice is 2.4 % slower
+// than the best of the four on average; worst with four rows, where two are faster with small groups or short k (17 of 20
+// calls; 2889 tiles, k = 560, groups of 64, 16 vectors: 5.7 and 7.4).
 inline uint32_t w4_rows(uint32_t m, uint32_t n) {
   const uint32_t tiles = (n + kW4Rows - 1) / kW4Rows, most = m <= 6 ? 2 : m <= 10 ? 3 : 4;
   if (m <= 2) return tiles > 1024 ? 2 : 1;
   uint32_t best = 1;
   uint64_t least = ~0ull;
   for (uint32_t r = 1; r <= most; ++r) {
-    const uint64_t groups = (tiles + r - 1) / r, cost = (groups + 255) / 256 * (4 * r + m) + (r == 4 && groups <= 256 ? 17 : 0);
+    const uint64_t groups = (tiles + r - 1) / r, cost = (groups + 255) / 256 * (4 * r + m);
+    if (r == 4 && groups <= 256) continue;
     if (cost <= least) { least = cost; best = r; }
   }
   return best;
