@@ -2,8 +2,8 @@
 // of different lengths packed one behind the other) and single-token queries of a batch that
 // shares a prefix.
 //
-// Scores never leave the registers.  With m the running maximum of a row's scores and p = exp(s - m),
-// a row's state is (m, l = sum of p, acc = sum of p v); a new maximum rescales l and acc by
+// Scores never leave the registers.  With m the running maximum of a row's scores and p = exp(s - m) (a softmax
+// in one pass, Milakov and Gimelshein 2018), a row's state is (m, l = sum of p, acc = sum of p v); a new maximum rescales l and acc by
 // exp(m_old - m_new), and the output is acc / l.  Everything is held in fp32; q, k, v and the p that
 // enter the second product are bf16, so each p is off by at most 2^-8 of itself, which is
 // what the output's own rounding costs.
@@ -21,8 +21,9 @@
 // 128-bit read serves at once, and the 16 tokens of a transposing read, fall into different banks.
 //
 // What bounds long prompts is the matrix pipe, and the clock that it is left with: 32768 tokens, 8 heads of 128 on one
-// K/V head, take 1.92 ms, 1.15 PFLOP/s (8192^3 of the GEMM tile: 1.5), with the pipe busy for 65 % of the cycles at 1.55 GHz.
-// 8192 tokens, 32/8 heads, 505 us (1.09); 4096, 32 heads, 140 (0.98); 16384, 16 heads of 64, 580 (0.95).
+// K/V head, take 1.87 to 1.94 ms, 1.13 to 1.18 PFLOP/s (8192^3 of the GEMM tile: 1.5), 3.06 million cycles in which the compute
+// units have work, so 1.6 GHz, and in 69 % of them the pipe is busy.
+// 8192 tokens, 32/8 heads, 487 us (1.13); 4097, 32 heads, 148 (0.93); 16384, 16 heads of 64, 567 (0.97).
 // Short ones are a chain of latencies: 128 tokens, 12 heads of 64, 5.4 us, of which an empty launch is 2.4; 512
 // tokens, 32/8 heads of 128, 13.6.
 #pragma once

@@ -3,7 +3,7 @@
 // y[v][r] = sum over groups g of s[r][g] * sum over k of g of (code[r][k] - zero[r][g]) x[v][k].
 //
 // What bounds it is reading the codes, half a byte each.  A code becomes a bf16 with one AND-OR for
-// two of them: 0x4300 | code is 128 + code.  The 128 and the zero point are taken out again by a second
+// two of them: 0x4300 | code is 128 + code (a small integer as the mantissa of a power of two, an old way).  The 128 and the zero point are taken out again by a second
 // MFMA with the constant -(128 + zero), which is exact in bf16, so that a group's sum has the
 // rounding of fp32 alone; then the scale is applied, in fp32.  The vectors are the 16 rows of an MFMA,
 // weight rows its columns, so one vector costs what sixteen do and a lane needs the scale of one row.
@@ -18,8 +18,8 @@
 // number of vectors nor on the variant.
 //
 // Measured (us; the codes, scales and zero points read once at 5.1 TB/s in brackets, and an empty launch is 2.4): 1 vector,
-// 4096 x 4096 3.5 [1.7], 4096 x 11008 in groups of 64 with zero points 7.7 [4.8]; 16 vectors, 11008 x 4096 8.3 [4.6]; 5 vectors,
-// 50257 x 4096 in groups of 32 with zero points 30.0 [23.9].  With many vectors a short product is bound by reading x
+// 4096 x 4096 3.6 [1.7], 4096 x 11008 in groups of 64 with zero points 7.5 [4.8]; 16 vectors, 11008 x 4096 8.3 [4.6]; 5 vectors,
+// 50257 x 4096 in groups of 32 with zero points 29.5 [23.9].  With many vectors a short product is bound by reading x
 // from the L2s once per workgroup (16 vectors, 4096 x 16384: 19.7 [7.3]).  Beginning the rows of tiles at different columns, so that
 // not all ask for the same x at once, gave 9.9 for 10.9 with 8 vectors, 16384 x 4096, and 33.1 for 31.5 with 5, 50257 x 4096.
 #pragma once
