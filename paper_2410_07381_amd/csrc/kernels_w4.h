@@ -2,11 +2,11 @@
 //
 // y[v][r] = sum over groups g of s[r][g] * sum over k of g of (code[r][k] - zero[r][g]) x[v][k].
 //
-// What bounds it is reading the codes, half a byte each.  A code becomes a bf16 with one AND-OR for
-// two of them: 0x4300 | code is 128 + code (a small integer as the mantissa of a power of two, an old way).  The 128 and the zero point are taken out again by a second
-// MFMA with the constant -(128 + zero), which is exact in bf16, so that a group's sum has the
-// rounding of fp32 alone; then the scale is applied, in fp32.  The vectors are the 16 rows of an MFMA,
-// weight rows its columns, so one vector costs what sixteen do and a lane needs the scale of one row.
+// What bounds it is reading the codes, half a byte each.  A code becomes a bf16 with one AND-OR for two of
+// them: 0x4300 | code is 128 + code, a small integer as the mantissa of a power of two.  The 128 and the zero
+// point are taken out again by a second MFMA with the constant -(128 + zero), which is exact in bf16, so that a
+// group's sum has the rounding of fp32 alone; then the scale is applied, in fp32.  The vectors are the 16 rows
+// of an MFMA, weight rows its columns, so one vector costs what sixteen do and a lane needs the scale of one row.
 //
 // The codes lie in memory as the lanes want them: a tile is 16 rows by 128 weights, 1 KB that a wave
 // reads with one 16-byte load a lane; word i of lane 16 q + r holds weights 32 i + 8 q to 32 i + 8 q + 7
