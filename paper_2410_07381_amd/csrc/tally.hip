@@ -62,7 +62,7 @@ static_assert(kMaxShared + kRingCount == kMaxNative && (uint32_t)GemmCover::kRin
   static_assert(GemmRingT<ra, rb, r>::MIN_WAVES == ring_per_cu(ra, rb, r), "as many as the launch bounds say");
 GEMM_RINGS(GEMM_RING_CHECK)
 
-typedef std::array<uint32_t, 5> CallSizes;
+typedef std::array<uint32_t, 4> CallSizes;
 
 struct KernelOps {
   const char *name;
@@ -97,7 +97,8 @@ struct KernelOps {
   bool together;
   // the original form's kernel depends on what else is on the GPU
   bool chooses;
-  // what a block's time depends on and the grid does not say (null: nothing that keeps measurements apart)
+  // what a block's time depends on and the grid does not say (null: nothing that keeps measurements apart).  Not the
+  // exact rows and tokens: prompts that differ by a few tokens share what was measured
   CallSizes (*sizes)(const void *args);
 };
 
@@ -622,12 +623,12 @@ uint32_t w4_choice(const void *args, uint32_t, uint64_t *) { return w4_range(arg
 CallSizes w4_sizes(const void *args) {
   tally_gemv_w4_args a;
   memcpy(&a, args, sizeof(a));
-  return {a.m, a.n, a.k, a.group, a.zeros != nullptr};
+  return {a.m, a.k, a.group, a.zeros != nullptr};
 }
 CallSizes prompt_sizes(const void *args) {
   tally_attn_prompt_args a;
   memcpy(&a, args, sizeof(a));
-  return {a.total, a.n_seqs, a.heads, a.kv_heads, a.dim};
+  return {a.n_seqs, a.heads, a.kv_heads, a.dim};
 }
 hipError_t launch_native_w4(hipStream_t s, const void *args, tally_dim3 g, uint32_t how) {
 #define W4_CASE(i, ...) case i: return launch_native_t<__VA_ARGS__>(s, args, g, how);
