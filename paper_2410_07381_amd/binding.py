@@ -467,11 +467,12 @@ def pack_w4(codes):
     [ceil(n / 16), ceil(k / 128), 64, 4] of 16 rows by 128 columns, filled up with zeros."""
     import torch
     n, k = codes.shape
-    # (a code of more bits would change its neighbours)
-    assert not codes.is_floating_point() and (codes.numel() == 0 or (int(codes.min()) >= 0 and int(codes.max()) <= 15))
+    assert not codes.is_floating_point()
     tiles, blocks = -(-n // 16), -(-k // 128)
     full = torch.zeros((tiles * 16, blocks * 128), dtype=torch.int64, device=codes.device)
     full[:n, :k] = codes
+    # (a code of more bits would change its neighbours)
+    assert full.numel() == 0 or (int(full.min()) >= 0 and int(full.max()) <= 15)
     at = torch.tensor([0, 16, 4, 20, 8, 24, 12, 28], device=codes.device)
     words = (full.view(tiles, 16, blocks, 4, 4, 8) << at).sum(-1)      # tile, row, block, word, quarter
     words = words.permute(0, 2, 4, 1, 3).reshape(tiles, blocks, 64, 4)

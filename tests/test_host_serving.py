@@ -274,7 +274,8 @@ def test_the_binding_refuses_types_that_would_be_taken_for_others(B):
     for codes in (torch.tensor([[16] * 8]), torch.tensor([[-1] * 8]), torch.ones(1, 8)):
         with pytest.raises(AssertionError):
             B.pack_w4(codes)
-    assert B.pack_w4(torch.full((1, 8), 15)).shape == (1, 1, 64, 4)
+    for kind in (torch.uint8, torch.int8, torch.int16, torch.uint16, torch.int32, torch.uint32, torch.int64):
+        assert (B.pack_w4(torch.full((1, 8), 15).to(kind))[0, 0, 0] == torch.tensor([-1, 0, 0, 0])).all()
     assert B.pack_w4_groups(torch.full((3, 2), 128, dtype=torch.uint8)).max() == 128
     with pytest.raises(AssertionError):
         B.pack_w4_groups(torch.full((3, 2), 129, dtype=torch.uint8))
