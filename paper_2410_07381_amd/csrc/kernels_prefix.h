@@ -15,7 +15,7 @@
 //
 // Measured (us of a call; K and V read once at 5.1 TB/s in brackets): 16 sequences of 0 to 3001 tokens, 28/4 heads of 128,
 // 14.0 [9.6]; 64 of 0 to 2048, 32/8, 64.7 [52.5]; 32 behind 4096 tokens with 0 to 512 of their own 18.4 [9.9]; 64 behind 65500
-// with 0 to 1024 109 to 114 [78.6]; 4 behind 512, 12 heads of 64, 6.2, of which an empty launch is 2.4.
+// with 0 to 1024 109 to 118 [78.6]; 4 behind 512, 12 heads of 64, 6.2, of which an empty launch is 2.4.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
