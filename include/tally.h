@@ -65,7 +65,10 @@ typedef enum {
   TALLY_K_ATTN_PROMPT_BF16 = 10,  /* causal attention over whole prompts, packed            */
   TALLY_K_ATTN_PREFIX_BF16 = 11,  /* one token per sequence of a batch behind a shared prefix (native only) */
   TALLY_K_GEMV_W4_BF16 = 12,      /* products with 4-bit weights, one to sixteen vectors     */
-  TALLY_K_COUNT = 13
+  TALLY_K_ROPE_BF16 = 13,         /* rotary positions, of whole heads or a part of them     */
+  TALLY_K_KV_APPEND_FP8 = 14,     /* keys, rotated on the way, and values to a paged 8-bit cache */
+  TALLY_K_ATTN_PAGED_FP8 = 15,    /* one token per sequence over that cache (native only)   */
+  TALLY_K_COUNT = 16
 } tally_kernel_id;
 
 typedef struct { uint32_t x, y, z; } tally_dim3;
@@ -189,6 +192,83 @@ typedef struct {
   uint32_t m, n, k, group, ld_x, ld_y;
 } tally_gemv_w4_args;
 
+/* Rotary positions.  Of each head's first `rot` dims, pair i (i < rot / 2) is turned by the angle
+ * positions[t] * freqs[i]:
+ *   out1 = magnitude (x1 cos - x2 sin),  out2 = magnitude (x2 cos + x1 sin),
+ * where the pair is dims (i, i + rot / 2), or (2 i, 2 i + 1) with TALLY_ROPE_INTERLEAVED.  The dims behind
+ * them are copied.  TALLY_ROPE_INVERSE turns by the negative angle, still times magnitude: the transpose of
+ * the operator, so it takes the gradient of out to that of x.
+ * x, out: total x heads x dim, bf16; out may be x itself (each run then turns on what the one before left), any other
+ * overlap is undefined.  dim a multiple of 16 up to 512, rot a multiple of 16 up to dim.  freqs: rot / 2 fp32,
+ * radians per position; positions: total int32, any; both in DEVICE memory.  magnitude 0 stands for 1; negative,
+ * above 64 or not finite is refused.  ld_*: elements between tokens (multiples of 8, at most 2^20, 0: dense),
+ * x and out 16-byte aligned, total at most 2^30 and total x heads at most 2^36.
+ * Arithmetic: the product positions[t] * freqs[i], its sine and cosine in fp64 (angles up to 2^31 radians), which are
+ * rounded to fp32; the products with x in fp32; the outputs are rounded once.
+ * Logical grid: blocks of 1 to 32 tokens, by the sizes (tally_logical_grid), below 2^24. */
+#define TALLY_ROPE_INTERLEAVED 1u
+#define TALLY_ROPE_INVERSE 2u
+typedef struct {
+  const uint16_t *x; uint16_t *out; const float *freqs; const int32_t *positions;
+  uint32_t total, heads, dim, rot, ld_x, ld_out, flags;
+  float magnitude;
+} tally_rope_args;
+
+/* A paged cache in 8 bits.  A page has room for `page` (16, 32, 64 or 128) tokens of one sequence, all K/V heads;
+ * row s of `table` (int32, seq_pages of them, rows ld_table apart, 0: dense) names sequence s's pages in order, so
+ * that its token i is token i % page of page table[s][i / page].  Numbers are bytes, OCP e4m3, and a byte e for each page
+ * and head says that those of the block stand for 2^(e - 127) times as much (e from 1 to 254):
+ *   k_pages: n_pages x kv_heads x page x dim,  v_pages: n_pages x kv_heads x page / 16 x dim x 16 (the values of 16
+ *   tokens in a dim lie side by side, as the product with them wants them), k_exps, v_exps: n_pages x kv_heads.
+ * A page may stand in several rows for reading; a page that a call writes to must stand in one.
+ *
+ * Append: the tokens cu_seqlens[s] .. cu_seqlens[s + 1] - 1 of k and v (total x kv_heads x dim, bf16, packed as for
+ * TALLY_K_ATTN_PROMPT_BF16) are sequence s's last ones: lens[s] says how many it has WITH them.  With rot > 0 k is
+ * turned as TALLY_K_ROPE_BF16 does (flags without TALLY_ROPE_INVERSE) by its place in the sequence, or by positions
+ * (total int32, or NULL).  Then, for each block:
+ *   e = the smallest that has |x| <= 448 x 2^(e - 127) for all new numbers of the block; where the page holds tokens before them,
+ *   at least the e that is there;
+ *   a number is stored as the e4m3 nearest to x / 2^(e - 127), ties to even; NaN and infinities as NaN, and they
+ *   do not count for e;
+ *   where e grows, the numbers held before the new ones are stored anew: divided by a power of two, so all are exact but those
+ *   that fall below the smallest normal, which are rounded again.
+ * k is turned in fp64 and rounded once, to its code.  So a call made twice leaves what it left the first time.
+ * What a page holds behind a sequence's last token, and pages that no new token goes to, stay as they are.  Tokens that
+ * belong to no sequence, whose place is negative or beyond seq_pages x page, or whose page is none of 0 .. n_pages - 1,
+ * are not stored.  cu_seqlens, lens, table, positions, freqs are DEVICE memory; values of cu_seqlens outside [0, total] count
+ * as its ends, nothing outside the tensors is touched whatever they hold.
+ * dim 64 or 128; rot a multiple of 16 up to dim (0: freqs and positions are not looked at); magnitude as above; k, v and the
+ * pages 16-byte aligned; ld_k, ld_v as ld_* above; total at most 2^30, n_pages at most 2^30, seq_pages x page at most 2^28.
+ * Logical grid: (kv_heads in groups of 4, 2 or 1: 64 / page heads, at least one) x (total / page + 2 n_seqs), below 2^24;
+ * sequence s has the slots from cu_seqlens[s] / page + 2 s on for the pages that its new tokens go to. */
+typedef struct {
+  const uint16_t *k; const uint16_t *v; const int32_t *cu_seqlens; const int32_t *lens; const int32_t *table;
+  const float *freqs; const int32_t *positions;
+  uint8_t *k_pages; uint8_t *v_pages; uint8_t *k_exps; uint8_t *v_exps;
+  uint32_t total, n_seqs, kv_heads, dim, page, n_pages, seq_pages, ld_table, ld_k, ld_v, rot, flags;
+  float magnitude;
+} tally_kv_append_args;
+
+/* Single-token attention over such a cache: query head h of sequence b attends to its first lens[b] tokens,
+ *   out[b][h] = sum_t p_t v_t / sum_t p_t,  p_t = exp(scale q[b][h] . k_t),
+ * with k_t and v_t those of K/V head h / (heads / kv_heads).  Zeros where there is no token at all (where there
+ * are, and all scores are -inf, NaN).
+ * q, out: batch x heads x dim, bf16; heads a multiple of kv_heads, dim 64 or 128.  lens: batch int32 in DEVICE memory;
+ * values outside [0, seq_pages x page] count as its ends.  What lies in pages behind lens does not reach the result, whatever
+ * it is, nor do entries of the table behind it; an entry that is none of 0 .. n_pages - 1 stands for a page whose
+ * tokens do not count.  ld_q, ld_out, scale and arithmetic as for TALLY_K_ATTN_PROMPT_BF16: what is stored in 8 bits enters the products
+ * exactly, p is rounded to bf16 before the second one, and the sum is of the rounded ones.
+ * scratch: caller-owned device memory of tally_attn_paged_scratch_bytes() bytes, 16-byte aligned; two calls that
+ * may overlap need one each.  batch x heads at most 2^20, seq_pages x page at most 2^28, batch x seq_pages x page
+ * at most 2^36, n_pages at most 2^30. */
+typedef struct {
+  const uint16_t *q; uint16_t *out;
+  const uint8_t *k_pages; const uint8_t *v_pages; const uint8_t *k_exps; const uint8_t *v_exps;
+  const int32_t *table; const int32_t *lens; void *scratch;
+  uint32_t batch, heads, kv_heads, dim, page, n_pages, seq_pages, ld_table, ld_q, ld_out;
+  float scale;
+} tally_attn_paged_args;
+
 typedef struct {
   uint32_t kernel_id;        /* tally_kernel_id                                           */
   tally_dim3 grid, block;    /* LOGICAL grid and block, as the original kernel is launched */
@@ -227,6 +307,9 @@ size_t tally_attn_decode_scratch_bytes(uint32_t heads);
 /* Scratch of TALLY_K_ATTN_PREFIX_BF16; 0 for sizes that it refuses. */
 size_t tally_attn_prefix_scratch_bytes(uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t dim,
                                        uint32_t prefix, uint32_t own_cap);
+/* Scratch of TALLY_K_ATTN_PAGED_FP8; 0 for sizes that it refuses. */
+size_t tally_attn_paged_scratch_bytes(uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t dim, uint32_t page,
+                                      uint32_t seq_pages);
 
 /* ---- the three launch forms ------------------------------------------------------- */
 

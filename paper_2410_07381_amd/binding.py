@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from typing import NamedTuple
 
 import numpy as np
 
@@ -35,6 +36,8 @@ LIB_PATH = os.path.join(_HERE, "libtally.so")
 K_SAXPY, K_REDUCE_SUM, K_REDUCE_FINAL, K_GEMM_BF16, K_GEMV_BF16 = 0, 1, 2, 3, 4
 K_SOFTMAX_F32, K_LAYERNORM_F32, K_ATTN_DECODE_BF16, K_GEMM_BF16_SMALL = 5, 6, 7, 8
 K_GEMM_BF16_N128, K_ATTN_PROMPT_BF16, K_ATTN_PREFIX_BF16, K_GEMV_W4_BF16 = 9, 10, 11, 12
+K_ROPE_BF16, K_KV_APPEND_FP8, K_ATTN_PAGED_FP8 = 13, 14, 15
+ROPE_INTERLEAVED, ROPE_INVERSE = 1, 2
 JOB_QUEUED, JOB_RUNNING, JOB_STOPPED, JOB_COMPLETE = 0, 1, 2, 3
 OK, ERR_INVALID_ARG, ERR_BAD_STATE, ERR_HIP, ERR_NOMEM, ERR_UNSUPPORTED = 0, -1, -2, -3, -4, -5
 CFG_PTB, CFG_SLICED, CFG_NATIVE, CFG_AUTO = 0, 1, 2, 3
@@ -44,7 +47,7 @@ POLICY_TALLY, POLICY_PRIORITY_NATIVE, POLICY_NONE = 0, 1, 2
 
 EXPORTS = [
     "tally_create", "tally_destroy", "tally_logical_grid", "tally_attn_decode_scratch_bytes",
-    "tally_attn_prefix_scratch_bytes",
+    "tally_attn_prefix_scratch_bytes", "tally_attn_paged_scratch_bytes",
     "tally_launch_native", "tally_launch_sliced", "tally_launch_ptb", "tally_preempt",
     "tally_resume", "tally_progress", "tally_pump", "tally_wait", "tally_job_free",
     "tally_launch_ptb_until", "tally_resume_until", "tally_coverage", "tally_marker",
@@ -125,6 +128,30 @@ class GemvW4Args(C.Structure):
                 ("group", C.c_uint32), ("ld_x", C.c_uint32), ("ld_y", C.c_uint32)]
 
 
+class RopeArgs(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("out", C.c_void_p), ("freqs", C.c_void_p), ("positions", C.c_void_p),
+                ("total", C.c_uint32), ("heads", C.c_uint32), ("dim", C.c_uint32), ("rot", C.c_uint32),
+                ("ld_x", C.c_uint32), ("ld_out", C.c_uint32), ("flags", C.c_uint32), ("magnitude", C.c_float)]
+
+
+class KvAppendArgs(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("cu_seqlens", C.c_void_p), ("lens", C.c_void_p),
+                ("table", C.c_void_p), ("freqs", C.c_void_p), ("positions", C.c_void_p),
+                ("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("k_exps", C.c_void_p), ("v_exps", C.c_void_p),
+                ("total", C.c_uint32), ("n_seqs", C.c_uint32), ("kv_heads", C.c_uint32), ("dim", C.c_uint32),
+                ("page", C.c_uint32), ("n_pages", C.c_uint32), ("seq_pages", C.c_uint32), ("ld_table", C.c_uint32),
+                ("ld_k", C.c_uint32), ("ld_v", C.c_uint32), ("rot", C.c_uint32), ("flags", C.c_uint32),
+                ("magnitude", C.c_float)]
+
+
+class AttnPagedArgs(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("out", C.c_void_p), ("k_pages", C.c_void_p), ("v_pages", C.c_void_p),
+                ("k_exps", C.c_void_p), ("v_exps", C.c_void_p), ("table", C.c_void_p), ("lens", C.c_void_p),
+                ("scratch", C.c_void_p), ("batch", C.c_uint32), ("heads", C.c_uint32), ("kv_heads", C.c_uint32),
+                ("dim", C.c_uint32), ("page", C.c_uint32), ("n_pages", C.c_uint32), ("seq_pages", C.c_uint32),
+                ("ld_table", C.c_uint32), ("ld_q", C.c_uint32), ("ld_out", C.c_uint32), ("scale", C.c_float)]
+
+
 class KernelDesc(C.Structure):
     _fields_ = [("kernel_id", C.c_uint32), ("grid", Dim3), ("block", Dim3),
                 ("args", C.c_void_p), ("args_size", C.c_size_t)]
@@ -200,6 +227,7 @@ def _load():
         "tally_logical_grid": ([u32, vp, C.c_size_t, P(Dim3), P(Dim3)], i32),
         "tally_attn_decode_scratch_bytes": ([u32], C.c_size_t),
         "tally_attn_prefix_scratch_bytes": ([u32] * 6, C.c_size_t),
+        "tally_attn_paged_scratch_bytes": ([u32] * 6, C.c_size_t),
         "tally_launch_native": ([vp, P(KernelDesc), i32], i32),
         "tally_launch_attn_decode_static": ([vp, P(AttnDecodeArgs), i32], i32),
         "tally_launch_sliced": ([vp, P(KernelDesc), u32, u32, i32, P(vp)], i32),
@@ -273,6 +301,7 @@ _ARGS_FOR = {
     K_GEMV_BF16: GemvArgs,
     K_SOFTMAX_F32: SoftmaxArgs, K_LAYERNORM_F32: LayerNormArgs, K_ATTN_DECODE_BF16: AttnDecodeArgs,
     K_ATTN_PROMPT_BF16: AttnPromptArgs, K_ATTN_PREFIX_BF16: AttnPrefixArgs, K_GEMV_W4_BF16: GemvW4Args,
+    K_ROPE_BF16: RopeArgs, K_KV_APPEND_FP8: KvAppendArgs, K_ATTN_PAGED_FP8: AttnPagedArgs,
 }
 
 
@@ -487,6 +516,142 @@ def pack_w4_groups(t):
     full = torch.zeros((-(-n // 16) * 16, groups), dtype=t.dtype, device=t.device)
     full[:n] = t
     return full.view(-1, 16, groups).transpose(1, 2).contiguous()
+
+
+# ---------------------------------------------------------------- rotary positions and the paged cache
+def rope_freqs(rot, base=10000.0, factor=1.0, scaling="positions", context=None, turns=(1.0, 32.0), device=None):
+    """Frequencies of the rot / 2 pairs, base ** (-2 i / rot) radians a position, as rope_bf16 and kv_append_fp8 take
+    them: (fp32 tensor, magnitude).  For contexts `factor` times as long as those of training:
+      "positions"  every frequency is divided by factor (arXiv 2306.15595);
+      "base"       the base is raised so that the slowest pair turns factor times slower and the fastest as before;
+      "parts"      pairs that make fewer than turns[0] turns within `context` positions (those of training) are divided by
+                   factor, those that make more than turns[1] stay, in between both are mixed evenly; q and k grow
+                   by 0.1 ln(factor) + 1 (arXiv 2309.00071)."""
+    import math
+
+    import torch
+    assert rot > 0 and rot % 2 == 0 and base > 0 and factor >= 1 and scaling in ("positions", "base", "parts")
+    i = torch.arange(rot // 2, dtype=torch.float64)
+    if scaling == "base":
+        assert rot > 2
+        base = base * factor ** (rot / (rot - 2))
+    freqs, magnitude = base ** (-2 * i / rot), 1.0
+    if scaling == "positions":
+        freqs = freqs / factor
+    elif scaling == "parts":
+        assert context and turns[1] > turns[0]
+        keep = ((context * freqs / (2 * math.pi) - turns[0]) / (turns[1] - turns[0])).clamp(0, 1)
+        freqs = freqs * keep + freqs / factor * (1 - keep)
+        magnitude = 0.1 * math.log(factor) + 1.0
+    return freqs.to(torch.float32).to(device), magnitude
+
+
+def _floats(t):
+    import torch
+    return t.dtype == torch.float32 and t.dim() == 1 and t.is_contiguous()
+
+
+def rope_bf16(x, out, freqs, positions, interleaved=False, inverse=False, magnitude=None):
+    """Rotary positions: x, out [total, heads, dim], 16-bit storage tensors that may be views with padded tokens (the first
+    heads of a fused projection); out may be x.  The first 2 x len(freqs) dims of each head are turned by positions
+    (int32 [total]) times freqs (fp32, radians): pairs (i, i + len(freqs)), or (2 i, 2 i + 1) with interleaved.  inverse: by the negative
+    angle, the operator's transpose, for gradients.  magnitude: what the turned dims are multiplied with, None for 1."""
+    total, heads, dim = x.shape
+    assert out.shape == x.shape and _is_bf16(x, out) and _floats(freqs)
+    assert _is_int32(positions) and positions.numel() == total
+    args = RopeArgs(x.data_ptr(), out.data_ptr(), freqs.data_ptr(), positions.data_ptr(), total, heads, dim,
+                    2 * freqs.numel(), _rows(x, dim), _rows(out, dim),
+                    (ROPE_INTERLEAVED if interleaved else 0) | (ROPE_INVERSE if inverse else 0), _scale(magnitude))
+    return Kernel(K_ROPE_BF16, args, (x, out, freqs, positions))
+
+
+class PagedCache(NamedTuple):
+    """Keys and values in pages of 8-bit numbers (include/tally.h has the layout): k [pages, kv_heads, page, dim], v [pages,
+    kv_heads, page / 16, dim, 16], uint8 or float8_e4m3fn; k_exps, v_exps uint8 [pages, kv_heads]."""
+    k: object
+    v: object
+    k_exps: object
+    v_exps: object
+
+    @classmethod
+    def empty(cls, pages, kv_heads, page, dim, device="cuda"):
+        import torch
+        assert page in (16, 32, 64, 128) and dim in (64, 128)
+        z = lambda *s: torch.zeros(s, dtype=torch.uint8, device=device)
+        return cls(z(pages, kv_heads, page, dim), z(pages, kv_heads, page // 16, dim, 16), z(pages, kv_heads), z(pages, kv_heads))
+
+    def values(self):
+        """What the pages stand for, fp32: keys and values [pages, kv_heads, page, dim]."""
+        import torch
+
+        def of(codes, exps):
+            scale = torch.exp2(exps.to(torch.float64) - 127).to(torch.float32)
+            return codes.view(torch.float8_e4m3fn).to(torch.float32) * scale.view(*exps.shape, *[1] * (codes.dim() - 2))
+        pages, heads, page, dim = self.k.shape
+        return of(self.k, self.k_exps), of(self.v, self.v_exps).transpose(3, 4).reshape(pages, heads, page, dim)
+
+
+def _pages(cache, dim):
+    """(pages, kv_heads, page) of a cache for heads of `dim`."""
+    import torch
+    pages, heads, page, width = cache.k.shape
+    assert width == dim and page > 0 and page % 16 == 0 and cache.v.shape == (pages, heads, page // 16, dim, 16)
+    assert cache.k_exps.shape == cache.v_exps.shape == (pages, heads)
+    assert all(t.dtype in (torch.uint8, torch.float8_e4m3fn) and t.is_contiguous() for t in cache[:2])
+    assert all(t.dtype == torch.uint8 and t.is_contiguous() for t in cache[2:])
+    return pages, heads, page
+
+
+def _table(table, seqs):
+    """(pages per sequence, entries between rows) of a table of pages."""
+    import torch
+    assert table.dtype == torch.int32 and table.dim() == 2 and table.shape[0] == seqs and table.shape[1] > 0
+    return table.shape[1], _rows(table)
+
+
+def kv_append_fp8(k, v, cu_seqlens, lens, table, cache, freqs=None, positions=None, interleaved=False, magnitude=None):
+    """Keys and values of packed tokens go to a paged cache: k, v [total, kv_heads, dim], 16-bit storage tensors that may be views
+    with padded tokens; cu_seqlens int32 [sequences + 1]: where each sequence's tokens begin and the last one's end; lens int32
+    [sequences]: how many tokens each has WITH these, its last ones; table int32 [sequences, pages of one]; cache a PagedCache.
+    With freqs, keys are turned on the way as rope_bf16 does, by their place in the sequence or by positions (int32
+    [total]).  All but freqs=None and positions=None on the device."""
+    total, kv_heads, dim = k.shape
+    assert v.shape == k.shape and _is_bf16(k, v)
+    assert _is_int32(cu_seqlens) and cu_seqlens.numel() >= 2
+    seqs = cu_seqlens.numel() - 1
+    assert _is_int32(lens) and lens.numel() == seqs
+    pages, heads, page = _pages(cache, dim)
+    assert heads == kv_heads
+    seq_pages, ld_table = _table(table, seqs)
+    assert freqs is None or _floats(freqs)
+    assert positions is None or (freqs is not None and _is_int32(positions) and positions.numel() == total)
+    ptr = lambda t: None if t is None else t.data_ptr()
+    args = KvAppendArgs(k.data_ptr(), v.data_ptr(), cu_seqlens.data_ptr(), lens.data_ptr(), table.data_ptr(), ptr(freqs),
+                        ptr(positions), *(t.data_ptr() for t in cache), total, seqs, kv_heads, dim, page, pages, seq_pages, ld_table,
+                        _rows(k, dim), _rows(v, dim), 0 if freqs is None else 2 * freqs.numel(),
+                        ROPE_INTERLEAVED if interleaved else 0, _scale(magnitude))
+    return Kernel(K_KV_APPEND_FP8, args, (k, v, cu_seqlens, lens, table, *cache, freqs, positions))
+
+
+def attn_paged_fp8(q, cache, table, lens, out, scratch=None, scale=None):
+    """One query per head and sequence over a paged cache: q, out [batch, heads, dim], 16-bit storage tensors, padded sequences
+    allowed; table int32 [batch, pages of one], of whose tokens lens (int32 [batch]) count; scratch:
+    attn_paged_scratch_bytes() bytes, None where that is 0.  scale: None for dim ** -0.5."""
+    batch, heads, dim = q.shape
+    assert out.shape == q.shape and _is_bf16(q, out)
+    pages, kv_heads, page = _pages(cache, dim)
+    seq_pages, ld_table = _table(table, batch)
+    assert _is_int32(lens) and lens.numel() == batch
+    size = attn_paged_scratch_bytes(batch, heads, kv_heads, dim, page, seq_pages)
+    assert size == 0 if scratch is None else scratch.is_contiguous() and scratch.numel() * scratch.element_size() >= size
+    args = AttnPagedArgs(q.data_ptr(), out.data_ptr(), *(t.data_ptr() for t in cache), table.data_ptr(), lens.data_ptr(),
+                         None if scratch is None else scratch.data_ptr(), batch, heads, kv_heads, dim, page, pages, seq_pages,
+                         ld_table, _rows(q, dim), _rows(out, dim), _scale(scale))
+    return Kernel(K_ATTN_PAGED_FP8, args, (q, out, *cache, table, lens, scratch))
+
+
+def attn_paged_scratch_bytes(batch, heads, kv_heads, dim, page, seq_pages):
+    return int(_lib.tally_attn_paged_scratch_bytes(batch, heads, kv_heads, dim, page, seq_pages))
 
 
 # ---------------------------------------------------------------- context / jobs

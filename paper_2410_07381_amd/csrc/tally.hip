@@ -27,6 +27,8 @@
 #include "kernels_gemm.h"
 #include "kernels_prefix.h"
 #include "kernels_stream.h"
+#include "kernels_paged.h"
+#include "kernels_rope.h"
 #include "kernels_w4.h"
 #include "launch_forms.h"
 #include "turnaround.h"
@@ -51,6 +53,7 @@ double now_us() {
       .count();
 }
 
+bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // ---------------------------------------------------------------------------- registry
@@ -590,6 +593,94 @@ int grid_gemv_w4(const void *p, tally_dim3 *g, tally_dim3 *b) {
   *b = {64 * kW4Waves, 1, 1};
   return TALLY_OK;
 }
+bool magnitude_ok(float m) { return m >= 0.f && m <= 64.f; }
+int grid_rope(const void *p, tally_dim3 *g, tally_dim3 *b) {
+  auto *a = static_cast<const tally_rope_args *>(p);
+  if (!a->x || !a->out || !a->freqs || !a->positions || !a->total || a->total > (1u << 30) || !a->heads || !a->dim || a->dim % 16 ||
+      a->dim > 512 || !a->rot || a->rot % 16 || a->rot > a->dim || !magnitude_ok(a->magnitude) ||
+      (a->flags & ~(TALLY_ROPE_INTERLEAVED | TALLY_ROPE_INVERSE)))
+    return TALLY_ERR_INVALID_ARG;
+  if (!aligned16(a->x) || !aligned16(a->out) || !aligned4(a->freqs) || !aligned4(a->positions)) return TALLY_ERR_INVALID_ARG;
+  const uint64_t row = (uint64_t)a->heads * a->dim;
+  if (!attn_ld_ok(a->ld_x, row) || !attn_ld_ok(a->ld_out, row)) return TALLY_ERR_INVALID_ARG;
+  const uint32_t blocks = cdiv(a->total, rope_tokens(*a));
+  if (blocks >= (1u << 24)) return TALLY_ERR_INVALID_ARG;
+  *g = {blocks, 1, 1};
+  *b = kBlock256;
+  return TALLY_OK;
+}
+// What the operators on a paged cache share
+bool pages_ok(uint32_t kv_heads, uint32_t page, uint32_t n_pages, uint32_t seq_pages, uint32_t ld_table) {
+  return kv_heads <= (1u << 16) && (page == 16 || page == 32 || page == 64 || page == 128) && n_pages && n_pages <= (1u << 30) &&
+         seq_pages && (uint64_t)seq_pages * page <= (1u << 28) && (!ld_table || ld_table >= seq_pages);
+}
+int grid_append(const void *p, tally_dim3 *g, tally_dim3 *b) {
+  auto *a = static_cast<const tally_kv_append_args *>(p);
+  if (!a->k || !a->v || !a->cu_seqlens || !a->lens || !a->table || !a->k_pages || !a->v_pages || !a->k_exps || !a->v_exps ||
+      !a->total || a->total > (1u << 30) || !a->n_seqs || a->n_seqs > (1u << 24) || !attn_heads_ok(a->kv_heads, a->kv_heads, a->dim) ||
+      !pages_ok(a->kv_heads, a->page, a->n_pages, a->seq_pages, a->ld_table) || a->rot % 16 || a->rot > a->dim ||
+      !magnitude_ok(a->magnitude) || (a->flags & ~TALLY_ROPE_INTERLEAVED) || (a->rot && !a->freqs))
+    return TALLY_ERR_INVALID_ARG;
+  if (!aligned16(a->k) || !aligned16(a->v) || !aligned16(a->k_pages) || !aligned16(a->v_pages) || !aligned4(a->cu_seqlens) ||
+      !aligned4(a->lens) || !aligned4(a->table) || (a->rot && (!aligned4(a->freqs) || !aligned4(a->positions))))
+    return TALLY_ERR_INVALID_ARG;
+  const uint64_t row = (uint64_t)a->kv_heads * a->dim;
+  if (!attn_ld_ok(a->ld_k, row) || !attn_ld_ok(a->ld_v, row)) return TALLY_ERR_INVALID_ARG;
+  const uint64_t blocks = append_blocks(*a);
+  if (blocks >= (1u << 24)) return TALLY_ERR_INVALID_ARG;
+  *g = {(uint32_t)blocks, 1, 1};
+  *b = kBlock256;
+  return TALLY_OK;
+}
+bool paged_sizes_ok(uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t dim, uint32_t page, uint32_t seq_pages) {
+  return batch && attn_heads_ok(heads, kv_heads, dim) && (uint64_t)batch * heads <= (1u << 20) && pages_ok(kv_heads, page, 1, seq_pages, 0) &&
+         (uint64_t)batch * seq_pages * page <= (1ull << 36);
+}
+int grid_paged(const void *p, tally_dim3 *g, tally_dim3 *b) {
+  auto *a = static_cast<const tally_attn_paged_args *>(p);
+  if (!paged_sizes_ok(a->batch, a->heads, a->kv_heads, a->dim, a->page, a->seq_pages) || !attn_scale_ok(a->scale) ||
+      !pages_ok(a->kv_heads, a->page, a->n_pages, a->seq_pages, a->ld_table))
+    return TALLY_ERR_INVALID_ARG;
+  if (!a->q || !a->out || !a->k_pages || !a->v_pages || !a->k_exps || !a->v_exps || !a->table || !a->lens || !aligned16(a->q) ||
+      !aligned16(a->out) || !aligned16(a->k_pages) || !aligned16(a->v_pages) || !aligned4(a->table) || !aligned4(a->lens) ||
+      !aligned16(a->scratch) || (!a->scratch && !paged_plan(*a).single))
+    return TALLY_ERR_INVALID_ARG;
+  const uint64_t row = (uint64_t)a->heads * a->dim;
+  if (!attn_ld_ok(a->ld_q, row) || !attn_ld_ok(a->ld_out, row)) return TALLY_ERR_INVALID_ARG;
+  *g = {a->heads, a->batch, 1};
+  *b = kBlock256;
+  return TALLY_OK;
+}
+hipError_t launch_native_paged(hipStream_t s, const void *args, tally_dim3, uint32_t how) {
+  return launch_attn_paged(s, args, how & kUrgent);
+}
+uint32_t paged_choice(const void *args, uint32_t, uint64_t *groups) {
+  tally_attn_paged_args a;
+  memcpy(&a, args, sizeof(a));
+  const PagedPlan p = paged_plan(a);
+  *groups = (uint64_t)p.slots * a.kv_heads * p.row_tiles;
+  return a.dim == 64;
+}
+template <int DIM>
+hipError_t footprint_paged(uint32_t *lds_bytes, uint32_t *waves, uint32_t *regs_per_lane) {
+  hipFuncAttributes attr;
+  hipError_t e = hipFuncGetAttributes(&attr, (const void *)attn_paged_partial<DIM>);
+  if (e != hipSuccess) return e;
+  *lds_bytes = (uint32_t)attr.sharedSizeBytes;
+  *waves = 4;
+  *regs_per_lane = ((uint32_t)attr.numRegs + 7u) & ~7u;
+  return hipSuccess;
+}
+CallSizes rope_sizes(const void *args) {
+  tally_rope_args a;
+  memcpy(&a, args, sizeof(a));
+  return {a.heads, a.dim, a.rot, a.flags & TALLY_ROPE_INTERLEAVED};
+}
+CallSizes append_sizes(const void *args) {
+  tally_kv_append_args a;
+  memcpy(&a, args, sizeof(a));
+  return {a.n_seqs, a.kv_heads, a.dim, a.page};
+}
 hipError_t launch_native_prefix(hipStream_t s, const void *args, tally_dim3, uint32_t how) {
   return launch_attn_prefix(s, args, how & kUrgent);
 }
@@ -787,9 +878,16 @@ const KernelOps kOps[TALLY_K_COUNT] = {
     {"gemv_w4_bf16", sizeof(tally_gemv_w4_args), true, grid_gemv_w4, launch_native_w4, launch_sliced_w4, launch_ptb_w4,
      nullptr, occupancy_w4, pause_fraction_t<GemvW4T<1, 1>>, footprint_w4, {W4_ALL(W4_FOOT)},
      w4_choice, w4_range, nullptr, nullptr, nullptr, false, false, w4_sizes},
+    {"rope_bf16", sizeof(tally_rope_args), true, grid_rope, launch_native_t<RopeBody>, launch_sliced_t<RopeBody>,
+     launch_ptb_t<RopeBody>, init_t<RopeBody>, occupancy_t<RopeBody>, pause_fraction_t<RopeBody>, footprint_t<RopeBody>,
+     {footprint_native_t<RopeBody>}, nullptr, nullptr, nullptr, nullptr, nullptr, false, false, rope_sizes},
+    OPS_DIM(AppendBody, AppendNarrowBody, "kv_append_fp8", grid_append, append_sizes),
+    {"attn_paged_fp8", sizeof(tally_attn_paged_args), false, grid_paged, launch_native_paged,
+     nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, {footprint_paged<128>, footprint_paged<64>},
+     paged_choice, nullptr, nullptr, nullptr, nullptr, false, false},
 };
 
-constexpr size_t kMaxArgs = 128;
+constexpr size_t kMaxArgs = 144;
 constexpr int kSlots = 64;
 constexpr int kMaxShunned = 64;
 constexpr int kMaxSide = 2 * 8 + 2;
@@ -1528,6 +1626,12 @@ size_t tally_attn_prefix_scratch_bytes(uint32_t batch, uint32_t heads, uint32_t 
                                        uint32_t own_cap) {
   return prefix_sizes_ok(batch, heads, kv_heads, dim, prefix, own_cap)
              ? prefix_scratch_bytes(batch, heads, kv_heads, dim, prefix, own_cap) : 0;
+}
+
+size_t tally_attn_paged_scratch_bytes(uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t dim, uint32_t page,
+                                      uint32_t seq_pages) {
+  return paged_sizes_ok(batch, heads, kv_heads, dim, page, seq_pages)
+             ? paged_scratch_bytes(batch, heads, kv_heads, dim, page, seq_pages) : 0;
 }
 
 int tally_launch_native(tally_ctx *ctx, const tally_kernel_desc *desc, int on_hi_stream) {
