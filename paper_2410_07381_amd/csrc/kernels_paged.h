@@ -24,58 +24,79 @@ namespace tally {
 constexpr uint32_t kUnit = 16;                             // tokens side by side in V's pages
 
 // ---- appending ---------------------------------------------------------------------------
-// K/V heads of a logical block: four waves with a unit of a head each.
-__host__ __device__ inline uint32_t append_heads(uint32_t page) { return page >= 64 ? 1 : 64 / page; }
+// A wave's piece of work is 1024 numbers of K and as many of V: 8 tokens of a head of 128, 16 of one of 64.
+//
+// Packed prompts (append_waves): a wave takes such a piece of a page and one K/V head after the other, since the sines and
+// cosines of its tokens are more work than all else on a head's keys.  A workgroup has all pieces of a page, which share their
+// largest magnitudes through LDS, or of several small pages.
+//
+// Calls with hardly more than a token a sequence (kAppendFew): a wave takes a page, and of it the pieces that have new tokens, twice
+// where they are several: mostly it is one, and waves for the others would be in its way.
+constexpr uint32_t kAppendFew = 4;                         // tokens a sequence
+constexpr uint64_t kAppendPieces = 4096;                   // for the waves, at least
+__host__ __device__ constexpr uint32_t append_tokens(uint32_t dim) { return 1024 / dim; }   // of a piece
+__host__ __device__ inline bool append_few(const tally_kv_append_args &a) { return a.total < kAppendFew * (uint64_t)a.n_seqs; }
+// waves of a workgroup, and slots (pages) that it has
+__host__ __device__ inline uint32_t append_waves(const tally_kv_append_args &a) {
+  const uint32_t pieces = a.page / append_tokens(a.dim);
+  return append_few(a) || pieces < 4 ? 4 : pieces;
+}
+__host__ __device__ inline uint32_t append_pages(const tally_kv_append_args &a) {
+  return append_few(a) ? 4 : append_waves(a) * append_tokens(a.dim) / a.page;
+}
+inline uint64_t append_slots(const tally_kv_append_args &a) { return (uint64_t)a.total / a.page + 2ull * a.n_seqs; }
+// K/V heads that a logical block goes through: as many as leave so many pieces for the waves.
+__host__ __device__ inline uint32_t append_heads(const tally_kv_append_args &a) {
+  const uint64_t pieces = (uint64_t)a.total / append_tokens(a.dim) * a.kv_heads;
+  uint32_t h = 1;
+  while (!append_few(a) && 2 * h <= a.kv_heads && 2 * h <= 8 && pieces / (2 * h) >= kAppendPieces) h *= 2;
+  return h;
+}
 inline uint64_t append_blocks(const tally_kv_append_args &a) {
-  const uint32_t h = append_heads(a.page);
-  return (uint64_t)((a.kv_heads + h - 1) / h) * ((uint64_t)a.total / a.page + 2ull * a.n_seqs);
+  const uint32_t h = append_heads(a), pages = append_pages(a);
+  return (uint64_t)((a.kv_heads + h - 1) / h) * ((append_slots(a) + pages - 1) / pages);
 }
 
 #ifdef __HIP_DEVICE_COMPILE__
-// Exponent of a block by the largest of its magnitudes' bits in fp32: the smallest e from 1 on with
-// m <= 448 x 2^(e - 127).  448 is 1.75 x 2^8, so a mantissa over 1.75 carries into the exponent.
+// Exponent of a block by the bits of the largest of its magnitudes: the smallest e from 1 on with m <= 448 x 2^(e - 127).  448 is
+// 1.75 x 2^8, so a mantissa over 1.75 carries into the exponent.
 __device__ __forceinline__ int block_exp(uint32_t top) {
   const int e = (int)((top + 0x1FFFFFu) >> 23) - 8;
   return e < 1 ? 1 : e > 254 ? 254 : e;
-}
-__device__ __forceinline__ uint32_t magnitude_bits(float x) {   // (none of what is no number)
-  const uint32_t b = __float_as_uint(x) & 0x7FFFFFFFu;
-  return b < 0x7F800000u ? b : 0u;
 }
 // fp64 to fp32 such that rounding the result to fewer than 20 bits is rounding the number itself: cut after 20
 // bits, the last of them set where anything was cut off.
 __device__ __forceinline__ float cut(double x) {
   const uint64_t b = __builtin_bit_cast(uint64_t, x);
-  const uint32_t hi = (uint32_t)(b >> 32) | ((uint32_t)b != 0u ? 1u : 0u);
-  return (float)__builtin_bit_cast(double, (uint64_t)hi << 32);
+  uint32_t any;                                            // (written out: as an expression it is a comparison and a choice)
+  asm("v_min_u32 %0, 1, %1" : "=v"(any) : "v"((uint32_t)b));
+  return (float)__builtin_bit_cast(double, (uint64_t)((uint32_t)(b >> 32) | any) << 32);
 }
-// Four numbers times 2^by to codes.  (fma with 0: infinities become NaN, numbers stay.)
-__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, int by) {
-  auto f = [&](float x) { return __builtin_ldexpf(__builtin_fmaf(x, 0.f, x), by); };
-  const int w = __builtin_amdgcn_cvt_pk_fp8_f32(f(a), f(b), 0, false);
-  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(f(c), f(d), w, true);
+// 2^by for by from -127 on, 0 below.
+__device__ __forceinline__ float power_of_two(int by) {
+  return __uint_as_float(by >= -126 ? (uint32_t)(by + 127) << 23 : by == -127 ? 0x400000u : 0u);
 }
-__device__ __forceinline__ uint32_t shift_codes(uint32_t w, int by) {
+// Four numbers times a power of two to codes.
+__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d, float by) {
+  const int w = __builtin_amdgcn_cvt_pk_fp8_f32(a * by, b * by, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c * by, d * by, w, true);
+}
+__device__ __forceinline__ uint32_t shift_codes(uint32_t w, float by) {
   const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
   return codes4(lo[0], lo[1], hi[0], hi[1], by);
 }
-__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
-#pragma unroll
-  for (int by = 32; by; by >>= 1) {
-    const uint32_t w = (uint32_t)__shfl_xor((int)v, by);
-    v = v > w ? v : w;
-  }
-  return v;
-}
+typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t same(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
 #endif
 
-template <int DIM>
+// WAVES of a workgroup; FEW: a page a wave.
+template <int DIM, int WAVES, bool FEW>
 struct AppendBodyT {
   using Args = tally_kv_append_args;
-  static constexpr int THREADS = kThreads;
-  static constexpr int MIN_WAVES = 2;
-  static constexpr unsigned DYN_LDS = 0;
-  static constexpr bool END_BARRIER = true;                // (the waves' largest magnitudes)
+  static constexpr int THREADS = 64 * WAVES;
+  static constexpr int MIN_WAVES = WAVES == 16 ? 4 : 3;
+  static constexpr unsigned DYN_LDS = FEW ? 0 : WAVES * 8192;   // (a wave's sines and cosines)
+  static constexpr bool END_BARRIER = !FEW;                // (the waves' largest magnitudes)
   static constexpr bool YIELDS = false;
   static constexpr bool RANGE = false;
   static __device__ __forceinline__ void run(const Args &a, uint32_t bx, uint32_t, uint32_t) { append<false>(a, bx); }
@@ -85,200 +106,298 @@ struct AppendBodyT {
   static __device__ __forceinline__ void append(const Args &a, uint32_t block) {
 #ifdef __HIP_DEVICE_COMPILE__
     typedef uint32_t u32x2_nt __attribute__((ext_vector_type(2)));
-    constexpr uint32_t PIECES = DIM / 16, ROUNDS = 16 * PIECES / 64;   // pieces of 16 numbers of a token; rounds of a unit
-    constexpr uint32_t SIDE = DIM / 2;                       // lanes of V side by side, two dims each
-    constexpr int VT = DIM / 8;                              // tokens of such a lane
-    constexpr int MORE = 2;                                  // units of a wave, at most
-    __shared__ uint32_t s_top[2][4];
-    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t P = a.page, heads = append_heads(P), groups = (a.kv_heads + heads - 1) / heads;
-    const uint32_t slot = block / groups, per_head = P >= 64 ? 4u : P / kUnit, units = P / kUnit;
-    const uint32_t head = block % groups * heads + wave / per_head, unit0 = wave % per_head;
-    // the sequence of this slot: the last one that starts at or before it, 63 candidates at a time; the lane behind
-    // the last candidate has where that one ends
+    constexpr uint32_t TOK = append_tokens(DIM), PIECES = DIM / 16;   // tokens of a wave's piece of work; 16 numbers of a token a lane
+    // Of V a lane has eight tokens of two dims: the whole unit of 16 tokens and 64 dims, so that two lanes make up a dim's 16 bytes.  (Few
+    // tokens, of heads of 128: the same eight as of K and all dims; the unit's other half need not be gone through.)
+    constexpr bool WHOLE = !FEW || DIM == 64;
+    constexpr uint32_t SIDE = WHOLE ? 32 : 64;               // lanes side by side
+    constexpr int AUX = NT ? 2 : 0;
+    const uint32_t lane = threadIdx.x & 63, wave = same(threadIdx.x >> 6);
+    const uint32_t shift = (uint32_t)__builtin_ctz(a.page), P = a.page;
+    const uint32_t HN = FEW ? 1 : append_heads(a), groups = (a.kv_heads + HN - 1) / HN;
+    const uint32_t per_page = FEW ? 1 : P / TOK, h0 = block % groups * HN;
+    const uint32_t slot = block / groups * (WAVES / per_page) + wave / per_page;
+    // The sequence of this slot: the last one that starts at or before it, 63 candidates at a time; the lane behind the last
+    // candidate has where that one ends.
     uint32_t seq = 0, first, last;
+    int32_t said;
     for (uint32_t n = a.n_seqs;;) {
       const uint32_t step = (n + 62) / 63, s = lane * step < n ? lane * step : n;
-      const int32_t v = a.cu_seqlens[seq + s];
+      const int32_t v = a.cu_seqlens[seq + s], w = a.lens[seq + (s < n ? s : n - 1)];
       const uint32_t edge = v < 0 ? 0u : (uint32_t)v < a.total ? (uint32_t)v : a.total;
-      const bool ok = s < n && edge / P + 2 * (seq + s) <= slot;
+      const bool ok = s < n && (edge >> shift) + 2 * (seq + s) <= slot;
       const uint32_t c = (uint32_t)__popcll(__builtin_amdgcn_ballot_w64(ok)), i = c ? c - 1 : 0;
       seq += i * step;
       if (step == 1) {
         first = (uint32_t)__builtin_amdgcn_readlane((int)edge, (int)i);
         last = (uint32_t)__builtin_amdgcn_readlane((int)edge, (int)i + 1);
+        said = __builtin_amdgcn_readlane(w, (int)i);
         break;
       }
       n = n - i * step < step ? n - i * step : step;
     }
     const int32_t count = last > first ? (int32_t)(last - first) : 0;
-    const int32_t said = a.lens[seq], len = said < 0 ? 0 : said < (1 << 30) ? said : 1 << 30;
+    const int32_t len = said < 0 ? 0 : said < (1 << 30) ? said : 1 << 30;
     const int32_t begin = len - count, cap = (int32_t)(a.seq_pages * P);   // (place of the first new token)
     const int32_t lo = begin > 0 ? begin : 0, hi = len < cap ? len : cap;
-    const uint32_t nth = slot - (first / P + 2 * seq);
-    // (all of it the same for the whole workgroup; slots before the first sequence wrap)
-    if (hi <= lo || nth > (uint32_t)(hi - 1) / P - (uint32_t)lo / P) return;
-    const uint32_t at = (uint32_t)lo / P + nth;
-    const int32_t id = a.table[(uint64_t)seq * (a.ld_table ? a.ld_table : a.seq_pages) + at];
-    if (id < 0 || (uint32_t)id >= a.n_pages) return;
-    // new tokens of the page: [from, to)
-    const int32_t base = (int32_t)(at * P);
+    const uint32_t nth = slot - ((first >> shift) + 2 * seq);
+    // (slots before the first sequence wrap)
+    bool there = hi > lo && nth <= ((uint32_t)(hi - 1) >> shift) - ((uint32_t)lo >> shift);
+    if (FEW && !there) return;
+    const uint32_t at = there ? ((uint32_t)lo >> shift) + nth : 0u;
+    const int32_t base = (int32_t)(at << shift);
+    // new tokens of the page: [from, to); the first of them is row `row` of k and v
     const uint32_t from = (uint32_t)(lo > base ? lo - base : 0), to = hi - base < (int32_t)P ? (uint32_t)(hi - base) : P;
-    const uint32_t row0 = first + (uint32_t)(base - begin);   // row of the page's place 0 (wraps where that is an old one)
-    const bool mine = head < a.kv_heads;
-    const uint64_t block_at = (uint64_t)(uint32_t)id * a.kv_heads + (mine ? head : 0);
-    uint8_t *kp = a.k_pages + block_at * P * DIM, *vp = a.v_pages + block_at * P * DIM;
-    int old_k = 0, old_v = 0;
-    if (from != 0) { old_k = a.k_exps[block_at]; old_v = a.v_exps[block_at]; }
+    const uint32_t row = there ? first + (uint32_t)(base + (int32_t)from - begin) : 0u;
+    int32_t id = 0;
+    if (there) {
+      id = (int32_t)same((uint32_t)a.table[(uint64_t)seq * (a.ld_table ? a.ld_table : a.seq_pages) + at]);
+      there = id >= 0 && (uint32_t)id < a.n_pages;
+    }
+    if (FEW && !there) return;
     const uint32_t LDK = a.ld_k ? a.ld_k : a.kv_heads * DIM, LDV = a.ld_v ? a.ld_v : a.kv_heads * DIM;
     const uint32_t turned = a.rot / 16, half = a.rot / 2;
     const bool split = !(a.flags & TALLY_ROPE_INTERLEAVED);
-    const double by = a.magnitude > 0.f ? (double)a.magnitude : 1.0;
-    const uint32_t piece = lane % PIECES;
+    const uint32_t piece = lane % PIECES, tok = lane / PIECES;
     const bool turns = piece < turned, apart = turns && split;
-    const uint32_t one = piece * (apart ? 8 : 16), two = one + (apart ? half : 8);   // dims of the piece's halves
+    const uint32_t one = piece * (apart ? 8 : 16), two = one + (apart ? half : 8);   // dims of the lane's two eights
+    auto v_first = [&](uint32_t u0) { return (WHOLE ? u0 / kUnit * kUnit : u0) + lane / SIDE * 8; };
+    auto v_dim = [&](uint32_t u0) { return (WHOLE && DIM == 128 ? u0 % kUnit * 8 : 0u) + lane % SIDE * 2; };
 
-    float k[MORE][ROUNDS][16];
-    uint32_t v[MORE][VT];
-    uint32_t top_k = 0, top_v = 0;
+    // Sines and cosines of the lane's pairs, of tokens u0 .. u0 + TOK - 1 of the page.
+    extern __shared__ __align__(1024) unsigned char tally_dyn_lds[];
+    Turn z[8], *table = reinterpret_cast<Turn *>(tally_dyn_lds) + (FEW ? 0 : wave * (TOK * DIM / 2));
+    auto make_turns = [&](uint32_t u0) {
+      const double by = a.magnitude > 0.f ? (double)a.magnitude : 1.0;
+      if constexpr (FEW) {
+        const uint32_t t = u0 + tok;
+        int32_t position = base + (int32_t)t;
+        if (a.positions) position = t >= from && t < to ? a.positions[row + (t - from)] : 0;
+        float f[8];
 #pragma unroll
-    for (int m = 0; m < MORE; ++m) {
-      const uint32_t unit = unit0 + m * 4;
-      const bool live = mine && unit < units && unit * kUnit < to && unit * kUnit + kUnit > from;
-      if (!live) continue;
+        for (int e = 0; e < 8; ++e) f[e] = a.freqs[turns ? piece * 8 + e : 0];
 #pragma unroll
-      for (uint32_t r = 0; r < ROUNDS; ++r) {
-        const uint32_t t = unit * kUnit + r * (64 / PIECES) + lane / PIECES;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) k[m][r][e] = 0.f;
-        if (t < from || t >= to) continue;
-        const uint32_t row = row0 + t;
-        const uint16_t *x = a.k + (uint64_t)row * LDK + head * DIM;
-        const u32x4_nt u = RopeBody::load<NT>(x + one), w = RopeBody::load<NT>(x + two);
-        float (&o)[16] = k[m][r];                          // (o[e] and o[8 + e]: a pair)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float u0 = bf16_lo(u[e]), u1 = bf16_hi(u[e]), w0 = bf16_lo(w[e]), w1 = bf16_hi(w[e]);
-          if (split) o[2 * e] = u0, o[2 * e + 1] = u1, o[8 + 2 * e] = w0, o[9 + 2 * e] = w1;
-          else o[e] = u0, o[8 + e] = u1, o[4 + e] = w0, o[12 + e] = w1;
+        for (int e = 0; e < 8; ++e) {
+          z[e] = turn_of(position, f[e]);
+          z[e].c *= by, z[e].s *= by;
         }
-        if (turns) {
-          const int32_t position = a.positions ? a.positions[row] : base + (int32_t)t;
+      } else {
+        // A lane makes those of one pair and eight neighbours: where positions are neighbours too the first, and the others by turning
+        // on and on by the frequency.  They stay in LDS, a piece's pairs side by side for lanes that are.
+        const uint32_t pair = lane % PIECES * 8 + lane / PIECES % 8, t0 = u0 + lane / (DIM / 2) * 8;
+        const float f = a.freqs[pair < half ? pair : 0];
+        Turn w = turn_of(base + (int32_t)t0, f);
+        const Turn on = turn_of(1, f);
+        w.c *= by, w.s *= by;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const Turn z = turn_of(position, a.freqs[piece * 8 + e]);
-            const double c = z.c * by, s = z.s * by, p0 = (double)o[e], q0 = (double)o[8 + e];
-            o[e] = cut(__builtin_fma(p0, c, -(q0 * s)));
-            o[8 + e] = cut(__builtin_fma(q0, c, p0 * s));
+        for (uint32_t j = 0; j < 8; ++j) {
+          if (a.positions) {
+            const uint32_t t = t0 + j;
+            w = turn_of(t >= from && t < to ? a.positions[row + (t - from)] : 0, f);
+            w.c *= by, w.s *= by;
           }
-        }
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const uint32_t b = magnitude_bits(o[e]);
-          top_k = top_k > b ? top_k : b;
+          table[(t0 - u0 + j) * (DIM / 2) + lane % (DIM / 2)] = w;
+          w = Turn{__builtin_fma(w.c, on.c, -(w.s * on.s)), __builtin_fma(w.s, on.c, w.c * on.s)};
         }
       }
-      const uint32_t t0 = unit * kUnit + lane / SIDE * VT;
+    };
+    float k[16];                                           // (k[e] and k[8 + e]: a pair)
+    uint32_t v[8];
+    uint4 x, y;
+    // New numbers of tokens u0 .. u0 + TOK - 1 of the page, and of V's part, are asked for; zeros for other tokens.
+    auto ask = [&](uint32_t u0, uint32_t head) {
+      const buf_t kb = make_buf(a.k + (uint64_t)row * LDK + head * DIM, ((to - from - 1) * LDK + DIM) * 2);
+      const buf_t vb = make_buf(a.v + (uint64_t)row * LDV + head * DIM, ((to - from - 1) * LDV + DIM) * 2);
+      const uint32_t t = (u0 + tok - from) * LDK;
+      x = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(kb, (t + one) * 2, 0, AUX));
+      y = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(kb, (t + two) * 2, 0, AUX));
+      const uint32_t tv = v_first(u0) - from, col = v_dim(u0);
 #pragma unroll
-      for (int i = 0; i < VT; ++i) {
-        v[m][i] = 0;
-        if (t0 + i < from || t0 + i >= to) continue;
-        v[m][i] = *reinterpret_cast<const uint32_t *>(a.v + (uint64_t)(row0 + t0 + i) * LDV + head * DIM + lane % SIDE * 2);
-        const uint32_t b = magnitude_bits(bf16_lo(v[m][i])), d = magnitude_bits(bf16_hi(v[m][i]));
-        top_v = top_v > b ? top_v : b;
-        top_v = top_v > d ? top_v : d;
+      for (int j = 0; j < 8; ++j) v[j] = __builtin_amdgcn_raw_buffer_load_b32(vb, ((tv + j) * LDV + col) * 2, 0, AUX);
+    };
+    // What was asked for, keys turned.
+    auto take = [&] {
+      // pairs that are neighbours come apart: words of first ones and of second ones
+      const uint32_t u[4] = {x.x, x.y, x.z, x.w}, w[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t c = e < 2 ? u[2 * e] : w[2 * e - 4], d = e < 2 ? u[2 * e + 1] : w[2 * e - 3];
+        const uint32_t p = split ? u[e] : __builtin_amdgcn_perm(d, c, 0x05040100u), q = split ? w[e] : __builtin_amdgcn_perm(d, c, 0x07060302u);
+        k[2 * e] = bf16_lo(p), k[2 * e + 1] = bf16_hi(p);
+        k[8 + 2 * e] = bf16_lo(q), k[9 + 2 * e] = bf16_hi(q);
       }
-    }
-    top_k = wave_max_u32(top_k);
-    top_v = wave_max_u32(top_v);
-    if (lane == 0) s_top[0][wave] = top_k, s_top[1][wave] = top_v;
-    __syncthreads();
-    const uint32_t w0 = wave / per_head * per_head;
-    for (uint32_t i = 0; i < per_head; ++i) {
-      top_k = top_k > s_top[0][w0 + i] ? top_k : s_top[0][w0 + i];
-      top_v = top_v > s_top[1][w0 + i] ? top_v : s_top[1][w0 + i];
-    }
-    if (!mine) return;                                     // (no barrier behind it)
-    int ek = block_exp(top_k), ev = block_exp(top_v);
-    if (from != 0) {
-      ek = ek > old_k ? ek : old_k;
-      ev = ev > old_v ? ev : old_v;
-    }
-    if (unit0 == 0 && lane == 0) {
-      a.k_exps[block_at] = (uint8_t)ek;
-      a.v_exps[block_at] = (uint8_t)ev;
-    }
+      if (turns) {
 #pragma unroll
-    for (int m = 0; m < MORE; ++m) {
-      const uint32_t unit = unit0 + m * 4, first_token = unit * kUnit;
-      if (unit >= units || first_token >= to) continue;
-      const bool live = first_token + kUnit > from;
+        for (int e = 0; e < 8 && !FEW; ++e) z[e] = table[tok * (DIM / 2) + e * PIECES + piece];
 #pragma unroll
-      for (uint32_t r = 0; r < ROUNDS; ++r) {
-        const uint32_t t = first_token + r * (64 / PIECES) + lane / PIECES;
-        uint8_t *row = kp + t * DIM;
-        if (live && t >= from && t < to) {
-          const float (&o)[16] = k[m][r];
-          u32x2_nt u, w;
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            if (split) {
-              u[e] = codes4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3], 127 - ek);
-              w[e] = codes4(o[8 + 4 * e], o[9 + 4 * e], o[10 + 4 * e], o[11 + 4 * e], 127 - ek);
-            } else {
-              u[e] = codes4(o[2 * e], o[8 + 2 * e], o[2 * e + 1], o[9 + 2 * e], 127 - ek);
-              w[e] = codes4(o[4 + 2 * e], o[12 + 2 * e], o[5 + 2 * e], o[13 + 2 * e], 127 - ek);
-            }
-          }
-          *reinterpret_cast<u32x2_nt *>(row + one) = u;
-          *reinterpret_cast<u32x2_nt *>(row + two) = w;
-        } else if (t < from && ek != old_k) {
-          u32x2_nt u = *reinterpret_cast<u32x2_nt *>(row + one), w = *reinterpret_cast<u32x2_nt *>(row + two);
-#pragma unroll
-          for (int e = 0; e < 2; ++e) u[e] = shift_codes(u[e], old_k - ek), w[e] = shift_codes(w[e], old_k - ek);
-          *reinterpret_cast<u32x2_nt *>(row + one) = u;
-          *reinterpret_cast<u32x2_nt *>(row + two) = w;
+        for (int e = 0; e < 8; ++e) {
+          const double p0 = (double)k[e], q0 = (double)k[8 + e];
+          k[e] = cut(__builtin_fma(p0, z[e].c, -(q0 * z[e].s)));
+          k[8 + e] = cut(__builtin_fma(q0, z[e].c, p0 * z[e].s));
         }
       }
-      // V: VT tokens of two dims; a unit that is not all new is put together with what is there
-      if (!live && ev == old_v) continue;
-      const uint32_t t0 = first_token + lane / SIDE * VT;
-      uint8_t *col = vp + first_token * DIM + lane % SIDE * 32 + lane / SIDE * VT;
-      const bool whole = first_token >= from && first_token + kUnit <= to;
+    };
+    // A lane's largest magnitudes so far: K's, and of V's bits two side by side.  (K's maxima leave NaN out; infinities, and what of
+    // V is no number, have to be left out by name, where there are any.)
+    float mk = 0.f;
+    u16x2_t mv = {0, 0};
+    auto tops = [&] {
+      const float mk0 = mk;
+      const u16x2_t mv0 = mv;
 #pragma unroll
-      for (int d = 0; d < 2; ++d) {
-        uint32_t w[VT / 4];
+      for (int e = 0; e < 8; ++e) mk = fmaxf(mk, fmaxf(__builtin_fabsf(k[2 * e]), __builtin_fabsf(k[2 * e + 1])));
 #pragma unroll
-        for (int i = 0; i < VT / 4; ++i) w[i] = 0;
-        if (!whole)
+      for (int j = 0; j < 8; ++j) mv = __builtin_elementwise_max(mv, __builtin_bit_cast(u16x2_t, v[j] & 0x7FFF7FFFu));
+      if (__builtin_amdgcn_ballot_w64(mk == INFINITY || mv[0] >= 0x7F80 || mv[1] >= 0x7F80)) {
+        mk = mk0, mv = mv0;
 #pragma unroll
-          for (int i = 0; i < VT / 4; ++i) w[i] = *reinterpret_cast<const uint32_t *>(col + d * 16 + 4 * i);
+        for (int e = 0; e < 16; ++e) mk = fmaxf(mk, __builtin_fabsf(k[e]) < INFINITY ? __builtin_fabsf(k[e]) : 0.f);
 #pragma unroll
-        for (int i = 0; i < VT / 4; ++i) {
-          uint32_t is_new = 0, before = 0;
-#pragma unroll
-          for (uint32_t j = 0; j < 4; ++j) {
-            const uint32_t t = t0 + 4 * i + j;
-            is_new |= t >= from && t < to ? 0xFFu << (8 * j) : 0u;
-            before |= t < from ? 0xFFu << (8 * j) : 0u;
-          }
-          uint32_t c = 0;
-          if (live) {
-            auto number = [&](int j) { return d ? bf16_hi(v[m][4 * i + j]) : bf16_lo(v[m][4 * i + j]); };
-            c = codes4(number(0), number(1), number(2), number(3), 127 - ev);
-          }
-          if (ev != old_v) w[i] = (w[i] & ~before) | (shift_codes(w[i], old_v - ev) & before);
-          w[i] = (w[i] & ~is_new) | (c & is_new);
+        for (int j = 0; j < 8; ++j) {
+          u16x2_t w = __builtin_bit_cast(u16x2_t, v[j] & 0x7FFF7FFFu);
+          w[0] = w[0] < 0x7F80 ? w[0] : 0, w[1] = w[1] < 0x7F80 ? w[1] : 0;
+          mv = __builtin_elementwise_max(mv, w);
         }
-        if constexpr (VT == 16) *reinterpret_cast<u32x4_nt *>(col + d * 16) = u32x4_nt{w[0], w[1], w[2], w[3]};
-        else *reinterpret_cast<u32x2_nt *>(col + d * 16) = u32x2_nt{w[0], w[1]};
+      }
+    };
+    // Over the wave: K's for the lower lanes, V's for the upper ones.
+    auto over_wave = [&] {
+      float p = mk, q = __uint_as_float((uint32_t)(mv[0] > mv[1] ? mv[0] : mv[1]) << 16);
+      asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(p), "+v"(q));
+      p = q = fmaxf(p, q);
+      asm("s_nop 1\n\tv_permlane16_swap_b32 %0, %1" : "+v"(p), "+v"(q));
+      return row16_all<MaxOp>(fmaxf(p, q));
+    };
+    // What a block's exponents become, and what was loaded, or what was there, to its codes.
+    struct Block { uint8_t *kp, *vp; int old_k, old_v, ek, ev; };
+    auto block_of = [&](uint32_t head, uint64_t &index) {
+      index = (uint64_t)(uint32_t)id * a.kv_heads + head;
+      Block w{a.k_pages + (index << shift) * DIM, a.v_pages + (index << shift) * DIM, 0, 0, 0, 0};
+      if (from != 0) w.old_k = a.k_exps[index], w.old_v = a.v_exps[index];
+      return w;
+    };
+    auto grow = [&](Block &w, uint64_t index, float top, bool write) {
+      w.ek = block_exp(__builtin_amdgcn_readlane(__float_as_int(top), 0)), w.ev = block_exp(__builtin_amdgcn_readlane(__float_as_int(top), 32));
+      if (from != 0) {
+        w.ek = w.ek > w.old_k ? w.ek : w.old_k;
+        w.ev = w.ev > w.old_v ? w.ev : w.old_v;
+      }
+      if (write && lane == 0) {
+        a.k_exps[index] = (uint8_t)w.ek;
+        a.v_exps[index] = (uint8_t)w.ev;
+      }
+    };
+    auto store = [&](uint32_t u0, const Block &b, bool live) {
+      const uint32_t t = u0 + tok;
+      uint8_t *to_row = b.kp + t * DIM;
+      if (live && t >= from && t < to) {
+        const float by = power_of_two(127 - b.ek);
+        const uint32_t p0 = codes4(k[0], k[1], k[2], k[3], by), p1 = codes4(k[4], k[5], k[6], k[7], by);
+        const uint32_t q0 = codes4(k[8], k[9], k[10], k[11], by), q1 = codes4(k[12], k[13], k[14], k[15], by);
+        const u32x2_nt u = {split ? p0 : __builtin_amdgcn_perm(q0, p0, 0x05010400u), split ? p1 : __builtin_amdgcn_perm(q0, p0, 0x07030602u)};
+        const u32x2_nt w = {split ? q0 : __builtin_amdgcn_perm(q1, p1, 0x05010400u), split ? q1 : __builtin_amdgcn_perm(q1, p1, 0x07030602u)};
+        *reinterpret_cast<u32x2_nt *>(to_row + one) = u;
+        *reinterpret_cast<u32x2_nt *>(to_row + two) = w;
+      } else if (t < from && b.ek != b.old_k) {
+        const float by = power_of_two(b.old_k - b.ek);
+        u32x2_nt u = *reinterpret_cast<u32x2_nt *>(to_row + one), w = *reinterpret_cast<u32x2_nt *>(to_row + two);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) u[e] = shift_codes(u[e], by), w[e] = shift_codes(w[e], by);
+        *reinterpret_cast<u32x2_nt *>(to_row + one) = u;
+        *reinterpret_cast<u32x2_nt *>(to_row + two) = w;
+      }
+      // V: what is not all new is put together with what is there
+      if (!live && b.ev == b.old_v) return;
+      const uint32_t t0 = v_first(u0), dim = v_dim(u0);
+      uint8_t *unit = b.vp + t0 / kUnit * (kUnit * DIM);
+      uint32_t w[2][2];
+      const float by = power_of_two(127 - b.ev);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        w[0][j] = live ? codes4(bf16_lo(v[4 * j]), bf16_lo(v[4 * j + 1]), bf16_lo(v[4 * j + 2]), bf16_lo(v[4 * j + 3]), by) : 0u;
+        w[1][j] = live ? codes4(bf16_hi(v[4 * j]), bf16_hi(v[4 * j + 1]), bf16_hi(v[4 * j + 2]), bf16_hi(v[4 * j + 3]), by) : 0u;
+      }
+      const uint32_t begins = u0 / kUnit * kUnit;
+      if (begins < from || begins + kUnit > to) {
+        const float v_shift = power_of_two(b.old_v - b.ev);
+        // bytes of the lane's eight tokens below a place
+        auto below = [&](uint32_t place) { return place <= t0 ? 0ull : place >= t0 + 8 ? ~0ull : (1ull << 8 * (place - t0)) - 1; };
+        const uint64_t before = below(from), fresh = live ? below(to) & ~before : 0ull;
+#pragma unroll
+        for (int d = 0; d < 2; ++d) {
+          const u32x2_nt old = *reinterpret_cast<const u32x2_nt *>(unit + (dim + d) * kUnit + t0 % kUnit);
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const uint32_t gone = (uint32_t)(before >> 32 * j), is_new = (uint32_t)(fresh >> 32 * j);
+            uint32_t x = old[j];
+            if (b.ev != b.old_v) x = (x & ~gone) | (shift_codes(x, v_shift) & gone);
+            w[d][j] = (x & ~is_new) | (w[d][j] & is_new);
+          }
+        }
+      }
+      if constexpr (WHOLE) {
+        // (the lower lanes take the first dim of the pair, the upper ones the second, all 16 tokens)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(w[0][j]), "+v"(w[1][j]));
+        *reinterpret_cast<u32x4_nt *>(unit + (dim + lane / SIDE) * kUnit) = u32x4_nt{w[0][0], w[0][1], w[1][0], w[1][1]};
+      } else {
+#pragma unroll
+        for (int d = 0; d < 2; ++d) *reinterpret_cast<u32x2_nt *>(unit + (dim + d) * kUnit + t0 % kUnit) = u32x2_nt{w[d][0], w[d][1]};
+      }
+    };
+
+    if constexpr (FEW) {
+      uint64_t index;
+      Block b = block_of(h0, index);
+      const uint32_t u_first = from / TOK * TOK, u_last = (to - 1) / TOK * TOK;
+      for (uint32_t u0 = u_first; u0 <= u_last; u0 += TOK) {
+        ask(u0, h0);
+        if (a.rot) make_turns(u0);
+        take();
+        tops();
+      }
+      grow(b, index, over_wave(), true);
+      store(u_last, b, true);                              // (loaded last)
+      for (uint32_t u0 = u_first; u0 < u_last; u0 += TOK) {
+        ask(u0, h0);
+        if (a.rot) make_turns(u0);
+        take();
+        store(u0, b, true);
+      }
+      if (b.ek != b.old_k || b.ev != b.old_v)
+        for (uint32_t u0 = 0; u0 < u_first; u0 += TOK) store(u0, b, false);
+    } else {
+      __shared__ float s_top[2][2][WAVES];
+      const uint32_t u0 = wave % per_page * TOK, begins = u0 / kUnit * kUnit;
+      const bool live = there && begins < to && begins + kUnit > from, held = there && begins < from;   // new ones in the unit; old ones
+      if (live) ask(u0, h0);
+      if (live && a.rot) make_turns(u0);
+      for (uint32_t i = 0; i < HN && h0 + i < a.kv_heads; ++i) {   // (the same for the whole workgroup)
+        uint64_t index = 0;
+        Block b{};
+        float top = 0.f;
+        if (live || held) b = block_of(h0 + i, index);
+        if (live) {
+          if (i) ask(u0, h0 + i);
+          take();
+          mk = 0.f, mv = u16x2_t{0, 0};
+          tops();
+          top = over_wave();
+        }
+        if (per_page > 1) {
+          if (lane % 32 == 0) s_top[i & 1][lane / 32][wave] = top;
+          __syncthreads();
+          // (a row of 16 lanes has all of the page's, some of them more than once)
+          top = row16_all<MaxOp>(s_top[i & 1][lane / 32][wave - wave % per_page + lane % per_page]);
+        }
+        if (!live && !held) continue;
+        grow(b, index, top, u0 == 0);
+        store(u0, b, live);
       }
     }
 #endif
   }
 };
-using AppendBody = AppendBodyT<128>;
-using AppendNarrowBody = AppendBodyT<64>;
 
 // ---- single-token attention ----------------------------------------------------------------
 // How a call is cut up.  How long sequences are is known on the device alone, and a batch's lengths may differ by any
@@ -325,9 +444,16 @@ struct PagedPart {
   uint32_t first, parts;                                   // its parts: first, first + 1, ...
   uint32_t strips;                                         // of each of them (the last may have fewer)
 };
-__device__ __forceinline__ uint32_t wave_sum_u32(uint32_t v) {
-#pragma unroll
-  for (int by = 32; by; by >>= 1) v += (uint32_t)__shfl_xor((int)v, by);
+// Sums over the lanes up to each one.  (By DPP operands: within rows of 16, then a row's last lane to the rows behind.)
+__device__ __forceinline__ uint32_t wave_scan_u32(uint32_t v) {
+#define SCAN_STEP(ctrl, rows) v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, ctrl, rows, 0xf, false)
+  SCAN_STEP(0x111, 0xf);
+  SCAN_STEP(0x112, 0xf);
+  SCAN_STEP(0x114, 0xf);
+  SCAN_STEP(0x118, 0xf);
+  SCAN_STEP(0x142, 0xa);
+  SCAN_STEP(0x143, 0xc);
+#undef SCAN_STEP
   return v;
 }
 __device__ __forceinline__ uint32_t paged_len(const tally_attn_paged_args &a, uint32_t seq) {
@@ -339,18 +465,13 @@ __device__ __forceinline__ bool paged_find(const tally_attn_paged_args &a, const
   const uint32_t lane = threadIdx.x & 63;
   uint32_t sum = 0;
   for (uint32_t i = lane; i < a.batch; i += 64) sum += (paged_len(a, i) + kPagedStrip - 1) / kPagedStrip;
-  const uint32_t all = wave_sum_u32(sum), even = (all + p.parts - 1) / p.parts, c = even > p.least ? even : p.least;
+  const uint32_t all = (uint32_t)__builtin_amdgcn_readlane((int)wave_scan_u32(sum), 63), even = (all + p.parts - 1) / p.parts, c = even > p.least ? even : p.least;
   uint32_t before = 0;
   for (uint32_t i0 = 0; i0 < a.batch; i0 += 64) {
     const uint32_t i = i0 + lane, len = i < a.batch ? paged_len(a, i) : 0u;
     const uint32_t strips = (len + kPagedStrip - 1) / kPagedStrip;
     const uint32_t mine = i < a.batch ? (strips ? (strips + c - 1) / c : 1u) : 0u;
-    uint32_t upto = mine;                                  // with those of the lanes before
-#pragma unroll
-    for (int by = 1; by < 64; by <<= 1) {
-      const uint32_t w = (uint32_t)__shfl_up((int)upto, by);
-      if (lane >= (uint32_t)by) upto += w;
-    }
+    const uint32_t upto = wave_scan_u32(mine);             // with those of the lanes before
     const uint64_t hit = __builtin_amdgcn_ballot_w64(of ? i == part : mine != 0 && part < before + upto);
     if (hit) {
       const int l = __builtin_ctzll(hit);
@@ -368,12 +489,15 @@ __device__ __forceinline__ bool paged_find(const tally_attn_paged_args &a, const
 }
 #endif
 
-template <int DIM>
+// SMALL: pages of 16 tokens, so that a tile's two units may lie in different ones.  Otherwise a tile has one page, whose
+// address is the same for all lanes.
+template <int DIM, bool SMALL>
 __global__ __launch_bounds__(256, 4) void attn_paged_partial(tally_attn_paged_args a, PagedPlan p, uint32_t urgent) {
 #ifdef __HIP_DEVICE_COMPILE__
   if (urgent) __builtin_amdgcn_s_setprio(3);
   typedef OnePass<DIM, 16, 32, 3> F;
   constexpr int KH = DIM / 64, DT = DIM / 16;              // 64-byte pieces of a key; blocks of 16 dims
+  constexpr int PAGES = SMALL ? 2 : 1;                     // of a tile
   __shared__ float2 s_ml[4][16];
   __shared__ __align__(16) float s_acc[4][16][DIM / 2];
   const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -385,6 +509,61 @@ __global__ __launch_bounds__(256, 4) void attn_paged_partial(tally_attn_paged_ar
   const uint32_t s0 = (part - mine.first) * mine.strips, n = mine.len;
   const uint32_t end = s0 * kPagedStrip < n ? (n - s0 * kPagedStrip < mine.strips * kPagedStrip ? n : (s0 + mine.strips) * kPagedStrip) : 0u;
   const uint32_t r = lane % 16, quarter = lane / 16, head = kv * p.group + row0 + r, LDQ = a.ld_q ? a.ld_q : a.heads * DIM;
+  const int32_t *table = a.table + (uint64_t)mine.seq * (a.ld_table ? a.ld_table : a.seq_pages);
+  const uint32_t last_page = n ? (n - 1) / a.page : 0u, shift = (uint32_t)__builtin_ctz(a.page);
+
+  // Where a tile lies: its pages (of one that does not exist, page 0), and in them the byte that it begins at.
+  struct Place { uint32_t id[PAGES]; bool there[PAGES]; uint32_t in; };
+  auto place_of = [&](uint32_t t0) {
+    Place w;
+#pragma unroll
+    for (int u = 0; u < PAGES; ++u) {
+      const uint32_t at = (t0 + u * kUnit) >> shift;
+      const int32_t id = table[at < last_page ? at : last_page];
+      w.there[u] = id >= 0 && (uint32_t)id < a.n_pages;
+      w.id[u] = w.there[u] ? (uint32_t)id : 0u;
+    }
+    w.in = (t0 & (a.page - 1)) * DIM;
+    return w;
+  };
+  // A lane's row of K in a tile is token 8 (r / 4) + 4 u + r % 4 for product u, so that it gets the scores of eight neighbours,
+  // 8 quarter + 4 u + i, and of V eight neighbours of each dim.
+  const uint32_t k_lane = ((SMALL ? 0 : r / 8 * kUnit) + r / 4 % 2 * 8 + r % 4) * DIM + quarter * 16;
+  const uint32_t v_lane = (SMALL ? 0 : quarter / 2 * kUnit * DIM) + r * 16 + quarter % 2 * 8;
+  auto block_of = [&](const Place &w, bool second) {       // of the lane
+    const uint64_t one = (uint64_t)w.id[0] * a.kv_heads + kv;
+    if constexpr (!SMALL) return one;
+    const uint64_t two = (uint64_t)w.id[PAGES - 1] * a.kv_heads + kv;
+    return second ? two : one;
+  };
+  uint4 k[2][KH];
+  uint2 v[DT];
+  uint32_t ke, ve;
+  auto ask_keys = [&](const Place &w) {
+    const uint8_t *at = a.k_pages + (block_of(w, r >= 8) << shift) * DIM + w.in + k_lane;
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int h = 0; h < KH; ++h) k[u][h] = *reinterpret_cast<const uint4 *>(at + u * 4 * DIM + h * 64);
+  };
+  auto ask_values = [&](const Place &w) {
+    const uint8_t *at = a.v_pages + (block_of(w, quarter >= 2) << shift) * DIM + w.in + v_lane;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) v[d] = *reinterpret_cast<const uint2 *>(at + d * 256);
+  };
+  auto ask_exps = [&](const Place &w) {
+    const uint64_t block = block_of(w, quarter >= 2);
+    ke = a.k_exps[block];
+    ve = a.v_exps[block];
+  };
+  uint32_t t0 = s0 * kPagedStrip + wave * kPagedTile;
+  Place now = place_of(t0), next = now;
+  if (t0 < end) {
+    ask_exps(now);
+    ask_keys(now);
+    ask_values(now);
+    next = place_of(t0 + 4 * kPagedTile);
+  }
   // q: fragment 2 h + j has dims 64 h + 16 quarter + 8 j and the seven behind
   bf16x8_t q[2 * KH];
 #pragma unroll
@@ -399,45 +578,16 @@ __global__ __launch_bounds__(256, 4) void attn_paged_partial(tally_attn_paged_ar
   float m = kNothing, l = 0.f;
   bool some = false;                                       // a token of this wave's counts
   const float c = (a.scale > 0.f ? a.scale : DIM == 128 ? 0.08838834764831845f : 0.125f) * kLog2e;
-  const int32_t *table = a.table + (uint64_t)mine.seq * (a.ld_table ? a.ld_table : a.seq_pages);
-  const uint32_t last_page = n ? (n - 1) / a.page : 0u;
-  // a lane's row of K in a tile: token 8 (r / 4) + 4 u + r % 4 for product u, so that it gets the scores of eight
-  // neighbours, 8 quarter + 4 u + i, and of V eight neighbours of each dim
-  for (uint32_t t0 = s0 * kPagedStrip + wave * kPagedTile; t0 < end; t0 += 4 * kPagedTile) {
-    // the two units' pages
-    const uint8_t *kb[2], *vb[2];
-    uint32_t ke[2], ve[2];
-    bool there[2];
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const uint32_t t = t0 + u * kUnit, at = t / a.page < last_page ? t / a.page : last_page;
-      const int32_t id = table[at];
-      there[u] = id >= 0 && (uint32_t)id < a.n_pages;
-      const uint64_t block = (uint64_t)(there[u] ? (uint32_t)id : 0u) * a.kv_heads + kv;
-      const uint64_t byte = block * a.page * DIM + t % a.page * DIM;
-      kb[u] = a.k_pages + byte;
-      vb[u] = a.v_pages + byte;
-      ke[u] = a.k_exps[block];
-      ve[u] = a.v_exps[block];
-    }
-    const uint8_t *k_at = (r >= 8 ? kb[1] : kb[0]) + (r / 4 % 2 * 8 + r % 4) * DIM + quarter * 16;
-    const uint8_t *v_at = (quarter >= 2 ? vb[1] : vb[0]) + r * 16 + quarter % 2 * 8;
-    uint4 k[2][KH];
-    uint2 v[DT];
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int h = 0; h < KH; ++h) k[u][h] = *reinterpret_cast<const uint4 *>(k_at + u * 4 * DIM + h * 64);
-#pragma unroll
-    for (int d = 0; d < DT; ++d) v[d] = *reinterpret_cast<const uint2 *>(v_at + d * 256);
-    auto wide = [](uint32_t lo, uint32_t hi, float by) {   // eight codes as bf16, times a power of two
-      uint4 w;
-      w.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, by, false));
-      w.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, by, true));
-      w.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, by, false));
-      w.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, by, true));
-      return __builtin_bit_cast(bf16x8_t, w);
-    };
+  auto wide = [](uint32_t lo, uint32_t hi, float by) {     // eight codes as bf16, times a power of two
+    uint4 w;
+    w.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, by, false));
+    w.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, by, true));
+    w.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, by, false));
+    w.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, by, true));
+    return __builtin_bit_cast(bf16x8_t, w);
+  };
+  for (; t0 < end; t0 += 4 * kPagedTile) {
+    const bool more = t0 + 4 * kPagedTile < end;
     f32x4_t s[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
@@ -448,27 +598,35 @@ __global__ __launch_bounds__(256, 4) void attn_paged_partial(tally_attn_paged_ar
         s[u] = F::mma(wide(k[u][h].z, k[u][h].w, 1.f), q[2 * h + 1], s[u]);
       }
     }
-    const float by = c * __uint_as_float((quarter >= 2 ? ke[1] : ke[0]) << 23), v_by = __uint_as_float((quarter >= 2 ? ve[1] : ve[0]) << 23);
+    const float by = c * __uint_as_float(ke << 23), v_by = __uint_as_float(ve << 23);
+    __builtin_amdgcn_sched_barrier(0);
+    if (more) {                                            // (the registers of this tile's are free)
+      ask_exps(next);
+      ask_keys(next);
+    }
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int u = 0; u < 2; ++u) s[u] *= by;
-    // tokens of the lane's eight that count
-    const uint32_t t = t0 + quarter * 8;
-    const uint32_t count = !(quarter >= 2 ? there[1] : there[0]) || t >= end ? 0u : end - t < 8u ? end - t : 8u;
-    if (t0 + kPagedTile > end || !there[0] || !there[1]) {
+    if (t0 + kPagedTile > end || !now.there[0] || !now.there[PAGES - 1]) {
+      // tokens of the lane's eight that count
+      const uint32_t t = t0 + quarter * 8;
+      const uint32_t count = !(quarter >= 2 ? now.there[PAGES - 1] : now.there[0]) || t >= end ? 0u : end - t < 8u ? end - t : 8u;
 #pragma unroll
       for (uint32_t j = 0; j < 8; ++j)
         if (j >= count) s[j / 4][j % 4] = -INFINITY;
       const uint32_t lo = count >= 4 ? ~0u : (1u << 8 * count) - 1, hi = count >= 8 ? ~0u : count > 4 ? (1u << 8 * (count - 4)) - 1 : 0u;
 #pragma unroll
       for (int d = 0; d < DT; ++d) v[d].x &= lo, v[d].y &= hi;
+      some |= __builtin_amdgcn_ballot_w64(count != 0) != 0;
+    } else {
+      some = true;
     }
-    some |= __builtin_amdgcn_ballot_w64(count != 0) != 0;
     float top = s[0][0];
 #pragma unroll
     for (int j = 1; j < 8; ++j) top = fmaxf(top, s[j / 4][j % 4]);
     top = across_rows<MaxOp>(top);
-    const float now = fmaxf(m, top), fade = F::exp2(m - now);
-    m = now;
+    const float upto = fmaxf(m, top), fade = F::exp2(m - upto);
+    m = upto;
     l *= fade;
     uint32_t w[4];
 #pragma unroll
@@ -482,6 +640,13 @@ __global__ __launch_bounds__(256, 4) void attn_paged_partial(tally_attn_paged_ar
       acc[d] *= fade;
       acc[d] = F::mma(wide(v[d].x, v[d].y, v_by), weights, acc[d]);
     }
+    __builtin_amdgcn_sched_barrier(0);
+    if (more) {
+      ask_values(next);
+      now = next;
+      next = place_of(t0 + 8 * kPagedTile);
+    }
+    __builtin_amdgcn_sched_barrier(0);
   }
   // The four waves' states: each row's maximum and sum first, then the weighted acc, half of the dims at a time.
   l = across_rows<AddOp>(l);
@@ -546,18 +711,40 @@ __global__ __launch_bounds__(256) void attn_paged_merge(tally_attn_paged_args a,
   const uint64_t row = (uint64_t)mine.first * a.heads + head;
   const float2 *ml = reinterpret_cast<const float2 *>(a.scratch) + row;
   const float *rec = static_cast<const float *>(a.scratch) + paged_acc_at((uint64_t)p.slots * a.heads) + row * DIM + lane % LANES * 4;
+  constexpr uint32_t ROUND = 4 * SIDE, U = 4;              // parts at a time
+  const uint32_t first = wave * SIDE + lane / LANES;
+  // (the first round's loads do not wait for the weights)
+  f32x4_t v[U];
+  float2 own[U];
+  auto ask = [&](uint32_t i) {
+#pragma unroll
+    for (uint32_t u = 0; u < U; ++u) {
+      v[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      own[u] = make_float2(kNothing, kNoTokens);
+      if (i + u * ROUND >= mine.parts) continue;
+      v[u] = *reinterpret_cast<const f32x4_t *>(rec + (uint64_t)(i + u * ROUND) * a.heads * DIM);
+      own[u] = ml[(uint64_t)(i + u * ROUND) * a.heads];
+    }
+  };
+  ask(first);
   float top = kNothing;
   for (uint32_t i = lane; i < mine.parts; i += 64) top = fmaxf(top, ml[(uint64_t)i * a.heads].x);
   top = wave_max(top);
   float sum = 0.f;
   bool any = false;
   f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
-  for (uint32_t i = wave * SIDE + lane / LANES; i < mine.parts; i += 4 * SIDE) {
-    const float2 s = ml[(uint64_t)i * a.heads];
-    const float w = __builtin_amdgcn_exp2f(s.x - top);
-    any |= !(s.y < 0.f);
-    sum += s.y < 0.f ? 0.f : s.y * w;
-    acc += *reinterpret_cast<const f32x4_t *>(rec + (uint64_t)i * a.heads * DIM) * w;
+  for (uint32_t i = first;;) {
+#pragma unroll
+    for (uint32_t u = 0; u < U; ++u) {
+      const bool none = own[u].y < 0.f;                    // (a part without tokens has an acc of zeros)
+      const float w = none ? 0.f : __builtin_amdgcn_exp2f(own[u].x - top);
+      any |= !none;
+      sum += none ? 0.f : own[u].y * w;
+      acc += v[u] * w;
+    }
+    i += ROUND * U;
+    if (i - first >= mine.parts) break;                    // (the same for every lane)
+    ask(i);
   }
   if constexpr (SIDE == 4) {
 #pragma unroll
@@ -598,7 +785,7 @@ inline PagedPlan paged_plan(const tally_attn_paged_args &a) { return paged_plan(
 template <int DIM>
 hipError_t launch_paged_dim(hipStream_t s, const tally_attn_paged_args &a, uint32_t urgent) {
   const PagedPlan p = paged_plan(a);
-  const hipError_t e = launch(attn_paged_partial<DIM>, dim3(p.slots * a.kv_heads * p.row_tiles), dim3(256), 0, s, a, p, urgent);
+  const hipError_t e = launch(a.page == 16 ? attn_paged_partial<DIM, true> : attn_paged_partial<DIM, false>, dim3(p.slots * a.kv_heads * p.row_tiles), dim3(256), 0, s, a, p, urgent);
   if (e != hipSuccess || p.single) return e;
   return launch(attn_paged_merge<DIM>, dim3(a.heads * a.batch), dim3(256), 0, s, a, p, urgent);
 }

@@ -627,9 +627,9 @@ int grid_append(const void *p, tally_dim3 *g, tally_dim3 *b) {
   const uint64_t row = (uint64_t)a->kv_heads * a->dim;
   if (!attn_ld_ok(a->ld_k, row) || !attn_ld_ok(a->ld_v, row)) return TALLY_ERR_INVALID_ARG;
   const uint64_t blocks = append_blocks(*a);
-  if (blocks >= (1u << 24)) return TALLY_ERR_INVALID_ARG;
+  if (blocks * append_waves(*a) >= (1u << 26)) return TALLY_ERR_INVALID_ARG;   // (a launch has fewer than 2^32 threads)
   *g = {(uint32_t)blocks, 1, 1};
-  *b = kBlock256;
+  *b = {64 * append_waves(*a), 1, 1};
   return TALLY_OK;
 }
 bool paged_sizes_ok(uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t dim, uint32_t page, uint32_t seq_pages) {
@@ -659,17 +659,69 @@ uint32_t paged_choice(const void *args, uint32_t, uint64_t *groups) {
   memcpy(&a, args, sizeof(a));
   const PagedPlan p = paged_plan(a);
   *groups = (uint64_t)p.slots * a.kv_heads * p.row_tiles;
-  return a.dim == 64;
+  return (a.dim == 64 ? 2 : 0) + (a.page == 16);
 }
-template <int DIM>
+template <int DIM, bool SMALL>
 hipError_t footprint_paged(uint32_t *lds_bytes, uint32_t *waves, uint32_t *regs_per_lane) {
   hipFuncAttributes attr;
-  hipError_t e = hipFuncGetAttributes(&attr, (const void *)attn_paged_partial<DIM>);
+  hipError_t e = hipFuncGetAttributes(&attr, (const void *)attn_paged_partial<DIM, SMALL>);
   if (e != hipSuccess) return e;
   *lds_bytes = (uint32_t)attr.sharedSizeBytes;
   *waves = 4;
   *regs_per_lane = ((uint32_t)attr.numRegs + 7u) & ~7u;
   return hipSuccess;
+}
+// Appending: a kernel for each width of a head and number of waves
+#define APPEND_ALL(X) X(0, AppendBodyT<128, 4, false>) X(1, AppendBodyT<128, 8, false>) X(2, AppendBodyT<128, 16, false>) \
+  X(3, AppendBodyT<128, 4, true>) X(4, AppendBodyT<64, 4, false>) X(5, AppendBodyT<64, 8, false>) X(6, AppendBodyT<64, 4, true>)
+uint32_t append_range(const void *args) {
+  tally_kv_append_args a;
+  memcpy(&a, args, sizeof(a));
+  const uint32_t waves = append_waves(a);
+  return a.dim == 64 ? (append_few(a) ? 6 : waves == 8 ? 5 : 4) : append_few(a) ? 3 : waves == 16 ? 2 : waves == 8 ? 1 : 0;
+}
+uint32_t append_choice(const void *args, uint32_t, uint64_t *) { return append_range(args); }
+hipError_t launch_native_append(hipStream_t s, const void *args, tally_dim3 g, uint32_t how) {
+#define APPEND_CASE(i, ...) case i: return launch_native_t<__VA_ARGS__>(s, args, g, how);
+  switch (append_range(args)) { APPEND_ALL(APPEND_CASE) }
+#undef APPEND_CASE
+  return hipErrorInvalidValue;
+}
+hipError_t launch_sliced_append(hipStream_t s, const void *args, uint32_t nblocks, const SliceCtl &c) {
+#define APPEND_CASE(i, ...) case i: return launch_sliced_t<__VA_ARGS__>(s, args, nblocks, c);
+  switch (append_range(args)) { APPEND_ALL(APPEND_CASE) }
+#undef APPEND_CASE
+  return hipErrorInvalidValue;
+}
+hipError_t launch_ptb_append(hipStream_t s, const void *args, const PtbCtl &c) {
+#define APPEND_CASE(i, ...) case i: return launch_ptb_t<__VA_ARGS__>(s, args, c);
+  switch (append_range(args)) { APPEND_ALL(APPEND_CASE) }
+#undef APPEND_CASE
+  return hipErrorInvalidValue;
+}
+// (the most and the fewest of any variant's, which stand for all of them)
+hipError_t footprint_append(uint32_t *lds_bytes, uint32_t *waves, uint32_t *regs_per_lane) {
+  *lds_bytes = *waves = *regs_per_lane = 0;
+  hipError_t e = hipSuccess;
+  uint32_t f[3];
+#define APPEND_MOST(i, ...)                                                                                \
+  if (e == hipSuccess && (e = footprint_t<__VA_ARGS__>(&f[0], &f[1], &f[2])) == hipSuccess) {              \
+    if (f[0] > *lds_bytes) *lds_bytes = f[0];                                                              \
+    if (f[1] > *waves) *waves = f[1];                                                                      \
+    if (f[2] > *regs_per_lane) *regs_per_lane = f[2];                                                      \
+  }
+  APPEND_ALL(APPEND_MOST)
+#undef APPEND_MOST
+  return e;
+}
+int occupancy_append(int *blocks_per_cu) {
+  int rc = TALLY_OK, n = 0;
+  *blocks_per_cu = 0x7fffffff;
+#define APPEND_LEAST(i, ...)                                                                               \
+  if (rc == TALLY_OK && (rc = occupancy_t<__VA_ARGS__>(&n)) == TALLY_OK && n < *blocks_per_cu) *blocks_per_cu = n;
+  APPEND_ALL(APPEND_LEAST)
+#undef APPEND_LEAST
+  return rc;
 }
 CallSizes rope_sizes(const void *args) {
   tally_rope_args a;
@@ -848,6 +900,7 @@ struct TakesTogether<Body, std::enable_if_t<Body::TOGETHER>> : std::true_type {}
    {footprint_native_t<Wide>, footprint_native_t<Narrow>}, dim_choice<Wide, Narrow>, dim_range<Wide, Narrow>, \
    nullptr, nullptr, nullptr, false, false, sizes}
 
+#define APPEND_FOOT(i, ...) footprint_native_t<__VA_ARGS__>,
 #define W4_FOOT(i, ...) footprint_native_t<__VA_ARGS__>,
 const KernelOps kOps[TALLY_K_COUNT] = {
     OPS(SaxpyBody, "saxpy", grid_saxpy),
@@ -881,9 +934,11 @@ const KernelOps kOps[TALLY_K_COUNT] = {
     {"rope_bf16", sizeof(tally_rope_args), true, grid_rope, launch_native_t<RopeBody>, launch_sliced_t<RopeBody>,
      launch_ptb_t<RopeBody>, init_t<RopeBody>, occupancy_t<RopeBody>, pause_fraction_t<RopeBody>, footprint_t<RopeBody>,
      {footprint_native_t<RopeBody>}, nullptr, nullptr, nullptr, nullptr, nullptr, false, false, rope_sizes},
-    OPS_DIM(AppendBody, AppendNarrowBody, "kv_append_fp8", grid_append, append_sizes),
+    {"kv_append_fp8", sizeof(tally_kv_append_args), true, grid_append, launch_native_append, launch_sliced_append, launch_ptb_append,
+     init_t<AppendBodyT<128, 16, false>>, occupancy_append, pause_fraction_t<AppendBodyT<128, 4, false>>, footprint_append, {APPEND_ALL(APPEND_FOOT)},
+     append_choice, append_range, nullptr, nullptr, nullptr, false, false, append_sizes},
     {"attn_paged_fp8", sizeof(tally_attn_paged_args), false, grid_paged, launch_native_paged,
-     nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, {footprint_paged<128>, footprint_paged<64>},
+     nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, {footprint_paged<128, false>, footprint_paged<128, true>, footprint_paged<64, false>, footprint_paged<64, true>},
      paged_choice, nullptr, nullptr, nullptr, nullptr, false, false},
 };
 
