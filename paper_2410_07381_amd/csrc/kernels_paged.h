@@ -33,7 +33,7 @@ constexpr uint32_t kUnit = 16;                             // tokens side by sid
 // Calls with hardly more than a token a sequence (kAppendFew): a wave takes a page, and of it the pieces that have new tokens, twice
 // where they are several: mostly it is one, and waves for the others would be in its way.
 constexpr uint32_t kAppendFew = 4;                         // tokens a sequence
-constexpr uint64_t kAppendPieces = 4096;                   // for the waves, at least
+constexpr uint64_t kAppendPieces = 8192;                   // from so many on a wave has two heads, from four times as many on four
 __host__ __device__ constexpr uint32_t append_tokens(uint32_t dim) { return 1024 / dim; }   // of a piece
 __host__ __device__ inline bool append_few(const tally_kv_append_args &a) { return a.total < kAppendFew * (uint64_t)a.n_seqs; }
 // waves of a workgroup, and slots (pages) that it has
@@ -45,11 +45,11 @@ __host__ __device__ inline uint32_t append_pages(const tally_kv_append_args &a) 
   return append_few(a) ? 4 : append_waves(a) * append_tokens(a.dim) / a.page;
 }
 inline uint64_t append_slots(const tally_kv_append_args &a) { return (uint64_t)a.total / a.page + 2ull * a.n_seqs; }
-// K/V heads that a logical block goes through: as many as leave so many pieces for the waves.
+// K/V heads that a logical block goes through, one after the other.
 __host__ __device__ inline uint32_t append_heads(const tally_kv_append_args &a) {
   const uint64_t pieces = (uint64_t)a.total / append_tokens(a.dim) * a.kv_heads;
   uint32_t h = 1;
-  while (!append_few(a) && 2 * h <= a.kv_heads && 2 * h <= 8 && pieces / (2 * h) >= kAppendPieces) h *= 2;
+  while (!append_few(a) && h < 4 && 2 * h <= a.kv_heads && pieces >= kAppendPieces * h * h) h *= 2;
   return h;
 }
 inline uint64_t append_blocks(const tally_kv_append_args &a) {
@@ -86,6 +86,7 @@ __device__ __forceinline__ uint32_t shift_codes(uint32_t w, float by) {
   return codes4(lo[0], lo[1], hi[0], hi[1], by);
 }
 typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x2_nt __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ uint32_t same(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
 #endif
 
@@ -105,7 +106,6 @@ struct AppendBodyT {
   template <bool NT>
   static __device__ __forceinline__ void append(const Args &a, uint32_t block) {
 #ifdef __HIP_DEVICE_COMPILE__
-    typedef uint32_t u32x2_nt __attribute__((ext_vector_type(2)));
     constexpr uint32_t TOK = append_tokens(DIM), PIECES = DIM / 16;   // tokens of a wave's piece of work; 16 numbers of a token a lane
     // Of V a lane has eight tokens of two dims: the whole unit of 16 tokens and 64 dims, so that two lanes make up a dim's 16 bytes.  (Few
     // tokens, of heads of 128: the same eight as of K and all dims; the unit's other half need not be gone through.)
@@ -414,8 +414,9 @@ struct PagedPlan {
   uint32_t least, parts;                                   // strips of a part at least; parts over all sequences, beside one more for each
   uint32_t slots;                                          // parts that there may be
   uint32_t single;                                         // no sequence can have two: nothing to merge
+  uint32_t past;                                           // the caches may be larger than what the GPU's caches hold
 };
-inline PagedPlan paged_plan(uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t page, uint32_t seq_pages) {
+inline PagedPlan paged_plan(uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t dim, uint32_t page, uint32_t seq_pages) {
   PagedPlan p;
   p.group = heads / kv_heads;
   p.row_tiles = (p.group + kPagedRows - 1) / kPagedRows;
@@ -426,18 +427,24 @@ inline PagedPlan paged_plan(uint32_t batch, uint32_t heads, uint32_t kv_heads, u
   const uint64_t most = (strips + p.least - 1) / p.least;  // of one sequence
   p.single = most <= 1;
   const uint64_t all = batch * (most ? most : 1);
+  p.past = 2ull * batch * seq_pages * page * kv_heads * dim >= kInfinityCache;
   p.slots = (uint32_t)(all < (uint64_t)p.parts + batch ? all : (uint64_t)p.parts + batch);
   return p;
 }
 // Scratch: (max, sum) of each part's heads, and behind them each one's acc.
 __host__ __device__ inline uint64_t paged_acc_at(uint64_t records) { return (records * 2 + 3) / 4 * 4; }   // in floats
 inline size_t paged_scratch_bytes(uint32_t batch, uint32_t heads, uint32_t kv_heads, uint32_t dim, uint32_t page, uint32_t seq_pages) {
-  const PagedPlan p = paged_plan(batch, heads, kv_heads, page, seq_pages);
+  const PagedPlan p = paged_plan(batch, heads, kv_heads, dim, page, seq_pages);
   const uint64_t n = p.single ? 0 : (uint64_t)p.slots * heads;
   return (size_t)(paged_acc_at(n) + n * dim) * sizeof(float);
 }
 
 #ifdef __HIP_DEVICE_COMPILE__
+template <bool NT, class T>
+__device__ __forceinline__ T past(const T *p) {
+  if constexpr (NT) return __builtin_nontemporal_load(p);
+  else return *p;
+}
 // A sequence's parts, and of them one.
 struct PagedPart {
   uint32_t seq, len;                                       // len: tokens of the sequence
@@ -490,8 +497,8 @@ __device__ __forceinline__ bool paged_find(const tally_attn_paged_args &a, const
 #endif
 
 // SMALL: pages of 16 tokens, so that a tile's two units may lie in different ones.  Otherwise a tile has one page, whose
-// address is the same for all lanes.
-template <int DIM, bool SMALL>
+// address is the same for all lanes.  NT: caches that are larger than what the GPU's caches hold are read past them.
+template <int DIM, bool SMALL, bool NT>
 __global__ __launch_bounds__(256, 4) void attn_paged_partial(tally_attn_paged_args a, PagedPlan p, uint32_t urgent) {
 #ifdef __HIP_DEVICE_COMPILE__
   if (urgent) __builtin_amdgcn_s_setprio(3);
@@ -544,12 +551,12 @@ __global__ __launch_bounds__(256, 4) void attn_paged_partial(tally_attn_paged_ar
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int h = 0; h < KH; ++h) k[u][h] = *reinterpret_cast<const uint4 *>(at + u * 4 * DIM + h * 64);
+      for (int h = 0; h < KH; ++h) k[u][h] = __builtin_bit_cast(uint4, past<NT>(reinterpret_cast<const u32x4_nt *>(at + u * 4 * DIM + h * 64)));
   };
   auto ask_values = [&](const Place &w) {
     const uint8_t *at = a.v_pages + (block_of(w, quarter >= 2) << shift) * DIM + w.in + v_lane;
 #pragma unroll
-    for (int d = 0; d < DT; ++d) v[d] = *reinterpret_cast<const uint2 *>(at + d * 256);
+    for (int d = 0; d < DT; ++d) v[d] = __builtin_bit_cast(uint2, past<NT>(reinterpret_cast<const u32x2_nt *>(at + d * 256)));
   };
   auto ask_exps = [&](const Place &w) {
     const uint64_t block = block_of(w, quarter >= 2);
@@ -780,12 +787,14 @@ __global__ __launch_bounds__(256) void attn_paged_merge(tally_attn_paged_args a,
 #endif
 }
 
-inline PagedPlan paged_plan(const tally_attn_paged_args &a) { return paged_plan(a.batch, a.heads, a.kv_heads, a.page, a.seq_pages); }
+inline PagedPlan paged_plan(const tally_attn_paged_args &a) { return paged_plan(a.batch, a.heads, a.kv_heads, a.dim, a.page, a.seq_pages); }
 
 template <int DIM>
 hipError_t launch_paged_dim(hipStream_t s, const tally_attn_paged_args &a, uint32_t urgent) {
   const PagedPlan p = paged_plan(a);
-  const hipError_t e = launch(a.page == 16 ? attn_paged_partial<DIM, true> : attn_paged_partial<DIM, false>, dim3(p.slots * a.kv_heads * p.row_tiles), dim3(256), 0, s, a, p, urgent);
+  auto kernel = a.page == 16 ? (p.past ? attn_paged_partial<DIM, true, true> : attn_paged_partial<DIM, true, false>)
+                             : (p.past ? attn_paged_partial<DIM, false, true> : attn_paged_partial<DIM, false, false>);
+  const hipError_t e = launch(kernel, dim3(p.slots * a.kv_heads * p.row_tiles), dim3(256), 0, s, a, p, urgent);
   if (e != hipSuccess || p.single) return e;
   return launch(attn_paged_merge<DIM>, dim3(a.heads * a.batch), dim3(256), 0, s, a, p, urgent);
 }

@@ -46,6 +46,7 @@ __device__ __forceinline__ Turn turn_of(int32_t position, float freq) {
   return Turn{(quadrant + 1) & 2 ? -u : u, quadrant & 2 ? -v : v};
 }
 
+constexpr uint64_t kInfinityCache = 256ull << 20;          // bytes
 constexpr uint32_t kRopeTable = 2048;                      // pairs of a workgroup's tokens
 constexpr uint32_t kRopeItems = 1024;                      // pieces of 16 dims that a workgroup should have
 
@@ -64,7 +65,10 @@ struct RopeBody {
   static constexpr bool END_BARRIER = true;                // (the table)
   static constexpr bool YIELDS = false;
   static constexpr bool RANGE = false;
-  static __device__ __forceinline__ void run(const Args &a, uint32_t bx, uint32_t, uint32_t) { turn<false>(a, bx); }
+  static __device__ __forceinline__ void run(const Args &a, uint32_t bx, uint32_t, uint32_t) {
+    if (4ull * a.total * a.heads * a.dim >= kInfinityCache) turn<true>(a, bx);
+    else turn<false>(a, bx);
+  }
   static __device__ __forceinline__ void run_be(const Args &a, uint32_t bx, uint32_t, uint32_t) { turn<true>(a, bx); }
 
   template <bool NT>

@@ -659,12 +659,12 @@ uint32_t paged_choice(const void *args, uint32_t, uint64_t *groups) {
   memcpy(&a, args, sizeof(a));
   const PagedPlan p = paged_plan(a);
   *groups = (uint64_t)p.slots * a.kv_heads * p.row_tiles;
-  return (a.dim == 64 ? 2 : 0) + (a.page == 16);
+  return (a.dim == 64 ? 4 : 0) + (a.page == 16 ? 2 : 0) + p.past;
 }
-template <int DIM, bool SMALL>
+template <int DIM, bool SMALL, bool NT>
 hipError_t footprint_paged(uint32_t *lds_bytes, uint32_t *waves, uint32_t *regs_per_lane) {
   hipFuncAttributes attr;
-  hipError_t e = hipFuncGetAttributes(&attr, (const void *)attn_paged_partial<DIM, SMALL>);
+  hipError_t e = hipFuncGetAttributes(&attr, (const void *)attn_paged_partial<DIM, SMALL, NT>);
   if (e != hipSuccess) return e;
   *lds_bytes = (uint32_t)attr.sharedSizeBytes;
   *waves = 4;
@@ -938,7 +938,8 @@ const KernelOps kOps[TALLY_K_COUNT] = {
      init_t<AppendBodyT<128, 16, false>>, occupancy_append, pause_fraction_t<AppendBodyT<128, 4, false>>, footprint_append, {APPEND_ALL(APPEND_FOOT)},
      append_choice, append_range, nullptr, nullptr, nullptr, false, false, append_sizes},
     {"attn_paged_fp8", sizeof(tally_attn_paged_args), false, grid_paged, launch_native_paged,
-     nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, {footprint_paged<128, false>, footprint_paged<128, true>, footprint_paged<64, false>, footprint_paged<64, true>},
+     nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, {footprint_paged<128, false, false>, footprint_paged<128, false, true>, footprint_paged<128, true, false>, footprint_paged<128, true, true>,
+      footprint_paged<64, false, false>, footprint_paged<64, false, true>, footprint_paged<64, true, false>, footprint_paged<64, true, true>},
      paged_choice, nullptr, nullptr, nullptr, nullptr, false, false},
 };
 

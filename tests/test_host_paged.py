@@ -215,7 +215,7 @@ def test_registers_leave_room_beside_a_paused_tile(B, tmp_path):
         lds, spilled = re.search(r"\.group_segment_fixed_size:\s+(\d+)", kernel), re.search(r"\.private_segment_fixed_size:\s+(\d+)", kernel)
         found[name.group(1)] = (int(regs.group(1)) + int(kernel.split()[0]), int(lds.group(1)), int(spilled.group(1)))
     mine = {n: r for n, r in found.items() if "attn_paged" in n}
-    assert len(mine) >= 4 and all(r[0] <= 128 and r[1] <= 31 * 1024 for r in mine.values()), mine
+    assert len(mine) == 10 and all(r[0] <= 128 and r[1] <= 31 * 1024 for r in mine.values()), mine
     # nothing in memory beside the registers, but what the workers of sixteen waves miss of 128
     rest = {n: r for n, r in found.items() if "attn_paged" in n or "RopeBody" in n or "AppendBodyT" in n}
-    assert len(rest) == 6 + 3 + 21 and all(r[2] <= (16 if "ptb" in n and "ELi16E" in n else 0) for n, r in rest.items()), rest
+    assert len(rest) == 10 + 3 + 21 and all(r[2] <= (16 if "ptb" in n and "ELi16E" in n else 0) for n, r in rest.items()), rest
