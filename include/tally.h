@@ -220,7 +220,8 @@ typedef struct {
  * and head says that those of the block stand for 2^(e - 127) times as much (e from 1 to 254):
  *   k_pages: n_pages x kv_heads x page x dim,  v_pages: n_pages x kv_heads x page / 16 x dim x 16 (the values of 16
  *   tokens in a dim lie side by side, as the product with them wants them), k_exps, v_exps: n_pages x kv_heads.
- * A page may stand in several rows for reading; a page that a call writes to must stand in one.
+ * A page may stand at several places of the table for reading; of one that a call writes to at more than one the contents are
+ * undefined.
  *
  * Append: the tokens cu_seqlens[s] .. cu_seqlens[s + 1] - 1 of k and v (total x kv_heads x dim, bf16, packed as for
  * TALLY_K_ATTN_PROMPT_BF16) are sequence s's last ones: lens[s] says how many it has WITH them.  With rot > 0 k is
@@ -232,7 +233,7 @@ typedef struct {
  *   do not count for e;
  *   where e grows, the numbers held before the new ones are stored anew: divided by a power of two, so all are exact but those
  *   that fall below the smallest normal, which are rounded again.
- * k is turned in fp64 and rounded once, to its code.  So a call made twice leaves what it left the first time.
+ * k is turned in fp64 and rounded once, to its code (turned to 2^128 or more it counts as infinite).  So a call made twice leaves what it left the first time.
  * What a page holds behind a sequence's last token, and pages that no new token goes to, stay as they are.  Tokens that
  * belong to no sequence, whose place is negative or beyond seq_pages x page, or whose page is none of 0 .. n_pages - 1,
  * are not stored.  cu_seqlens, lens, table, positions, freqs are DEVICE memory; values of cu_seqlens outside [0, total] count
@@ -241,7 +242,7 @@ typedef struct {
  * pages 16-byte aligned; ld_k, ld_v as ld_* above; total at most 2^30, n_pages at most 2^30, seq_pages x page at most 2^28.
  * Logical grid, below 2^32 threads in all (tally_logical_grid): of the total / page + 2 n_seqs slots sequence s has those from
  * cu_seqlens[s] / page + 2 s on, for the pages that its new tokens go to; a block has one slot or up to four, and one K/V head or
- * up to eight, by the sizes. */
+ * up to four, by the sizes. */
 typedef struct {
   const uint16_t *k; const uint16_t *v; const int32_t *cu_seqlens; const int32_t *lens; const int32_t *table;
   const float *freqs; const int32_t *positions;

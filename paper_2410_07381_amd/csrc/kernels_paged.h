@@ -26,30 +26,34 @@ constexpr uint32_t kUnit = 16;                             // tokens side by sid
 // ---- appending ---------------------------------------------------------------------------
 // A wave's piece of work is 1024 numbers of K and as many of V: 8 tokens of a head of 128, 16 of one of 64.
 //
-// Packed prompts (append_waves): a wave takes such a piece of a page and one K/V head after the other, since the sines and
-// cosines of its tokens are more work than all else on a head's keys.  A workgroup has all pieces of a page, which share their
-// largest magnitudes through LDS, or of several small pages.
+// Prompts (kind 0): a wave takes such a piece of a page and one K/V head after the other, since the sines and cosines of its tokens
+// are more work than all else on a head's keys.  A workgroup has all pieces of a page, which share their largest magnitudes through
+// LDS, or of several small pages.
 //
-// Calls with hardly more than a token a sequence (kAppendFew): a wave takes a page, and of it the pieces that have new tokens, twice
-// where they are several: mostly it is one, and waves for the others would be in its way.
-constexpr uint32_t kAppendFew = 4;                         // tokens a sequence
+// Single tokens (kind 1): where there is hardly more than one a sequence, a wave takes a page, and of it the pieces that have new
+// tokens: mostly it is one, and waves for the others would be in its way.  In between, and with more than four pieces to a page
+// (kind 4), a workgroup's four waves take a page's pieces in turn.  Both go through pieces twice where a wave has several.
 constexpr uint64_t kAppendPieces = 8192;                   // from so many on a wave has two heads, from four times as many on four
 __host__ __device__ constexpr uint32_t append_tokens(uint32_t dim) { return 1024 / dim; }   // of a piece
-__host__ __device__ inline bool append_few(const tally_kv_append_args &a) { return a.total < kAppendFew * (uint64_t)a.n_seqs; }
+__host__ __device__ inline uint32_t append_kind(const tally_kv_append_args &a) {
+  const uint64_t n = a.n_seqs;
+  return a.total <= n + n / 8 ? 1 : a.page / append_tokens(a.dim) > 4 && a.total < n * a.page / 8 ? 4 : 0;
+}
 // waves of a workgroup, and slots (pages) that it has
 __host__ __device__ inline uint32_t append_waves(const tally_kv_append_args &a) {
   const uint32_t pieces = a.page / append_tokens(a.dim);
-  return append_few(a) || pieces < 4 ? 4 : pieces;
+  return append_kind(a) || pieces < 4 ? 4 : pieces;
 }
 __host__ __device__ inline uint32_t append_pages(const tally_kv_append_args &a) {
-  return append_few(a) ? 4 : append_waves(a) * append_tokens(a.dim) / a.page;
+  const uint32_t kind = append_kind(a);
+  return kind ? 4 / kind : append_waves(a) * append_tokens(a.dim) / a.page;
 }
 inline uint64_t append_slots(const tally_kv_append_args &a) { return (uint64_t)a.total / a.page + 2ull * a.n_seqs; }
 // K/V heads that a logical block goes through, one after the other.
 __host__ __device__ inline uint32_t append_heads(const tally_kv_append_args &a) {
   const uint64_t pieces = (uint64_t)a.total / append_tokens(a.dim) * a.kv_heads;
   uint32_t h = 1;
-  while (!append_few(a) && h < 4 && 2 * h <= a.kv_heads && pieces >= kAppendPieces * h * h) h *= 2;
+  while (append_kind(a) == 0 && h < 4 && 2 * h <= a.kv_heads && pieces >= kAppendPieces * h * h) h *= 2;
   return h;
 }
 inline uint64_t append_blocks(const tally_kv_append_args &a) {
@@ -90,14 +94,14 @@ typedef uint32_t u32x2_nt __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ uint32_t same(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
 #endif
 
-// WAVES of a workgroup; FEW: a page a wave.
-template <int DIM, int WAVES, bool FEW>
+// WAVES of a workgroup; FEW: 0, or how many of them share a page (kinds 1 and 4).
+template <int DIM, int WAVES, int FEW>
 struct AppendBodyT {
   using Args = tally_kv_append_args;
   static constexpr int THREADS = 64 * WAVES;
   static constexpr int MIN_WAVES = WAVES == 16 ? 4 : 3;
   static constexpr unsigned DYN_LDS = FEW ? 0 : WAVES * 8192;   // (a wave's sines and cosines)
-  static constexpr bool END_BARRIER = !FEW;                // (the waves' largest magnitudes)
+  static constexpr bool END_BARRIER = FEW != 1;               // (the waves' largest magnitudes)
   static constexpr bool YIELDS = false;
   static constexpr bool RANGE = false;
   static __device__ __forceinline__ void run(const Args &a, uint32_t bx, uint32_t, uint32_t) { append<false>(a, bx); }
@@ -115,7 +119,7 @@ struct AppendBodyT {
     const uint32_t lane = threadIdx.x & 63, wave = same(threadIdx.x >> 6);
     const uint32_t shift = (uint32_t)__builtin_ctz(a.page), P = a.page;
     const uint32_t HN = FEW ? 1 : append_heads(a), groups = (a.kv_heads + HN - 1) / HN;
-    const uint32_t per_page = FEW ? 1 : P / TOK, h0 = block % groups * HN;
+    const uint32_t per_page = FEW ? FEW : P / TOK, h0 = block % groups * HN;
     const uint32_t slot = block / groups * (WAVES / per_page) + wave / per_page;
     // The sequence of this slot: the last one that starts at or before it, 63 candidates at a time; the lane behind the last
     // candidate has where that one ends.
@@ -346,28 +350,37 @@ struct AppendBodyT {
       }
     };
 
+    __shared__ float s_top[2][2][WAVES];
+    // The largest magnitudes over the page's waves.  (A row of 16 lanes has all of theirs, some more than once.)
+    auto over_page = [&](float top, uint32_t turn) {
+      if (per_page == 1) return top;
+      if (lane % 32 == 0) s_top[turn][lane / 32][wave] = top;
+      __syncthreads();
+      return row16_all<MaxOp>(s_top[turn][lane / 32][wave - wave % per_page + lane % per_page]);
+    };
     if constexpr (FEW) {
       uint64_t index;
       Block b = block_of(h0, index);
-      const uint32_t u_first = from / TOK * TOK, u_last = (to - 1) / TOK * TOK;
-      for (uint32_t u0 = u_first; u0 <= u_last; u0 += TOK) {
+      const uint32_t mine = FEW == 1 ? 0 : wave * TOK, begins = from / TOK * TOK + mine;
+      uint32_t have = ~0u;                                 // the piece that is loaded
+      for (uint32_t u0 = begins; u0 < to; u0 += FEW * TOK) {
         ask(u0, h0);
         if (a.rot) make_turns(u0);
         take();
         tops();
+        have = u0;
       }
-      grow(b, index, over_wave(), true);
-      store(u_last, b, true);                              // (loaded last)
-      for (uint32_t u0 = u_first; u0 < u_last; u0 += TOK) {
+      grow(b, index, over_page(over_wave(), 0), mine == 0);
+      if (have != ~0u) store(have, b, true);
+      for (uint32_t u0 = begins; u0 < to && u0 != have; u0 += FEW * TOK) {
         ask(u0, h0);
         if (a.rot) make_turns(u0);
         take();
         store(u0, b, true);
       }
       if (b.ek != b.old_k || b.ev != b.old_v)
-        for (uint32_t u0 = 0; u0 < u_first; u0 += TOK) store(u0, b, false);
+        for (uint32_t u0 = mine; u0 < from / TOK * TOK; u0 += FEW * TOK) store(u0, b, false);
     } else {
-      __shared__ float s_top[2][2][WAVES];
       const uint32_t u0 = wave % per_page * TOK, begins = u0 / kUnit * kUnit;
       const bool live = there && begins < to && begins + kUnit > from, held = there && begins < from;   // new ones in the unit; old ones
       if (live) ask(u0, h0);
@@ -384,12 +397,7 @@ struct AppendBodyT {
           tops();
           top = over_wave();
         }
-        if (per_page > 1) {
-          if (lane % 32 == 0) s_top[i & 1][lane / 32][wave] = top;
-          __syncthreads();
-          // (a row of 16 lanes has all of the page's, some of them more than once)
-          top = row16_all<MaxOp>(s_top[i & 1][lane / 32][wave - wave % per_page + lane % per_page]);
-        }
+        top = over_page(top, i & 1);
         if (!live && !held) continue;
         grow(b, index, top, u0 == 0);
         store(u0, b, live);
@@ -421,7 +429,8 @@ inline PagedPlan paged_plan(uint32_t batch, uint32_t heads, uint32_t kv_heads, u
   p.group = heads / kv_heads;
   p.row_tiles = (p.group + kPagedRows - 1) / kPagedRows;
   const uint64_t across = (uint64_t)kv_heads * p.row_tiles, strips = ((uint64_t)seq_pages * page + kPagedStrip - 1) / kPagedStrip;
-  p.least = strips <= 4 ? 4 : 2;
+  const uint64_t whole = batch * across / 32 < 4 ? 4 : batch * across / 32 > 16 ? 16 : batch * across / 32;
+  p.least = (uint32_t)(strips <= whole ? strips : 2);
   p.parts = across >= 1024 ? 1 : (uint32_t)(1024 / across);
   if (p.parts > 256) p.parts = 256;
   const uint64_t most = (strips + p.least - 1) / p.least;  // of one sequence
@@ -704,21 +713,25 @@ __global__ __launch_bounds__(256, 4) void attn_paged_partial(tally_attn_paged_ar
 #endif
 }
 
-// One row per workgroup: the parts' weights exp(m - max), each wave a quarter of the parts, 16 bytes of a part's acc to a lane.
-template <int DIM>
+// One row per workgroup of WAVES waves (a row: a query head of a sequence), or a row per wave: the parts' weights exp(m - max), 16
+// bytes of a part's acc to a lane.
+template <int DIM, int WAVES>
 __global__ __launch_bounds__(256) void attn_paged_merge(tally_attn_paged_args a, PagedPlan p, uint32_t urgent) {
 #ifdef __HIP_DEVICE_COMPILE__
   if (urgent) __builtin_amdgcn_s_setprio(3);
   constexpr uint32_t LANES = DIM / 4, SIDE = 64 / LANES;   // parts side by side in a wave
-  __shared__ float s_acc[4][DIM];
-  __shared__ float s_sum[4];
-  const uint32_t head = blockIdx.x % a.heads, seq = blockIdx.x / a.heads, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  __shared__ float s_acc[WAVES][DIM];
+  __shared__ float s_sum[WAVES];
+  const uint32_t lane = threadIdx.x & 63, wave = WAVES == 1 ? 0 : threadIdx.x >> 6;
+  const uint32_t unit = WAVES == 1 ? same(blockIdx.x * 4 + (threadIdx.x >> 6)) : blockIdx.x;
+  if (WAVES == 1 && unit >= a.heads * a.batch) return;
+  const uint32_t head = unit % a.heads, seq = unit / a.heads;
   PagedPart mine;
   if (!paged_find(a, p, seq, true, mine) || mine.parts == 1) return;
   const uint64_t row = (uint64_t)mine.first * a.heads + head;
   const float2 *ml = reinterpret_cast<const float2 *>(a.scratch) + row;
   const float *rec = static_cast<const float *>(a.scratch) + paged_acc_at((uint64_t)p.slots * a.heads) + row * DIM + lane % LANES * 4;
-  constexpr uint32_t ROUND = 4 * SIDE, U = 4;              // parts at a time
+  constexpr uint32_t ROUND = WAVES * SIDE, U = 4;          // parts at a time
   const uint32_t first = wave * SIDE + lane / LANES;
   // (the first round's loads do not wait for the weights)
   f32x4_t v[U];
@@ -767,22 +780,29 @@ __global__ __launch_bounds__(256) void attn_paged_merge(tally_attn_paged_args a,
     for (int e = 0; e < 4; ++e) acc[e] = halves(acc[e]);
     sum = halves(sum);
   }
-  if (lane < LANES) *reinterpret_cast<f32x4_t *>(&s_acc[wave][lane * 4]) = acc;
   any = __builtin_amdgcn_ballot_w64(any) != 0;
-  if (lane == 0) s_sum[wave] = any ? sum : kNoTokens;
-  __syncthreads();
-  if (threadIdx.x < DIM) {
-    const uint32_t d = threadIdx.x;
-    const float o = (s_acc[0][d] + s_acc[1][d]) + (s_acc[2][d] + s_acc[3][d]);
-    float all = 0.f;
-    bool any = false;
+  const uint64_t at = (uint64_t)seq * (a.ld_out ? a.ld_out : a.heads * DIM) + head * DIM;
+  if constexpr (WAVES == 1) {
+    const float over = any ? 1.f / sum : 0.f;
+    if (lane < LANES)
+      *reinterpret_cast<uint2 *>(a.out + at + lane * 4) = make_uint2(OnePass<DIM, 16, 32, 3>::pack(acc[0] * over, acc[1] * over),
+                                                                     OnePass<DIM, 16, 32, 3>::pack(acc[2] * over, acc[3] * over));
+  } else {
+    if (lane < LANES) *reinterpret_cast<f32x4_t *>(&s_acc[wave][lane * 4]) = acc;
+    if (lane == 0) s_sum[wave] = any ? sum : kNoTokens;
+    __syncthreads();
+    if (threadIdx.x < DIM) {
+      const uint32_t d = threadIdx.x;
+      const float o = (s_acc[0][d] + s_acc[1][d]) + (s_acc[2][d] + s_acc[3][d]);
+      float all = 0.f;
+      bool some = false;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      any |= !(s_sum[i] < 0.f);
-      all += s_sum[i] < 0.f ? 0.f : s_sum[i];
+      for (int i = 0; i < 4; ++i) {
+        some |= !(s_sum[i] < 0.f);
+        all += s_sum[i] < 0.f ? 0.f : s_sum[i];
+      }
+      a.out[at + d] = f32_to_bf16(some ? o / all : 0.f);
     }
-    const uint32_t LDO = a.ld_out ? a.ld_out : a.heads * DIM;
-    a.out[(uint64_t)seq * LDO + head * DIM + d] = f32_to_bf16(any ? o / all : 0.f);
   }
 #endif
 }
@@ -796,7 +816,8 @@ hipError_t launch_paged_dim(hipStream_t s, const tally_attn_paged_args &a, uint3
                              : (p.past ? attn_paged_partial<DIM, false, true> : attn_paged_partial<DIM, false, false>);
   const hipError_t e = launch(kernel, dim3(p.slots * a.kv_heads * p.row_tiles), dim3(256), 0, s, a, p, urgent);
   if (e != hipSuccess || p.single) return e;
-  return launch(attn_paged_merge<DIM>, dim3(a.heads * a.batch), dim3(256), 0, s, a, p, urgent);
+  if (p.slots <= 6 * a.batch) return launch(attn_paged_merge<DIM, 1>, dim3((a.heads * a.batch + 3) / 4), dim3(256), 0, s, a, p, urgent);
+  return launch(attn_paged_merge<DIM, 4>, dim3(a.heads * a.batch), dim3(256), 0, s, a, p, urgent);
 }
 inline hipError_t launch_attn_paged(hipStream_t s, const void *args, uint32_t urgent) {
   tally_attn_paged_args a;

@@ -672,13 +672,15 @@ hipError_t footprint_paged(uint32_t *lds_bytes, uint32_t *waves, uint32_t *regs_
   return hipSuccess;
 }
 // Appending: a kernel for each width of a head and number of waves
-#define APPEND_ALL(X) X(0, AppendBodyT<128, 4, false>) X(1, AppendBodyT<128, 8, false>) X(2, AppendBodyT<128, 16, false>) \
-  X(3, AppendBodyT<128, 4, true>) X(4, AppendBodyT<64, 4, false>) X(5, AppendBodyT<64, 8, false>) X(6, AppendBodyT<64, 4, true>)
+#define APPEND_ALL(X) X(0, AppendBodyT<128, 4, 0>) X(1, AppendBodyT<128, 8, 0>) X(2, AppendBodyT<128, 16, 0>) \
+  X(3, AppendBodyT<128, 4, 1>) X(4, AppendBodyT<128, 4, 4>) X(5, AppendBodyT<64, 4, 0>) X(6, AppendBodyT<64, 8, 0>) \
+  X(7, AppendBodyT<64, 4, 1>) X(8, AppendBodyT<64, 4, 4>)
 uint32_t append_range(const void *args) {
   tally_kv_append_args a;
   memcpy(&a, args, sizeof(a));
-  const uint32_t waves = append_waves(a);
-  return a.dim == 64 ? (append_few(a) ? 6 : waves == 8 ? 5 : 4) : append_few(a) ? 3 : waves == 16 ? 2 : waves == 8 ? 1 : 0;
+  const uint32_t waves = append_waves(a), kind = append_kind(a);
+  if (a.dim == 64) return kind == 1 ? 7 : kind == 4 ? 8 : waves == 8 ? 6 : 5;
+  return kind == 1 ? 3 : kind == 4 ? 4 : waves == 16 ? 2 : waves == 8 ? 1 : 0;
 }
 uint32_t append_choice(const void *args, uint32_t, uint64_t *) { return append_range(args); }
 hipError_t launch_native_append(hipStream_t s, const void *args, tally_dim3 g, uint32_t how) {
@@ -935,7 +937,7 @@ const KernelOps kOps[TALLY_K_COUNT] = {
      launch_ptb_t<RopeBody>, init_t<RopeBody>, occupancy_t<RopeBody>, pause_fraction_t<RopeBody>, footprint_t<RopeBody>,
      {footprint_native_t<RopeBody>}, nullptr, nullptr, nullptr, nullptr, nullptr, false, false, rope_sizes},
     {"kv_append_fp8", sizeof(tally_kv_append_args), true, grid_append, launch_native_append, launch_sliced_append, launch_ptb_append,
-     init_t<AppendBodyT<128, 16, false>>, occupancy_append, pause_fraction_t<AppendBodyT<128, 4, false>>, footprint_append, {APPEND_ALL(APPEND_FOOT)},
+     init_t<AppendBodyT<128, 16, 0>>, occupancy_append, pause_fraction_t<AppendBodyT<128, 4, 0>>, footprint_append, {APPEND_ALL(APPEND_FOOT)},
      append_choice, append_range, nullptr, nullptr, nullptr, false, false, append_sizes},
     {"attn_paged_fp8", sizeof(tally_attn_paged_args), false, grid_paged, launch_native_paged,
      nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, {footprint_paged<128, false, false>, footprint_paged<128, false, true>, footprint_paged<128, true, false>, footprint_paged<128, true, true>,

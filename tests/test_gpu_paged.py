@@ -187,6 +187,10 @@ APPEND = [
     ([1, 1, 1, 1, 1], [0, 5, 15, 16, 31], 8, 128, 16, 128), ([0, 3, 0, 0, 40, 1], [9, 30, 0, 16, 1, 127], 3, 64, 32, 48),
     ([64, 0, 65, 1], [64, 64, 0, 63], 1, 64, 64, 64), ([5, 200, 31], [0, 100, 33], 7, 128, 32, 128), ([255, 1], [1, 127], 2, 64, 128, 0),
     ([1] * 70, list(range(70)), 1, 64, 16, 64), ([1, 0, 2] * 50, [3] * 150, 2, 64, 16, 32),
+    # mostly one token, and one sequence that gets many: its pages are gone through by one wave, or four
+    ([1] * 30 + [0] * 260 + [250], [60 + i for i in range(291)], 2, 128, 128, 128), ([1] * 30 + [0] * 260 + [250], [5] * 291, 1, 64, 64, 48),
+    ([2] * 20 + [130], [126 - i for i in range(21)], 3, 128, 128, 128), ([3, 1, 60, 1, 0, 2] * 4, [62, 13, 100, 0, 0, 127] * 4, 1, 128, 64, 64),
+    ([3, 1, 100, 1, 0, 2] * 4, [62, 13, 100, 0, 0, 127] * 4, 2, 64, 128, 16),
 ]
 
 
@@ -214,6 +218,38 @@ def test_append(env, new, held, kv, dim, page, rot, form):
     _same(paged, want, form)
     _run(ctx, torch, kern, form)                           # again: what was left the first time
     _same(paged, want, "again")
+
+
+@pytest.mark.parametrize("new,held,kv,dim,page,rot,form", [
+    ([17000], [0], 4, 128, 64, 128, "hi"), ([33000], [5], 8, 128, 32, 64, "ptb"), ([23000], [100], 3, 128, 128, 128, "sliced"),
+    ([9000, 1, 13000], [3, 500, 17], 7, 64, 16, 64, "ptb"), ([40000], [0], 5, 64, 128, 0, "hi")])
+def test_append_with_several_heads_a_wave(env, new, held, kv, dim, page, rot, form):
+    """Calls so large that a wave goes through two heads, or four, one after the other; numbers of heads that they do not divide."""
+    test_append(env, new, held, kv, dim, page, rot, form)
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_thousands_of_sequences(env, form):
+    """More of them than two rounds of 63 find: appended to, few tokens each and most of them none, and attended to."""
+    B, ctx, torch = env
+    rng = np.random.default_rng(21)
+    n, page, dim = 5000, 16, 64
+    new, held = (rng.random(n) < 0.3).astype(int), rng.integers(0, 40, n)
+    new[[7, 4990]] = 45
+    lens = (new + held).astype(np.int32)
+    cu = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    table, pages = _deal(rng, lens, page)
+    cache = _cache(rng, pages, 1, page, dim)
+    x, q = _bits(rng, (int(cu[-1]), 2, dim)), _bits(rng, (n, 1, dim), 0.25)
+    paged, tx, tt, tl = _paged(B, torch, cache), _dev(torch, x), _dev(torch, table), _dev(torch, lens)
+    _run(ctx, torch, B.kv_append_fp8(tx[:, :1], tx[:, 1:], _dev(torch, cu), tl, tt, paged), form)
+    cache = OP.append(obf16.decode(x[:, :1]), obf16.decode(x[:, 1:]), cu, lens, table, cache)
+    _same(paged, cache)
+    if form in ("hi", "be"):
+        scratch = torch.zeros(max(B.attn_paged_scratch_bytes(n, 1, 1, dim, page, table.shape[1]), 1), dtype=torch.uint8, device="cuda")
+        out = torch.zeros((n, 1, dim), dtype=torch.int16, device="cuda")
+        _run(ctx, torch, B.attn_paged_fp8(_dev(torch, q), paged, tt, tl, out, scratch, scale=0.02), form)
+        _attn_ok(_host(out), *OP.attn_paged(obf16.decode(q), cache, table, lens, 0.02))
 
 
 @pytest.mark.parametrize("page", [16, 64])
@@ -318,7 +354,7 @@ PAGED = [
     ([63, 64, 65, 127, 128, 129], 8, 2, 128, 64, 0), ([255, 256, 257], 7, 1, 64, 128, 0), ([511, 512, 513], 5, 5, 64, 16, 0),
     ([1000, 0, 3, 700], 32, 8, 128, 64, 0), ([3001, 1, 2000], 28, 4, 128, 32, 0), ([2500], 16, 1, 128, 128, 0), ([1500, 100], 17, 1, 64, 32, 0),
     ([900, 33], 40, 1, 128, 16, 0), ([4000], 2, 2, 64, 64, 0), ([40, 300], 12, 12, 64, 16, 400), ([600, 5, 0, 77], 96, 2, 64, 16, 40),
-    ([20 * i % 97 for i in range(70)], 2, 1, 64, 16, 0), ([1] * 63 + [0] * 66 + [900], 1, 1, 64, 16, 0), ([130 + i for i in range(65)], 2, 2, 64, 32, 30),
+    ([20 * i % 97 for i in range(70)], 2, 1, 64, 16, 0), ([700 + i for i in range(40)], 8, 8, 64, 64, 8), ([1500, 3, 900] * 2, 4, 4, 128, 32, 70000), ([1] * 63 + [0] * 66 + [900], 1, 1, 64, 16, 0), ([130 + i for i in range(65)], 2, 2, 64, 32, 30),
 ]
 
 
