@@ -11,6 +11,7 @@ Floating point is carried in fp64 and rounded once to the storage type.
 Pinning status (see tests/test_oracle_*.py):
   grid / slicing / persistent-worker schedules  pinned (paper's worked examples, brute force)
   saxpy, reduce_sum, gemm, gemv, softmax, layernorm, attn_decode  pinned (closed forms, invariants)
+  rope, append, attn_paged (paged)               pinned (complex numbers, brute force, attn_prefix)
   turnaround estimate (Eq. 1) and selection rule  pinned (closed form, hand-made tables)
   latency / throughput figures                   parity unpinned (measured only)
 """

@@ -7,6 +7,14 @@
 // Pages consist of units of 16 tokens.  K's lie token by token, V's dim by dim with the 16 tokens of a dim side by side: a
 // lane's 8 or 16 bytes are then a fragment of the products' first operand as they come from memory (K's rows
 // are tokens, V's rows are dims), and nothing goes through LDS.
+//
+// What bounds both is memory, and for small calls one load waiting for another.  Measured (us of a call; what it reads and
+// writes once at the 5.12 TB/s of a copy in brackets; an empty launch is 2.4):
+//   appending, 8 heads of 128: one token 4.7; one for each of 64 sequences 6.2; 24 prompts of 1 to 4096 tokens 25 [16.3]; 32768 tokens 45.7 [39.3];
+//   attention: 4 sequences of up to 512 tokens, 12 heads of 64, 5.8; 16 of up to 3001, 28/4 heads of 128, 12.2 [4.9]; 32 of up to 4096, 32/8,
+//   31.9 [26.3]; 8 of up to 131071 173 to 188 from card to card [210], 6.2 to 5.7 TB/s.
+// FETCH_SIZE and WRITE_SIZE say that either moves what it has to and nothing beside it (append of 32768 tokens 135 MB in and 67 MB out;
+// 32 sequences of up to 4096 tokens 136 MB in).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -33,6 +41,16 @@ constexpr uint32_t kUnit = 16;                             // tokens side by sid
 // Single tokens (kind 1): where there is hardly more than one a sequence, a wave takes a page, and of it the pieces that have new
 // tokens: mostly it is one, and waves for the others would be in its way.  In between, and with more than four pieces to a page
 // (kind 4), a workgroup's four waves take a page's pieces in turn.  Both go through pieces twice where a wave has several.
+//
+// Figures (us, 8 heads of 128).  Sequences x tokens each, kinds 0 / 1: pages of 128, 8 x 1 6.1 / 4.9, 64 x 1 20.1 / 5.4; of 64, 64 x 1 11.5 / 5.4;
+// of 16, 64 x 1 6.4 / 6.2, 64 x 2 7.0 / 8.4, 200 x 2 12.3 / 11.6.  Kinds 0 / 1 / 4: pages of 128, 64 x 2 20.8 / 8.4 / 7.0, 64 x 8 21.3 / 9.8 / 7.1, 200 x 4
+// 59.6 / 12.5 / 14.9; of 64, 64 x 4 12.3 / 8.6 / 6.7, 64 x 8 (kind 0 from here on) 11.6 / 10.8.  127 x 1 and 380 tokens of one sequence, pages of 128:
+// kind 1 46, kind 4 16.
+// Heads a wave goes through, 1 / 2 / 4 / 8, one prompt, pages of 16: 7000 tokens 13.5 13.9 16.3 23.6; 13504 21.3 20.9 21.4 26.1; 22000 36.7 33.9
+// 36.2 35.5; 32768 51.5 47.4 46.1 46.0; 38229 60.1 55.5 57.7 66.2; 54613 82.9 75.4 76.8 79.0.  Fewer heads are more workgroups: 8 are best where
+// their number is just what fits on the GPU at once, and the worst a little beyond.
+// Tried: 16 tokens of a head of 128 a wave (194 registers, two waves per SIMD; 32768 tokens 47 to 55), the next head's numbers asked for ahead (pages
+// of 128 51 and 48, others the same, registers spilled in workers), a page's id and old bytes asked for earlier (64 tokens 6.4).
 constexpr uint64_t kAppendPieces = 8192;                   // from so many on a wave has two heads, from four times as many on four
 __host__ __device__ constexpr uint32_t append_tokens(uint32_t dim) { return 1024 / dim; }   // of a piece
 __host__ __device__ inline uint32_t append_kind(const tally_kv_append_args &a) {
@@ -415,7 +433,19 @@ struct AppendBodyT {
 // through the lengths, 64 at a time.
 //
 // A workgroup has 16 query heads at most of one K/V head and a part's tokens, each wave a tile of 32 in turn, with a state
-// of its own; the four are merged in LDS at the end.
+// of its own; the four are merged in LDS at the end.  128 registers and 17 KB of LDS: four of them on a compute unit, or one beside a
+// paused 256 x 256 GEMM tile.
+//
+// 1024 workgroups are what is on the GPU at once (us with 512 / 768 / 1024 / 2048: 32 sequences of up to 4096, 8 K/V heads, 36.6 36.0 34.4 34.6; 8 of up to
+// 131071 223 211 193 195; one of 32768 19.0 20.1 20.2 20.2).  A part has two strips at least (1 / 2 / 4: 16 of up to 3001, 4 K/V heads, 13.5 12.2 12.1; one of
+// 4096, 8 heads, 9.2 9.3 10.4).
+// One part a sequence saves the second kernel.  It pays up to 4 strips whatever the number of workgroups (4 sequences of 512, 12 heads of 64: 5.8, in two
+// parts 8.2; one of 1024, 8 heads, 9.9 and 9.2), up to 8 from 256 workgroups on (8 of 600, 32 heads, 10.8 and 12.1; with 64 of them, 8 of 1024, 8 heads,
+// 10.0 and 9.4), up to 16 from 512 on (64 of up to 2000, 8 heads, 32.8 and 34.9; with 128, 128 of 2000 on one head of 64, 14.3 and 12.2).  Eight waves a workgroup then: 6.2 for 5.8.
+// A row of the second kernel is a wave's where sequences have few parts, else a workgroup's (a wave / a workgroup: 64 of up to 1000, 3 parts, 19.9
+// 21.3; 64 of up to 8192, heads of 64, 3, 51.8 53.8; 32 of up to 4096, 5, 32.1 32.4; 16 of up to 3001, 17, 13.4 12.4; one of 32768 26.9 20.4).
+// Caches above 256 MB, which is what the Infinity Cache holds, are read past it (non-temporal; three caches in turn, ordinary / so: capacity 192 MB
+// 26.0 27.3, 224 29.7 28.3, 256 34.5 32.3, 320 40.3 37.2, 2.1 GB 192 173; one cache again and again 256 MB 28.8 31.4).
 constexpr uint32_t kPagedStrip = 128, kPagedTile = 32, kPagedRows = 16;
 struct PagedPlan {
   uint32_t group, row_tiles;                               // query heads of a K/V head; workgroups that share them

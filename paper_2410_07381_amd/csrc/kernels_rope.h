@@ -6,7 +6,10 @@
 // and x^14, are off by 2e-14 at most.  An angle belongs to a token and a pair, not to a head: a workgroup makes a table of them
 // in LDS for its tokens, a sine and a cosine per thread and turn, and all heads read it.
 //
-// What bounds it is reading and writing x once.
+// What bounds it is reading and writing x once.  Measured (us of a call; the bytes at the 5.12 TB/s of a copy in brackets, an empty launch is
+// 2.4): one token, 24 heads of 64, 3.3; 64 tokens, 40 heads of 128, 3.6; 4097 tokens, 32 heads, 11.6 [13.1, found in the Infinity Cache]; 13.5 thousand
+// tokens, 40 heads, 52.9 [54.0].  A call that moves more than that cache holds goes past it (one buffer again and again / three in turn,
+// ordinary: 192 MB 31.5 39.2, 256 MB 42.5 50.2, 320 MB 60.5 62.6; non-temporal 34.6 36.3, 45.1 46.7, 56.4 57.9).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
