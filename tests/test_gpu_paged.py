@@ -482,6 +482,30 @@ def test_caches_beyond_4_gib(env):
     _attn_ok(_host(out), *OP.attn_paged(obf16.decode(q), small, np.array([[0, 1, 2]]), [n]))
 
 
+def test_the_widest_rows(env):
+    """As many heads as a token's row has room for."""
+    B, ctx, torch = env
+    rng = np.random.default_rng(22)
+    x, freqs, at = _bits(rng, (3, 65536, 16)), (0.5 ** np.arange(8)).astype(np.float32), np.array([0, 70000, -9], np.int32)
+    out = torch.zeros((3, 65536, 16), dtype=torch.int16, device="cuda")
+    _run(ctx, torch, B.rope_bf16(_dev(torch, x), out, _dev(torch, freqs), _dev(torch, at), interleaved=True), "ptb")
+    _rope_ok(_host(out), *OP.rope(obf16.decode(x), at, freqs, True))
+    kv, dim, page, new, held = 700, 64, 16, [3, 0, 18], [20, 5, 1]
+    cu, lens = np.concatenate([[0], np.cumsum(new)]).astype(np.int32), (np.array(new) + held).astype(np.int32)
+    table, pages = _deal(rng, lens, page)
+    cache = _filled(rng, pages, kv, page, dim)
+    x, q = _bits(rng, (int(cu[-1]), 2 * kv, dim)), _bits(rng, (3, kv, dim), 0.5)
+    paged, tx, tt = _paged(B, torch, cache), _dev(torch, x), _dev(torch, table)
+    _run(ctx, torch, B.kv_append_fp8(tx[:, :kv], tx[:, kv:], _dev(torch, cu), _dev(torch, lens), tt, paged), "sliced")
+    cache = OP.append(obf16.decode(x[:, :kv]), obf16.decode(x[:, kv:]), cu, lens, table, cache)
+    _same(paged, cache)
+    _attn_ok(_attend(B, ctx, torch, q, cache, table, lens), *OP.attn_paged(obf16.decode(q), cache, table, lens))
+    # all query heads on one K/V head
+    table, pages = _deal(rng, [300, 40], 32)
+    cache, q = _filled(rng, pages, 1, 32, dim), _bits(rng, (2, 3001, dim), 0.5)
+    _attn_ok(_attend(B, ctx, torch, q, cache, table, [300, 40]), *OP.attn_paged(obf16.decode(q), cache, table, [300, 40]))
+
+
 # ---------------------------------------------------------------- together
 def test_a_prompt_and_the_steps_behind_it(env):
     """As a serving job uses them: prompts are turned, attended to and appended; then steps turn their token's q, append its key and
