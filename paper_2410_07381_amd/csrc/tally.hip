@@ -103,7 +103,14 @@ struct KernelOps {
   // what a block's time depends on and the grid does not say (null: nothing that keeps measurements apart).  Not the
   // exact rows and tokens: prompts that differ by a few tokens share what was measured
   CallSizes (*sizes)(const void *args);
+  // where the workers of one operator are so different that the largest must not stand for all: which of `worker_kernels`
+  // kernels the arguments take (null: one stands for all), and what one of its workgroups occupies and how many are resident
+  uint32_t (*worker_choice)(const void *args);
+  uint32_t worker_kernels;
+  hipError_t (*worker_footprint)(uint32_t kernel, uint32_t *lds_bytes, uint32_t *waves, uint32_t *regs_per_lane);
+  int (*worker_occupancy)(uint32_t kernel, int *blocks_per_cu);
 };
+constexpr uint32_t kMaxWorkerKernels = 9;
 
 template <class Body>
 hipError_t launch_native_t(hipStream_t s, const void *args, tally_dim3 g, uint32_t how) {
@@ -701,7 +708,8 @@ hipError_t launch_ptb_append(hipStream_t s, const void *args, const PtbCtl &c) {
 #undef APPEND_CASE
   return hipErrorInvalidValue;
 }
-// (the most and the fewest of any variant's, which stand for all of them)
+// What a worker occupies, and how many are resident at once: for who does not know the arguments the most and the fewest of any
+// variant's (with pages of 128 there is one workgroup on a compute unit, with others up to five).
 hipError_t footprint_append(uint32_t *lds_bytes, uint32_t *waves, uint32_t *regs_per_lane) {
   *lds_bytes = *waves = *regs_per_lane = 0;
   hipError_t e = hipSuccess;
@@ -725,6 +733,18 @@ int occupancy_append(int *blocks_per_cu) {
 #undef APPEND_LEAST
   return rc;
 }
+hipError_t footprint_append_of(uint32_t kernel, uint32_t *lds_bytes, uint32_t *waves, uint32_t *regs_per_lane) {
+#define APPEND_CASE(i, ...) case i: return footprint_t<__VA_ARGS__>(lds_bytes, waves, regs_per_lane);
+  switch (kernel) { APPEND_ALL(APPEND_CASE) }
+#undef APPEND_CASE
+  return hipErrorInvalidValue;
+}
+int occupancy_append_of(uint32_t kernel, int *blocks_per_cu) {
+#define APPEND_CASE(i, ...) case i: return occupancy_t<__VA_ARGS__>(blocks_per_cu);
+  switch (kernel) { APPEND_ALL(APPEND_CASE) }
+#undef APPEND_CASE
+  return TALLY_ERR_INVALID_ARG;
+}
 CallSizes rope_sizes(const void *args) {
   tally_rope_args a;
   memcpy(&a, args, sizeof(a));
@@ -733,7 +753,7 @@ CallSizes rope_sizes(const void *args) {
 CallSizes append_sizes(const void *args) {
   tally_kv_append_args a;
   memcpy(&a, args, sizeof(a));
-  return {a.n_seqs, a.kv_heads, a.dim, a.page};
+  return {a.n_seqs, a.kv_heads, a.dim, a.page | append_kind(a) << 16};
 }
 hipError_t launch_native_prefix(hipStream_t s, const void *args, tally_dim3, uint32_t how) {
   return launch_attn_prefix(s, args, how & kUrgent);
@@ -938,7 +958,8 @@ const KernelOps kOps[TALLY_K_COUNT] = {
      {footprint_native_t<RopeBody>}, nullptr, nullptr, nullptr, nullptr, nullptr, false, false, rope_sizes},
     {"kv_append_fp8", sizeof(tally_kv_append_args), true, grid_append, launch_native_append, launch_sliced_append, launch_ptb_append,
      init_t<AppendBodyT<128, 16, 0>>, occupancy_append, pause_fraction_t<AppendBodyT<128, 4, 0>>, footprint_append, {APPEND_ALL(APPEND_FOOT)},
-     append_choice, append_range, nullptr, nullptr, nullptr, false, false, append_sizes},
+     append_choice, append_range, nullptr, nullptr, nullptr, false, false, append_sizes,
+     append_range, 9, footprint_append_of, occupancy_append_of},
     {"attn_paged_fp8", sizeof(tally_attn_paged_args), false, grid_paged, launch_native_paged,
      nullptr, nullptr, nullptr, nullptr, nullptr, nullptr, {footprint_paged<128, false, false>, footprint_paged<128, false, true>, footprint_paged<128, true, false>, footprint_paged<128, true, true>,
       footprint_paged<64, false, false>, footprint_paged<64, false, true>, footprint_paged<64, true, false>, footprint_paged<64, true, true>},
@@ -1016,6 +1037,8 @@ struct tally_ctx {
   uint32_t num_cus;
   uint32_t lds_per_cu;
   uint32_t max_workers[TALLY_K_COUNT];  // persistent-worker workgroups resident at once, per kernel
+  // the same, and what one occupies, for each kernel that workers may take (KernelOps::worker_choice)
+  uint32_t worker_max[TALLY_K_COUNT][kMaxWorkerKernels], worker_foot[TALLY_K_COUNT][kMaxWorkerKernels][3];
   // what one workgroup occupies on a compute unit (LDS bytes, waves, registers per lane): of the
   // persistent-worker form, and of each kernel that the original form chooses from; asked of the
   // runtime once, at creation
@@ -1158,10 +1181,18 @@ const uint32_t *native_footprint(tally_ctx *ctx, const tally_kernel_desc *desc, 
   return ctx->foot_native[desc->kernel_id][ops.native_choice ? ops.native_choice(desc->args, how, groups) : 0];
 }
 
+// Workers that are resident at once.  (The arguments may not have been looked at yet: of refused ones the fewest.)
+uint32_t workers_at_most(const tally_ctx *ctx, const tally_kernel_desc *desc) {
+  const KernelOps *ops;
+  tally_dim3 grid;
+  if (!kOps[desc->kernel_id].worker_choice || check_desc(desc, &ops, &grid) != TALLY_OK) return ctx->max_workers[desc->kernel_id];
+  return ctx->worker_max[desc->kernel_id][ops->worker_choice(desc->args)];
+}
+
 // What one workgroup of a job of this kind occupies.
 const uint32_t *job_footprint(const tally_ctx *ctx, const tally_kernel_desc *desc, int kind, uint64_t *groups) {
   const KernelOps &ops = kOps[desc->kernel_id];
-  if (kind == KIND_PTB) return ctx->foot_worker[desc->kernel_id];
+  if (kind == KIND_PTB) return ops.worker_choice ? ctx->worker_foot[desc->kernel_id][ops.worker_choice(desc->args)] : ctx->foot_worker[desc->kernel_id];
   uint32_t i = 0;
   if (kind == KIND_SLICED) i = ops.sliced_choice ? ops.sliced_choice(desc->args) : 0;
   else if (ops.native_choice) i = ops.native_choice(desc->args, kShared, groups);
@@ -1636,6 +1667,16 @@ int tally_create(tally_ctx **out, void *hip_stream_hi, void *hip_stream_be) {
       }
       c->max_workers[k] = (uint32_t)per_cu * c->num_cus;
     }
+    for (uint32_t i = 0; kOps[k].worker_choice && i < kOps[k].worker_kernels; ++i) {
+      uint32_t *ft = c->worker_foot[k][i];
+      if ((e = kOps[k].worker_footprint(i, &ft[0], &ft[1], &ft[2])) != hipSuccess || kOps[k].worker_occupancy(i, &per_cu) != TALLY_OK ||
+          per_cu < 1) {
+        if (e != hipSuccess) g_last_hip = (int)e;
+        tally_destroy(c);
+        return TALLY_ERR_HIP;
+      }
+      c->worker_max[k][i] = (uint32_t)per_cu * c->num_cus;
+    }
   }
   if ((e = attn_decode_init()) != hipSuccess) {
     g_last_hip = (int)e;
@@ -1744,7 +1785,7 @@ int tally_launch_ptb_until(tally_ctx *ctx, const tally_kernel_desc *desc, uint32
   if (!ctx || !out || !desc || num_workers == 0 || chunk == 0) return TALLY_ERR_INVALID_ARG;
   if (desc->kernel_id >= TALLY_K_COUNT || chunk > (1u << 16)) return TALLY_ERR_INVALID_ARG;
   // every worker resident at once (an unsupported kernel is reported by new_job below)
-  if (kOps[desc->kernel_id].transformable && num_workers > ctx->max_workers[desc->kernel_id])
+  if (kOps[desc->kernel_id].transformable && num_workers > workers_at_most(ctx, desc))
     return TALLY_ERR_INVALID_ARG;
   tally_job *j;
   int rc = new_job(ctx, desc, KIND_PTB, coverage, &j);
@@ -1827,7 +1868,7 @@ int tally_kernel_footprint(tally_ctx *ctx, uint32_t kernel_id, int form, uint32_
 int tally_max_workers(tally_ctx *ctx, const tally_kernel_desc *desc, uint32_t *max_workers) {
   if (!ctx || !desc || !max_workers || desc->kernel_id >= TALLY_K_COUNT) return TALLY_ERR_INVALID_ARG;
   if (!kOps[desc->kernel_id].transformable) return TALLY_ERR_UNSUPPORTED;
-  *max_workers = ctx->max_workers[desc->kernel_id];
+  *max_workers = workers_at_most(ctx, desc);
   return TALLY_OK;
 }
 
@@ -2121,7 +2162,7 @@ void fill_turnaround(tally_ctx *ctx, const KernelOps *ops, const void *args, uin
 // The candidate set of Section 4.2: persistent-worker counts that are multiples of the
 // compute-unit count and fit (every worker resident), each with 1, 4 and 16 task indices per
 // fetch where the grid has that many blocks per worker; slices of 1/2 ... 1/256 of the grid.
-uint32_t candidate_configs(tally_ctx *ctx, uint32_t kernel_id, uint64_t total, tally_config *out,
+uint32_t candidate_configs(tally_ctx *ctx, const tally_kernel_desc *desc, uint64_t total, tally_config *out,
                            uint32_t cap) {
   uint32_t n = 0;
   auto push = [&](uint32_t kind, uint32_t param, uint32_t chunk) {
@@ -2129,7 +2170,7 @@ uint32_t candidate_configs(tally_ctx *ctx, uint32_t kernel_id, uint64_t total, t
       if (out[i].kind == kind && out[i].param == param && out[i].chunk == chunk) return;
     if (n < cap) out[n++] = tally_config{kind, param, chunk, 0.f, 0.f};
   };
-  const uint32_t maxw = ctx->max_workers[kernel_id];
+  const uint32_t maxw = workers_at_most(ctx, desc);
   for (uint32_t w = ctx->num_cus; w <= maxw; w += ctx->num_cus) {
     const uint32_t workers = (uint64_t)w < total ? w : (uint32_t)total;
     static const uint32_t chunks[3] = {1, 4, 16};
@@ -2174,7 +2215,7 @@ int tally_candidate_configs(tally_ctx *ctx, const tally_kernel_desc *desc, tally
   int rc = check_desc(desc, &ops, &g);
   if (rc) return rc;
   if (!ops->transformable) return TALLY_ERR_UNSUPPORTED;
-  *n = candidate_configs(ctx, desc->kernel_id, (uint64_t)g.x * g.y * g.z, out, cap);
+  *n = candidate_configs(ctx, desc, (uint64_t)g.x * g.y * g.z, out, cap);
   return TALLY_OK;
 }
 
@@ -2392,7 +2433,7 @@ int choose_config(tally_sched *s, const BeWork &w, tally_config *cfg, int *profi
   if (e.cands.empty()) {
     tally_config tmp[64];
     const uint64_t total = (uint64_t)w.desc.grid.x * w.desc.grid.y * w.desc.grid.z;
-    uint32_t n = candidate_configs(ctx, w.desc.kernel_id, total, tmp, 64);
+    uint32_t n = candidate_configs(ctx, &w.desc, total, tmp, 64);
     if (n == 0) return TALLY_ERR_UNSUPPORTED;
     e.cands.assign(tmp, tmp + n);
     e.sum_ms.assign(n, 0.0);
@@ -2672,7 +2713,7 @@ int tally_sched_submit_be(tally_sched *s, uint32_t client, const tally_kernel_de
   if (config) {
     if (config->kind > 2 || (config->kind != 2 && config->param == 0)) return TALLY_ERR_INVALID_ARG;
     if (config->kind != 2 && !ops->transformable) return TALLY_ERR_UNSUPPORTED;
-    if (config->kind == 0 && config->param > s->ctx->max_workers[kernel->kernel_id]) return TALLY_ERR_INVALID_ARG;
+    if (config->kind == 0 && config->param > workers_at_most(s->ctx, kernel)) return TALLY_ERR_INVALID_ARG;
     w.config = *config;
   } else {
     if (!ops->transformable) return TALLY_ERR_UNSUPPORTED;

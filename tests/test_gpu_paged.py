@@ -298,6 +298,33 @@ def test_append_one_by_one_with_blocks_that_grow(env):
         _same(paged, cache, f"token {i}")
 
 
+@pytest.mark.parametrize("page", [16, 64, 128])
+def test_append_as_workers_of_its_own_variant(env, page):
+    """As many workers as are resident of the kernel that the sizes take, not of the largest; no more are accepted; the candidates
+    go up to them."""
+    B, ctx, torch = env
+    rng = np.random.default_rng(23)
+    n, kv, dim = 6000, 8, 128
+    table, pages = _deal(rng, [n], page)
+    cache, x = OP.empty_cache(pages, kv, page, dim), _bits(rng, (n, 2 * kv, dim))
+    paged, tx = _paged(B, torch, cache), _dev(torch, x)
+    cu, lens = _dev(torch, np.array([0, n], np.int32)), _dev(torch, np.array([n], np.int32))
+    kern = B.kv_append_fp8(tx[:, :kv], tx[:, kv:], cu, lens, _dev(torch, table), paged)
+    most, units = ctx.max_workers(kern), B.device_info()["num_cus"]
+    assert most == units if page == 128 else most >= (3 if page == 16 else 1) * units
+    configs = [c for c in ctx.candidate_configs(kern) if c[0] == B.CFG_PTB]
+    assert max(c[1] for c in configs) == min(most, kern.total_blocks)
+    with pytest.raises(B.TallyError) as e:
+        ctx.launch_ptb(kern, most + 1)
+    assert e.value.status == B.ERR_INVALID_ARG
+    torch.cuda.synchronize()
+    job = ctx.launch_ptb(kern, min(most, kern.total_blocks), coverage=True)
+    assert job.wait() == 3 and (job.coverage()["count"] == 1).all()
+    job.free()
+    torch.cuda.synchronize()
+    _same(paged, OP.append(obf16.decode(x[:, :kv]), obf16.decode(x[:, kv:]), [0, n], [n], table, cache))
+
+
 def test_append_skips_what_has_no_place(env):
     """Pages that do not exist, places before the first and behind the last page, sequences that are empty or out of order."""
     B, ctx, torch = env
