@@ -202,7 +202,7 @@ typedef struct {
  * overlap is undefined.  dim a multiple of 16 up to 512, rot a multiple of 16 up to dim.  freqs: rot / 2 fp32,
  * radians per position; positions: total int32, any; both in DEVICE memory.  magnitude 0 stands for 1; negative,
  * above 64 or not finite is refused.  ld_*: elements between tokens (multiples of 8, at most 2^20, 0: dense),
- * x and out 16-byte aligned, total at most 2^30 and total x heads at most 2^36.
+ * x and out 16-byte aligned, total at most 2^30.
  * Arithmetic: the product positions[t] * freqs[i], its sine and cosine in fp64 (angles up to 2^31 radians), which are
  * rounded to fp32; the products with x in fp32; the outputs are rounded once.
  * Logical grid: blocks of 1 to 32 tokens, by the sizes (tally_logical_grid), below 2^24. */
@@ -233,7 +233,8 @@ typedef struct {
  *   do not count for e;
  *   where e grows, the numbers held before the new ones are stored anew: divided by a power of two, so all are exact but those
  *   that fall below the smallest normal, which are rounded again.
- * k is turned in fp64 and rounded once, to its code (turned to 2^128 or more it counts as infinite).  So a call made twice leaves what it left the first time.
+ * k is turned in fp64 and rounded once, to its code (turned to 2^128 or more it counts as infinite).  A call made twice leaves
+ * what it left the first time.
  * What a page holds behind a sequence's last token, and pages that no new token goes to, stay as they are.  Tokens that
  * belong to no sequence, whose place is negative or beyond seq_pages x page, or whose page is none of 0 .. n_pages - 1,
  * are not stored.  cu_seqlens, lens, table, positions, freqs are DEVICE memory; values of cu_seqlens outside [0, total] count
@@ -259,7 +260,8 @@ typedef struct {
  * values outside [0, seq_pages x page] count as its ends.  What lies in pages behind lens does not reach the result, whatever
  * it is, nor do entries of the table behind it; an entry that is none of 0 .. n_pages - 1 stands for a page whose
  * tokens do not count.  ld_q, ld_out, scale and arithmetic as for TALLY_K_ATTN_PROMPT_BF16: what is stored in 8 bits enters the products
- * exactly, p is rounded to bf16 before the second one, and the sum is of the rounded ones.
+ * exactly (of v what lies below 2^-126 may be lost), p is rounded to bf16 before the second one, and the sum is of the
+ * rounded ones; q may be as large as 2^96.
  * scratch: caller-owned device memory of tally_attn_paged_scratch_bytes() bytes, 16-byte aligned; two calls that
  * may overlap need one each.  batch x heads at most 2^20, seq_pages x page at most 2^28, batch x seq_pages x page
  * at most 2^36, n_pages at most 2^30. */

@@ -439,9 +439,10 @@ struct AppendBodyT {
 // 1024 workgroups are what is on the GPU at once (us with 512 / 768 / 1024 / 2048: 32 sequences of up to 4096, 8 K/V heads, 36.6 36.0 34.4 34.6; 8 of up to
 // 131071 223 211 193 195; one of 32768 19.0 20.1 20.2 20.2).  A part has two strips at least (1 / 2 / 4: 16 of up to 3001, 4 K/V heads, 13.5 12.2 12.1; one of
 // 4096, 8 heads, 9.2 9.3 10.4).
-// One part a sequence saves the second kernel.  It pays up to 4 strips whatever the number of workgroups (4 sequences of 512, 12 heads of 64: 5.8, in two
-// parts 8.2; one of 1024, 8 heads, 9.9 and 9.2), up to 8 from 256 workgroups on (8 of 600, 32 heads, 10.8 and 12.1; with 64 of them, 8 of 1024, 8 heads,
-// 10.0 and 9.4), up to 16 from 512 on (64 of up to 2000, 8 heads, 32.8 and 34.9; with 128, 128 of 2000 on one head of 64, 14.3 and 12.2).  Eight waves a workgroup then: 6.2 for 5.8.
+// One part a sequence saves the second kernel.  It pays up to 4 strips whatever the number of workgroups (4 sequences of 512, 12 heads of 64:
+// 5.8, in two parts 8.2; one of 1024, 8 heads, 9.9 and 9.2), up to 8 from 256 workgroups on (8 of 600, 32 heads, 10.8 and 12.1; with 64 of them,
+// 8 of 1024, 8 heads, 10.0 and 9.4), up to 16 from 512 on (64 of up to 2000, 8 heads, 32.8 and 34.9; with 128, 128 of 2000 on one head of 64,
+// 14.3 and 12.2).  Eight waves a workgroup then: 6.2 for 5.8.
 // A row of the second kernel is a wave's where sequences have few parts, else a workgroup's (a wave / a workgroup: 64 of up to 1000, 3 parts, 19.9
 // 21.3; 64 of up to 8192, heads of 64, 3, 51.8 53.8; 32 of up to 4096, 5, 32.1 32.4; 16 of up to 3001, 17, 13.4 12.4; one of 32768 26.9 20.4).
 // Caches above 256 MB, which is what the Infinity Cache holds, are read past it (non-temporal; three caches in turn, ordinary / so: capacity 192 MB

@@ -469,6 +469,30 @@ def test_attention_scale_and_rising_scores(env, scale):
     assert (np.abs(got - want) <= bound).all()
 
 
+@pytest.mark.parametrize("dim,page", [(64, 16), (128, 64)])
+def test_attention_numbers_near_both_ends(env, dim, page):
+    """Large queries on tiny keys and the other way round, values up to 2^96 and down to the smallest that can be stored."""
+    B, ctx, torch = env
+    rng = np.random.default_rng(10)
+    lens = [40, 300]
+    table, pages = _deal(rng, lens, page)
+    cache, q = _filled(rng, pages, 4, page, dim), obf16.decode(_bits(rng, (2, 8, dim), 0.25))
+    for head, (by_k, by_v) in enumerate([(-95, 94), (94, -117), (-95, -110), (0, -100)]):   # powers of two, exponents 1 to 216
+        cache["k_exps"][:, head] = cache["k_exps"][:, head].astype(int) + by_k
+        cache["v_exps"][:, head] = cache["v_exps"][:, head].astype(int) + by_v
+        q[:, 2 * head:2 * head + 2] *= 2.0 ** -by_k
+    q = TI.to_bf16_bits(q.astype(np.float32))
+    assert cache["v_exps"].min() == 1 and np.abs(obf16.decode(q)).max() < 2.0 ** 96
+    want, mass = OP.attn_paged(obf16.decode(q), cache, table, lens)
+    got = obf16.decode(_attend(B, ctx, torch, q, cache, table, lens))
+    # each value and each product with a weight may lose 2^-126, the sum of the weights is 1 or more, and the output once more
+    tokens = np.array(lens)[:, None, None]
+    bound = 2.0 ** -8 * np.abs(want) + (2.0 ** -8 + 2.0 ** -12) * mass + (2 * tokens + 1) * 2.0 ** -126
+    assert (np.abs(got - want) <= bound).all()
+    large = np.abs(want) > 2.0 ** -110                     # not lost in that
+    assert large[:, :2].any() and large[:, 6:].any()
+
+
 def test_attention_pages_shared_by_sequences_and_rows_apart(env):
     """A prefix's pages in every row of the table, a table and q with padding between rows."""
     B, ctx, torch = env
