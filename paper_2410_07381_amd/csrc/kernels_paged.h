@@ -645,7 +645,8 @@ __global__ __launch_bounds__(256, 4) void attn_paged_partial(tally_attn_paged_ar
         s[u] = F::mma(wide(k[u][h].z, k[u][h].w, 1.f), q[2 * h + 1], s[u]);
       }
     }
-    const float by = c * __uint_as_float(ke << 23), v_by = __uint_as_float(ve << 23);
+    const float by = c * __uint_as_float(ke << 23);
+    float v_by = __uint_as_float(ve << 23);
     __builtin_amdgcn_sched_barrier(0);
     if (more) {                                            // (the registers of this tile's are free)
       ask_exps(next);
@@ -664,6 +665,7 @@ __global__ __launch_bounds__(256, 4) void attn_paged_partial(tally_attn_paged_ar
       const uint32_t lo = count >= 4 ? ~0u : (1u << 8 * count) - 1, hi = count >= 8 ? ~0u : count > 4 ? (1u << 8 * (count - 4)) - 1 : 0u;
 #pragma unroll
       for (int d = 0; d < DT; ++d) v[d].x &= lo, v[d].y &= hi;
+      v_by = count ? v_by : 1.f;                           // (of a page that does not exist it is another's, which may be anything)
       some |= __builtin_amdgcn_ballot_w64(count != 0) != 0;
     } else {
       some = true;

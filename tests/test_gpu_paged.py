@@ -420,6 +420,27 @@ def test_attention_pages_that_do_not_exist_and_lengths_out_of_range(env):
         assert (got[1] == 0).all()                         # (not one page of it)
 
 
+@pytest.mark.parametrize("page", [16, 64])
+def test_attention_page_0_does_not_stand_in(env, page):
+    """Entries that are no page, in a cache whose page 0 no sequence has and holds NaN, by codes and by exponents that are none."""
+    B, ctx, torch = env
+    rng = np.random.default_rng(11)
+    heads, kv, dim = 4, 2, 128
+    cache = _filled(rng, 5, kv, page, dim)
+    cache["k"][0], cache["v"][0] = 0x7F, 0x7F
+    cache["k_exps"][0], cache["v_exps"][0] = 255, 255
+    table = np.array([[1, 5, 2], [-1, 3, 4], [-1, -1, -1]], np.int32)
+    lens = [3 * page, 3 * page - 5, 2 * page]
+    q = _bits(rng, (3, heads, dim))
+    plain = {n: c.copy() for n, c in cache.items()}
+    for n in plain:
+        plain[n][0] = 120                                  # (nothing of it is looked at)
+    want, mass = OP.attn_paged(obf16.decode(q), plain, table, lens)
+    got = _attend(B, ctx, torch, q, cache, table, lens)
+    _attn_ok(got, want, mass)
+    assert (got[2] == 0).all()
+
+
 @pytest.mark.parametrize("tokens", [40, 1500])
 def test_attention_numbers_that_are_none(env, tokens):
     """A NaN among the keys of one head, among the values of a dim; scores of -inf throughout, of inf: the rows that the formula
