@@ -221,6 +221,8 @@ struct AppendBodyT {
           table[(t0 - u0 + j) * (DIM / 2) + lane % (DIM / 2)] = w;
           w = Turn{__builtin_fma(w.c, on.c, -(w.s * on.s)), __builtin_fma(w.s, on.c, w.c * on.s)};
         }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // (other lanes of the wave read them; its LDS accesses are in order)
+        __builtin_amdgcn_wave_barrier();
       }
     };
     float k[16];                                           // (k[e] and k[8 + e]: a pair)
