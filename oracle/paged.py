@@ -80,7 +80,8 @@ def append(k, v, cu, lens, table, cache, freqs=None, positions=None, interleaved
         new = {"k": k[first:last], "v": v[first:last]}
         if freqs is not None and count:
             at = places if positions is None else np.asarray(positions)[first:last]
-            new["k"] = rope(k[first:last], at, freqs, interleaved, False, magnitude)[0]
+            turned = rope(k[first:last], at, freqs, interleaved, False, magnitude)[0]
+            new["k"] = np.where(np.abs(turned) >= 2.0 ** 128, np.inf, turned)   # (beyond what a key may be: infinite)
         for p in sorted({int(t) // page for t in places if 0 <= t < cap}):
             here = [i for i, t in enumerate(places) if t >= 0 and t // page == p]
             at, of = int(table[s, p]), int(places[here[0]]) % page

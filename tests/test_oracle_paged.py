@@ -136,3 +136,18 @@ def test_attention_over_pages_is_attention_over_a_row_of_tokens():
     none = np.zeros((0, kv, dim))
     want, want_mass = OS.attn_prefix(q, none, none, own["k"], own["v"], lens)
     assert np.allclose(out, want) and np.allclose(mass, want_mass) and (out[1] == 0).all()
+
+
+def test_keys_that_turn_past_the_largest_count_as_infinite():
+    """2^128 and beyond, by the turn or by the magnitude: NaN in the cache, and not counted for the block's exponent."""
+    big, k = 1.5 * 2.0 ** 127, np.zeros((3, 1, 16))
+    k[0, 0, 0], k[0, 0, 8] = big, big                      # a turn by 1: sum and difference, 1.38 and 0.30 times as much
+    k[1, 0, 1] = 2.0 ** 127                                # twice that is 2^128 itself
+    k[2, 0, 2] = 2.0 ** 127 * (1 - 2.0 ** -8)              # and this stays below
+    freqs, table = np.array([1.0, 0, 0, 0, 0, 0, 0, 0]), np.array([[0]])
+    got = OP.append(k, k, [0, 3], [3], table, OP.empty_cache(1, 1, 16, 16), freqs, [1, 0, 0], magnitude=2.0)
+    x = OP.CODES[got["k"][0, 0]] * 2.0 ** (got["k_exps"][0, 0] - 127.0)
+    a = 2 * big * (np.sin(1.0) + np.cos(1.0))
+    assert a >= 2.0 ** 128 and 2 * big * (np.sin(1.0) - np.cos(1.0)) < 2.0 ** 128
+    assert np.isnan(x[0, 8]) and np.isfinite(x[0, 0]) and np.isnan(x[1, 1]) and np.isfinite(x[2]).all() and x[2, 2] == 2.0 ** 128
+    assert got["k_exps"][0, 0] == OP.block_exp(np.array([2.0 ** 128 * (1 - 2.0 ** -8)]))
