@@ -243,7 +243,7 @@ typedef struct {
  * pages 16-byte aligned; ld_k, ld_v as ld_* above; total at most 2^30, n_pages at most 2^30, seq_pages x page at most 2^28.
  * Logical grid, below 2^32 threads in all (tally_logical_grid): of the total / page + 2 n_seqs slots sequence s has those from
  * cu_seqlens[s] / page + 2 s on, for the pages that its new tokens go to; a block has one slot or up to four, and one K/V head or
- * up to four, by the sizes. */
+ * two, by the sizes. */
 typedef struct {
   const uint16_t *k; const uint16_t *v; const int32_t *cu_seqlens; const int32_t *lens; const int32_t *table;
   const float *freqs; const int32_t *positions;

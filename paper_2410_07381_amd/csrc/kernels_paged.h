@@ -46,12 +46,15 @@ constexpr uint32_t kUnit = 16;                             // tokens side by sid
 // of 16, 64 x 1 6.4 / 6.2, 64 x 2 7.0 / 8.4, 200 x 2 12.3 / 11.6.  Kinds 0 / 1 / 4: pages of 128, 64 x 2 20.8 / 8.4 / 7.0, 64 x 8 21.3 / 9.8 / 7.1, 200 x 4
 // 59.6 / 12.5 / 14.9; of 64, 64 x 4 12.3 / 8.6 / 6.7, 64 x 8 (kind 0 from here on) 11.6 / 10.8.  127 x 1 and 380 tokens of one sequence, pages of 128:
 // kind 1 46, kind 4 16.
-// Heads a wave goes through, 1 / 2 / 4 / 8, one prompt, pages of 16: 7000 tokens 13.5 13.9 16.3 23.6; 13504 21.3 20.9 21.4 26.1; 22000 36.7 33.9
-// 36.2 35.5; 32768 51.5 47.4 46.1 46.0; 38229 60.1 55.5 57.7 66.2; 54613 82.9 75.4 76.8 79.0.  Fewer heads are more workgroups: 8 are best where
-// their number is just what fits on the GPU at once, and the worst a little beyond.
+// Heads a wave goes through, 1 / 2, one prompt: pages of 16, 7000 tokens 13.5 / 14.2, 8192 14.5 / 12.9, 13504 21.2 / 19.9, 20000 33.4 / 30.0; of 64,
+// 14.7 / 15.7, 15.4 / 13.6, 22.9 / 23.5, 35.6 / 32.9; of 128, 15.5 / 16.6, 17.2 / 16.2, 28.4 / 25.4, 41.7 / 41.5.  2 / 4: pages of 16 and 32, 32768
+// tokens 45.6 / 45.7, 38229 53.5 / 57.3, 54613 73.0 / 76.2, 65536 85.3 / 85.0; of 64, 49.7 / 47.3, 58.3 / 57.9, 78.6 / 78.0, 91.6 / 87.9; of 128, 56.3 / 53.6,
+// 67.2 / 72.0, 91.3 / 94.7, 104.8 / 99.9.  Pages of 16 and 32 never want four, those of 64 and 128 now two and now four,
+// which no size of a call tells beforehand; and with up to four a worker needs 133 to 137 registers, with up to two 120 to 127 (32768 tokens as workers, pages of 64 69.8 and 63.6, of 128
+// 79.1 and 62.1).
 // Tried: 16 tokens of a head of 128 a wave (194 registers, two waves per SIMD; 32768 tokens 47 to 55), the next head's numbers asked for ahead (pages
 // of 128 51 and 48, others the same, registers spilled in workers), a page's id and old bytes asked for earlier (64 tokens 6.4).
-constexpr uint64_t kAppendPieces = 8192;                   // from so many on a wave has two heads, from four times as many on four
+constexpr uint64_t kAppendPieces = 8192;                   // from so many on a wave has two heads
 __host__ __device__ constexpr uint32_t append_tokens(uint32_t dim) { return 1024 / dim; }   // of a piece
 __host__ __device__ inline uint32_t append_kind(const tally_kv_append_args &a) {
   const uint64_t n = a.n_seqs;
@@ -71,7 +74,7 @@ inline uint64_t append_slots(const tally_kv_append_args &a) { return (uint64_t)a
 __host__ __device__ inline uint32_t append_heads(const tally_kv_append_args &a) {
   const uint64_t pieces = (uint64_t)a.total / append_tokens(a.dim) * a.kv_heads;
   uint32_t h = 1;
-  while (append_kind(a) == 0 && h < 4 && 2 * h <= a.kv_heads && pieces >= kAppendPieces * h * h) h *= 2;
+  if (append_kind(a) == 0 && a.kv_heads > 1 && pieces >= kAppendPieces) h = 2;   // (a branch: the compiler then has code for each)
   return h;
 }
 inline uint64_t append_blocks(const tally_kv_append_args &a) {
