@@ -1,0 +1,54 @@
+"""GPU tests of the paged 8-bit cache at the ends of what it takes: turned keys of every size, memory beside the tensors, scores
+of hundreds.  Helpers and tolerances are those of test_gpu_paged.py; codes and exponents are the oracle's."""
+import numpy as np
+import pytest
+
+import tally_inputs as TI
+from oracle import bf16 as obf16
+from oracle import paged as OP
+from test_gpu_paged import SENTINEL, _attn_ok, _bits, _cache, _deal, _dev, _filled, _host, _paged, _run, _same, env  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+# new tokens of each sequence (dim, page) that take each way of appending: one wave a page, four waves a page, whole prompts
+KINDS = [(1, 128, 128), (1, 64, 16), (5, 128, 128), (9, 64, 128), (16, 128, 16), (33, 128, 128), (40, 64, 64), (70, 64, 32)]
+
+
+@pytest.mark.parametrize("form", ["hi", "ptb"])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("new,dim,page", KINDS)
+def test_append_turned_keys_next_to_borders_of_tiny_codes(env, new, dim, page, interleaved, form):
+    """Keys that the turn takes from a border of two codes to beside it, in blocks of each of the lowest exponents: where numbers
+    are subnormal in 32 bits that has to be known still when they are rounded to their code.  (The borders of a block lie within
+    2^18.8 of one another, so a partner times 2^-24 to 2^-34 is above 2^-53 of the key: both sides' 64 bits see it.)"""
+    B, ctx, torch = env
+    rng = np.random.default_rng(new + dim)
+    exps = np.arange(1, 13)
+    n, kv, half = len(exps), 2, dim // 2
+    borders = (OP.CODES[:126] + OP.CODES[1:127]) / 2
+    # (bf16 has no numbers as small as the smallest border: the magnitude brings them down)
+    magnitude = 2.0 ** -16
+    x = np.zeros((n * new, 2 * kv, dim))
+    sign = lambda s: rng.choice([-1.0, 1.0], s)
+    for s, e in enumerate(exps):
+        shape = (new, kv, dim)
+        low = rng.random(shape) < 0.6                      # the borders of subnormal codes, and all others
+        x[s * new:(s + 1) * new, :kv] = np.where(low, borders[rng.integers(0, 8, shape)], borders[rng.integers(0, 126, shape)]) * sign(shape) * 2.0 ** (e - 127.0) / magnitude
+        x[s * new, :kv, 0] = 448 * 2.0 ** (e - 127.0) / magnitude   # the block's largest, alone in its pair
+        x[s * new, :kv, 1 if interleaved else half] = 0
+    x[:, kv:] = rng.standard_normal((n * new, kv, dim))
+    bits = TI.to_bf16_bits(x.astype(np.float32))
+    assert (obf16.decode(bits[:, :kv]) == x[:, :kv]).all()
+    freqs = (2.0 ** -(24.0 + np.arange(half) % 11)).astype(np.float32)
+    freqs[0] = 0
+    held = rng.integers(0, page, n)
+    cu, lens = (np.arange(n + 1) * new).astype(np.int32), (held + new).astype(np.int32)
+    table, pages = _deal(rng, lens, page)
+    cache = _cache(rng, pages, kv, page, dim, 1, 1)        # (held numbers do not raise the exponent)
+    at = sign(n * new).astype(np.int32)
+    want = OP.append(obf16.decode(bits[:, :kv]), obf16.decode(bits[:, kv:]), cu, lens, table, cache, freqs, at, interleaved, magnitude)
+    assert set(exps) <= set(want["k_exps"].ravel())
+    paged, tx = _paged(B, torch, cache), _dev(torch, bits)
+    _run(ctx, torch, B.kv_append_fp8(tx[:, :kv], tx[:, kv:], _dev(torch, cu), _dev(torch, lens), _dev(torch, table), paged, _dev(torch, freqs),
+                                     _dev(torch, at), interleaved, magnitude), form)
+    _same(paged, want, form)
