@@ -2133,9 +2133,10 @@ int tally_select_config(const tally_config *c, uint32_t n, double threshold_ms) 
 namespace {
 
 ProfileKey profile_key(const tally_kernel_desc *d) {
-  // (a question about a descriptor that no launch would take has no entry, and nothing of it is read)
+  // (a question about a descriptor that no launch would take has no entry, and no sizes are made of what it has: they divide by some of it)
   const KernelOps *ops = d->kernel_id < TALLY_K_COUNT ? &kOps[d->kernel_id] : nullptr;
-  const bool read = ops && ops->sizes && d->args && d->args_size == ops->args_size;
+  tally_dim3 g, b;
+  const bool read = ops && ops->sizes && d->args && d->args_size == ops->args_size && ops->grid(d->args, &g, &b) == TALLY_OK;
   return std::make_tuple(d->kernel_id, d->grid.x, d->grid.y, d->grid.z, d->block.x, read ? ops->sizes(d->args) : CallSizes{});
 }
 

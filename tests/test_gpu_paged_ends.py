@@ -52,3 +52,21 @@ def test_append_turned_keys_next_to_borders_of_tiny_codes(env, new, dim, page, i
     _run(ctx, torch, B.kv_append_fp8(tx[:, :kv], tx[:, kv:], _dev(torch, cu), _dev(torch, lens), _dev(torch, table), paged, _dev(torch, freqs),
                                      _dev(torch, at), interleaved, magnitude), form)
     _same(paged, want, form)
+
+
+def test_questions_about_calls_that_are_refused(env):
+    """The profiler's records of descriptors that no launch takes, of sizes that stand below a division among them: there are none."""
+    B, ctx, torch = env
+    import ctypes as C
+    ctx.profile_reset()
+    args = dict(k=4096, v=4096, cu_seqlens=4096, lens=4096, table=4096, k_pages=4096, v_pages=4096, k_exps=4096, v_exps=4096, total=1000, n_seqs=3, kv_heads=2,
+                dim=64, page=16, n_pages=100, seq_pages=40)
+    for bad in (dict(dim=0), dict(dim=2048), dict(page=0), dict(n_seqs=0), dict(total=0), dict(k=None)):
+        a = B.KvAppendArgs(**dict(args, **bad))
+        with pytest.raises(B.TallyError):
+            B.logical_grid(B.K_KV_APPEND_FP8, a)
+        kern = B.Kernel.__new__(B.Kernel)
+        kern.args, kern.desc = a, B.KernelDesc(B.K_KV_APPEND_FP8, B.Dim3(10, 1, 1), B.Dim3(256, 1, 1), C.addressof(a), C.sizeof(a))
+        assert ctx.lookup_config(kern) is None and ctx.profile_table(kern) == ([], -1)
+        with pytest.raises(B.TallyError):
+            ctx.launch_native(kern)
