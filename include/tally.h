@@ -526,9 +526,10 @@ int tally_select_config(const tally_config *cands, uint32_t n, double threshold_
 /* Measure every candidate configuration of a kernel on the best-effort stream (`runs`
  * timed executions each, after one warm-up; the kernel really runs, so its outputs are
  * written `runs`+1 times per candidate), fill latency and turnaround, choose under
- * threshold_ms and cache the choice per (kernel, grid, block), for prompts and 4-bit products also
- * per sizes (m, k, group and whether there are zero points; n_seqs, heads, kv_heads, dim): their grids are the same
- * for very different work.  cands: in/out array.
+ * threshold_ms and cache the choice per (kernel, grid, block), for some kernels also per what a block's work depends on, since
+ * their grids are the same for very different work: 4-bit products (m, k, group and whether there are zero points), prompts
+ * (n_seqs, heads, kv_heads, dim), rotary positions (heads, dim, rot, the pairs' layout, tokens of a block), appending to the paged
+ * cache (n_seqs, kv_heads, dim, page, rot, the pairs' layout, whether there are positions, heads of a block).  cands: in/out array.
  * Turnaround of a persistent-worker candidate is Eq. 1; for a kernel whose workers pause
  * inside their blocks while preempted (and with the pause enabled, see
  * tally_set_yield_bound_us) it is the time of ONE block times the share of a block

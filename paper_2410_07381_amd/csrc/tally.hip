@@ -101,7 +101,8 @@ struct KernelOps {
   // the original form's kernel depends on what else is on the GPU
   bool chooses;
   // what a block's time depends on and the grid does not say (null: nothing that keeps measurements apart).  Not the
-  // exact rows and tokens: prompts that differ by a few tokens share what was measured
+  // exact rows and tokens: prompts that differ by a few tokens share what was measured where they have as many blocks (of
+  // rotary positions below 2048 tokens none do: a block is a token)
   CallSizes (*sizes)(const void *args);
   // where the workers of one operator are so different that the largest must not stand for all: which of `worker_kernels`
   // kernels the arguments take (null: one stands for all), and what one of its workgroups occupies and how many are resident
@@ -748,12 +749,14 @@ int occupancy_append_of(uint32_t kernel, int *blocks_per_cu) {
 CallSizes rope_sizes(const void *args) {
   tally_rope_args a;
   memcpy(&a, args, sizeof(a));
-  return {a.heads, a.dim, a.rot, a.flags & TALLY_ROPE_INTERLEAVED};
+  return {a.heads, a.dim, a.rot, rope_tokens(a) | (a.flags & TALLY_ROPE_INTERLEAVED ? 1u << 8 : 0u)};
 }
 CallSizes append_sizes(const void *args) {
   tally_kv_append_args a;
   memcpy(&a, args, sizeof(a));
-  return {a.n_seqs, a.kv_heads, a.dim, a.page | append_kind(a) << 16};
+  // (positions of their own: a sine and cosine for each token, where neighbours are turned on from one to the next)
+  const uint32_t turns = a.rot ? a.rot | (a.flags & TALLY_ROPE_INTERLEAVED ? 1u << 8 : 0u) | (a.positions ? 1u << 9 : 0u) : 0u;
+  return {a.n_seqs, a.kv_heads, a.dim | turns << 16, a.page | append_heads(a) << 8 | append_kind(a) << 16};
 }
 hipError_t launch_native_prefix(hipStream_t s, const void *args, tally_dim3, uint32_t how) {
   return launch_attn_prefix(s, args, how & kUrgent);

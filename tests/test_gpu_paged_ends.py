@@ -70,3 +70,36 @@ def test_questions_about_calls_that_are_refused(env):
         assert ctx.lookup_config(kern) is None and ctx.profile_table(kern) == ([], -1)
         with pytest.raises(B.TallyError):
             ctx.launch_native(kern)
+
+
+def test_measurements_of_blocks_with_different_work_are_kept_apart(env):
+    """Calls whose grids are equal and whose blocks' work is not: how many tokens or heads a block goes through, what is turned
+    and from what.  One call's records and choice are not another's."""
+    B, ctx, torch = env
+    z = lambda *s: torch.zeros(s, dtype=torch.int16, device="cuda")
+
+    def rope(total, dim, rot, **how):
+        x = z(total, 8, dim)
+        return B.rope_bf16(x, x, torch.zeros(rot // 2, device="cuda"), torch.zeros(total, dtype=torch.int32, device="cuda"), **how)
+
+    def append(total, rot, kv=8, dim=128, page=16, at=False, **how):
+        x, cache = z(total, 2 * kv, dim), B.PagedCache.empty(-(-total // page), kv, page, dim)
+        ints = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")
+        return B.kv_append_fp8(x[:, :kv], x[:, kv:], ints(0, total), ints(total), torch.arange(len(cache.k), dtype=torch.int32, device="cuda")[None],
+                               cache, torch.zeros(rot // 2, device="cuda") if rot else None,
+                               torch.zeros(total, dtype=torch.int32, device="cuda") if at else None, **how)
+    # 1500 blocks of a token, and 3000 tokens in blocks of two; a head a wave, and two
+    calls = [[rope(1500, 64, 64), rope(3000, 64, 64), rope(1500, 64, 32), rope(1500, 64, 64, interleaved=True), rope(1500, 128, 64)],
+             [append(480, 128), append(480, 0), append(480, 64), append(480, 128, interleaved=True), append(480, 128, at=True)],
+             [append(8192 + 16, 128), append(4112 - 16, 128), append(8192 + 16, 0)]]
+    ctx.profile_reset()
+    torch.cuda.synchronize()
+    for same in calls:
+        for i, kern in enumerate(same):
+            assert kern.desc.grid.x == same[0].desc.grid.x
+            for later in same[i:]:
+                assert ctx.profile_table(later) == ([], -1) and ctx.lookup_config(later) is None
+            ctx.profile(kern, [(B.CFG_PTB, 4, 1), (B.CFG_SLICED, 1 + i, 1)], runs=1)
+        assert [ctx.profile_table(k)[0][1]["param"] for k in same] == [1 + i for i in range(len(same))]
+    assert len(ctx.profile_table(append(475, 128))[0]) == 2   # (a few tokens fewer: the same blocks)
+    ctx.profile_reset()
