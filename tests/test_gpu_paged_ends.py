@@ -6,7 +6,7 @@ import pytest
 import tally_inputs as TI
 from oracle import bf16 as obf16
 from oracle import paged as OP
-from test_gpu_paged import SENTINEL, _attn_ok, _bits, _cache, _deal, _dev, _filled, _host, _paged, _run, _same, env  # noqa: F401
+from test_gpu_paged import SENTINEL, _attend, _attn_ok, _bits, _cache, _deal, _dev, _filled, _host, _paged, _run, _same, env  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -103,3 +103,50 @@ def test_measurements_of_blocks_with_different_work_are_kept_apart(env):
         assert [ctx.profile_table(k)[0][1]["param"] for k in same] == [1 + i for i in range(len(same))]
     assert len(ctx.profile_table(append(475, 128))[0]) == 2   # (a few tokens fewer: the same blocks)
     ctx.profile_reset()
+
+
+def _steep(rng, pattern, n):
+    """Scores of n tokens for the first query head: hundreds, in an order that a running maximum can go wrong with."""
+    low = rng.uniform(-200, -150, n)
+    if pattern == "rising":
+        return np.linspace(-300, 300, n)
+    if pattern == "falling":
+        return np.linspace(300, -300, n)
+    if pattern == "steps":                                 # from one tile of 32 tokens to the next, up and far down
+        return np.array([200.0, 250, 300, -175, -200])[np.arange(n) // 32 % 5]
+    at = {"first": [2], "last": [n - 2], "one wave": [n // 256 * 128 + 64 + 7], "ends": [1, n - 1], "a tile": range(n - 40, n - 30)}[pattern]
+    low[list(at)] = 300
+    return low
+
+
+@pytest.mark.parametrize("pattern", ["first", "last", "one wave", "ends", "a tile", "steps", "rising", "falling"])
+@pytest.mark.parametrize("n", [400, 1300, 4000])
+@pytest.mark.parametrize("dim,page", [(64, 16), (128, 64)])
+def test_attention_scores_of_hundreds(env, dim, page, n, pattern):
+    """Scores from -300 to 300: weights that vanish beside a later maximum, waves and parts whose state as a whole does.  400 tokens are
+    one part, 1300 six parts (a wave merges a row), 4000 sixteen (a workgroup does)."""
+    B, ctx, torch = env
+    rng = np.random.default_rng(n + dim)
+    heads, scale = 4, 0.125
+    table, pages = _deal(rng, [n], page)
+    cache = _filled(rng, pages, 1, page, dim)
+    assert (B.attn_paged_scratch_bytes(1, heads, 1, dim, page, table.shape[1]) == 0) == (n == 400)
+    q = rng.uniform(0.5, 1.5, (1, heads, dim)) * rng.choice([-1.0, 1.0], (1, heads, dim))
+    q[0, 1], q[0, 2] = -q[0, 0], q[0, 0] * 0.25            # the other way round, and less steep; the last one is its own
+    bits = TI.to_bf16_bits(q.astype(np.float32))
+    q = obf16.decode(bits)
+    k = _steep(rng, pattern, n)[:, None] * np.sign(q[0, 0]) / (scale * np.abs(q[0, 0]).sum()) * rng.uniform(0.75, 1.25, (n, dim))
+    # (the pages are then filled as an append fills them)
+    x = TI.to_bf16_bits(np.stack([k, rng.standard_normal((n, dim))], 1).astype(np.float32))
+    x = obf16.decode(x)
+    cache = OP.append(x[:, :1], x[:, 1:], [0, n], [n], table, cache)
+    want, mass = OP.attn_paged(q, cache, table, [n], scale)
+    codes, _ = OP.tokens_of(cache, "k", table[0], n)
+    scores = scale * codes[:, 0] @ q[0].T
+    size = scale * (np.abs(codes[:, 0]) @ np.abs(q[0]).T).max()
+    assert scores[:, 0].max() > 250 and np.ptp(scores[:, 0]) > 400 and size < 400
+    got = _attend(B, ctx, torch, bits, cache, table, [n], scale=scale)
+    # fp32's error of a score, dim + 3 roundings of at most `size`, is one of its weight; of the sums too
+    bound = 2.0 ** -8 * np.abs(want) + (2.0 ** -8 + 2.0 ** -12 + 2 * (dim + 3) * 2.0 ** -24 * size) * mass
+    err = np.abs(obf16.decode(got) - want)
+    assert (err <= bound).all(), f"worst {(err / bound).max():.2f} bounds"
