@@ -54,6 +54,41 @@ def test_append_turned_keys_next_to_borders_of_tiny_codes(env, new, dim, page, i
     _same(paged, want, form)
 
 
+@pytest.mark.parametrize("magnitude", [1.0, 1.2, 64.0])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("new,dim,page", KINDS)
+def test_append_turned_numbers_of_every_size(env, new, dim, page, interleaved, magnitude):
+    """Keys from zeros to the largest, NaN and infinities among them, turned: what comes to 2^128 or more is infinite, stored as NaN and
+    not counted for the block; what stays below is."""
+    B, ctx, torch = env
+    rng = np.random.default_rng(new + 2 * dim)
+    tops = [0.0, 2.0 ** -133, 2.0 ** -126, 1.75, 448.0, 2.0 ** 120, 2.0 ** 127, 3.3e38]
+    n, kv, half = len(tops), 2, dim // 2
+    pair = (lambda i: (2 * i, 2 * i + 1)) if interleaved else (lambda i: (i, i + half))
+    x = np.clip(rng.standard_normal((n * new, 2 * kv, dim)) / 2, -1, 1)
+    for s, top in enumerate(tops):
+        x[s * new:(s + 1) * new] *= top
+        x[s * new, :, pair(3)[0]] = x[s * new, :, pair(3)[1]] = top   # (turned, one of them grows and one falls)
+    bits = TI.to_bf16_bits(x.astype(np.float32))
+    for s, (head, d, b) in enumerate(((0, 7, 0x7F80), (1, 9, 0xFF80), (0, dim - 1, 0x7FC0), (1, 0, 0xFFC0))):
+        bits[(2 * s + 1) * new - 1, head, d] = b           # the last token of every other sequence
+        bits[(2 * s + 1) * new - 1, kv + head, d] = b
+    freqs = (0.9 ** np.arange(half)).astype(np.float32)
+    held = rng.integers(0, page, n)
+    cu, lens = (np.arange(n + 1) * new).astype(np.int32), (held + new).astype(np.int32)
+    table, pages = _deal(rng, lens, page)
+    cache = _cache(rng, pages, kv, page, dim, 1, 130)
+    by = float(np.float32(magnitude))
+    with np.errstate(invalid="ignore", over="ignore"):
+        want = OP.append(obf16.decode(bits[:, :kv]), obf16.decode(bits[:, kv:]), cu, lens, table, cache, freqs, None, interleaved, by)
+        turned = np.abs(OP.rope(obf16.decode(bits[:, :kv]), np.concatenate([np.arange(h, h + new) for h in held]), freqs, interleaved, False, by)[0])
+    assert ((turned >= 2.0 ** 128) & np.isfinite(turned)).any()
+    paged, tx = _paged(B, torch, cache), _dev(torch, bits)
+    _run(ctx, torch, B.kv_append_fp8(tx[:, :kv], tx[:, kv:], _dev(torch, cu), _dev(torch, lens), _dev(torch, table), paged, _dev(torch, freqs),
+                                     interleaved=interleaved, magnitude=magnitude), "hi")
+    _same(paged, want)
+
+
 def test_questions_about_calls_that_are_refused(env):
     """The profiler's records of descriptors that no launch takes, of sizes that stand below a division among them: there are none."""
     B, ctx, torch = env
@@ -150,3 +185,99 @@ def test_attention_scores_of_hundreds(env, dim, page, n, pattern):
     bound = 2.0 ** -8 * np.abs(want) + (2.0 ** -8 + 2.0 ** -12 + 2 * (dim + 3) * 2.0 ** -24 * size) * mass
     err = np.abs(obf16.decode(got) - want)
     assert (err <= bound).all(), f"worst {(err / bound).max():.2f} bounds"
+
+
+def _amid(torch, a, fill, beside=1 << 16):
+    """A tensor in the middle of a larger one that is filled otherwise; and that one."""
+    t = _dev(torch, a)
+    n = beside // t.element_size()
+    whole = torch.full((t.numel() + 2 * n,), fill, dtype=t.dtype, device="cuda")
+    whole[n:-n] = t.view(-1)
+    return whole[n:-n].view(t.shape), whole
+
+
+def _beside_is(whole, fill, beside=1 << 16):
+    n = beside // whole.element_size()
+    return bool((whole[:n] == fill).all()) and bool((whole[-n:] == fill).all())
+
+
+# tokens of each sequence, so that a page is one wave's, four waves', or all its pieces have a wave; the last two with two heads a wave
+PLACES = [(1, 64, 16, 2), (1, 128, 128, 3), (5, 128, 128, 2), (9, 64, 128, 3), (7, 128, 64, 1), (19, 64, 16, 3), (70, 64, 64, 2), (150, 128, 128, 2), (67, 128, 32, 5),
+          (800, 128, 16, 7), (1500, 64, 64, 7)]
+
+
+@pytest.mark.parametrize("form", ["hi", "be", "sliced", "ptb"])
+@pytest.mark.parametrize("new,dim,page,kv", PLACES)
+def test_append_touches_its_places_alone(env, new, dim, page, kv, form):
+    """Pages that do not exist, places before the first and behind the last page, lengths and ends of sequences out of range: what has no place
+    is not stored, and the bytes before and behind the pages and exponents stay as they are.  Around k and v there are NaN."""
+    B, ctx, torch = env
+    rng = np.random.default_rng(new + page)
+    n, wide = 13, -(-new // page) + 2
+    cu = (np.arange(n + 1) * new).astype(np.int32)
+    total = int(cu[-1])
+    cu[0], cu[-1] = -9, 1 << 30
+    lens = np.full(n, new, np.int64) + rng.integers(0, page, n)
+    table = np.full((n, wide), -1, np.int64)
+    ids = iter(rng.permutation(n * wide))
+    for s in range(n):
+        table[s] = [next(ids) for _ in range(wide)]
+    pages, at = n * wide + 2, (lens - 1) // page            # (two that are nobody's; the last token's)
+    for s, none in ((1, -1), (2, pages), (3, 1 << 30), (4, -(1 << 31)), (5, (1 << 31) - 1)):
+        table[s, at[s]] = none
+    lens[6], lens[7], lens[8] = new // 2, wide * page + new // 2, 0
+    lens[9], lens[10], lens[11] = -7, 1 << 30, (1 << 31) - 1
+    lens, table = lens.astype(np.int32), table.astype(np.int32)
+    cache, x = _cache(rng, pages, kv, page, dim), _bits(rng, (total, 2 * kv, dim))
+    freqs = (10000.0 ** (-np.arange(dim // 2) / (dim // 2))).astype(np.float32)
+    places = rng.integers(0, 1 << 20, total).astype(np.int32) if form in ("be", "ptb") else None
+    parts = {m: _amid(torch, cache[m], 0x5A) for m in ("k", "v", "k_exps", "v_exps")}
+    paged = B.PagedCache(*(parts[m][0] for m in ("k", "v", "k_exps", "v_exps")))
+    tx, whole_x = _amid(torch, x, 0x7FC0)
+    tt, _ = _amid(torch, table, pages - 1)
+    kern = B.kv_append_fp8(tx[:, :kv], tx[:, kv:], _dev(torch, cu), _dev(torch, lens), tt, paged, _dev(torch, freqs),
+                           None if places is None else _dev(torch, places), interleaved=kv % 2 == 0)
+    want = OP.append(obf16.decode(x[:, :kv]), obf16.decode(x[:, kv:]), cu, lens, table, cache, freqs, places, kv % 2 == 0)
+    assert all((want["k"][p] == cache["k"][p]).all() for p in (pages - 2, pages - 1)) and (want["k"] != cache["k"]).any()
+    _run(ctx, torch, kern, form)
+    _same(paged, want, form)
+    assert all(_beside_is(parts[m][1], 0x5A) for m in parts) and _beside_is(whole_x, 0x7FC0)
+    assert (_host(tx) == x).all() and (_host(tt) == table).all()
+
+
+@pytest.mark.parametrize("form", ["hi", "ptb"])
+@pytest.mark.parametrize("new,dim,page,kv", PLACES[::2])
+def test_append_whatever_the_indexes_hold(env, new, dim, page, kv, form):
+    """Ends of sequences in no order, any lengths, any table, of which only the pages of the pool may be written."""
+    B, ctx, torch = env
+    rng = np.random.default_rng(new + 3 * page)
+    n, wide, pages = 13, 5, 30
+    total = n * new
+    cache, x = _cache(rng, pages, kv, page, dim), _bits(rng, (total, 2 * kv, dim))
+    parts = {m: _amid(torch, cache[m], 0x5A) for m in ("k", "v", "k_exps", "v_exps")}
+    paged = B.PagedCache(*(parts[m][0] for m in ("k", "v", "k_exps", "v_exps")))
+    tx, _ = _amid(torch, x, 0x7FC0)
+    any_int = lambda shape, most: np.where(rng.random(shape) < 0.3, rng.integers(-(1 << 31), 1 << 31, shape), rng.integers(-3, most, shape)).astype(np.int32)
+    for _ in range(3):
+        cu, lens, table = any_int(n + 1, total + 3), any_int(n, wide * page + 3), any_int((n, wide), pages + 3)
+        _run(ctx, torch, B.kv_append_fp8(tx[:, :kv], tx[:, kv:], _dev(torch, cu), _dev(torch, lens), _dev(torch, table), paged), form)
+        assert all(_beside_is(parts[m][1], 0x5A) for m in parts) and (_host(tx) == x).all()
+
+
+@pytest.mark.parametrize("lens,heads,kv,dim,page,more", [
+    ([1300], 3, 1, 64, 16, 0), ([4000], 2, 2, 128, 64, 0), ([900, 33], 40, 1, 128, 16, 0), ([0, 5, 3000], 28, 4, 128, 32, 3), ([700 + i for i in range(40)], 8, 8, 64, 64, 40),
+    ([40, 300], 12, 12, 64, 16, 400)])
+def test_attention_stays_within_its_scratch(env, lens, heads, kv, dim, page, more):
+    """Scratch of the very size that is asked for, pages and table in the middle of others: nothing beside them is written or counts."""
+    B, ctx, torch = env
+    rng = np.random.default_rng(len(lens) + heads)
+    table, pages = _deal(rng, lens, page, more=more)
+    cache, q = _filled(rng, pages, kv, page, dim), _bits(rng, (len(lens), heads, dim))
+    size = B.attn_paged_scratch_bytes(len(lens), heads, kv, dim, page, table.shape[1])
+    assert size > 0
+    scratch, whole = _amid(torch, np.full(size, 0xFF, np.uint8), 0x5A)
+    paged = B.PagedCache(*(_amid(torch, cache[m], f)[0] for m, f in (("k", 0x7F), ("v", 0x7F), ("k_exps", 255), ("v_exps", 255))))
+    out, whole_out = _amid(torch, np.full((len(lens), heads, dim), SENTINEL, np.uint16), SENTINEL)
+    _run(ctx, torch, B.attn_paged_fp8(_amid(torch, q, 0x7FC0)[0], paged, _amid(torch, table, 0)[0], _dev(torch, np.array(lens, np.int32)), out, scratch), "hi")
+    _attn_ok(_host(out), *OP.attn_paged(obf16.decode(q), cache, table, lens))
+    assert _beside_is(whole, 0x5A) and _beside_is(whole_out, SENTINEL)
