@@ -240,7 +240,7 @@ typedef struct {
  * are not stored.  cu_seqlens, lens, table, positions, freqs are DEVICE memory; values of cu_seqlens outside [0, total] count
  * as its ends, nothing outside the tensors is touched whatever they hold.
  * dim 64 or 128; rot a multiple of 16 up to dim (0: freqs and positions are not looked at); magnitude as above; k, v and the
- * pages 16-byte aligned; ld_k, ld_v as ld_* above; total at most 2^30, n_pages at most 2^30, seq_pages x page at most 2^28.
+ * pages 16-byte aligned; ld_k, ld_v as ld_* above; total at most 2^30, n_seqs at most 2^24, n_pages at most 2^30, seq_pages x page at most 2^28.
  * Logical grid, below 2^32 threads in all (tally_logical_grid): of the total / page + 2 n_seqs slots sequence s has those from
  * cu_seqlens[s] / page + 2 s on, for the pages that its new tokens go to; a block has one slot or up to four, and one K/V head or
  * two, by the sizes. */
