@@ -521,12 +521,12 @@ def pack_w4_groups(t):
 # ---------------------------------------------------------------- rotary positions and the paged cache
 def rope_freqs(rot, base=10000.0, factor=1.0, scaling="positions", context=None, turns=(1.0, 32.0), device=None):
     """Frequencies of the rot / 2 pairs, base ** (-2 i / rot) radians a position, as rope_bf16 and kv_append_fp8 take
-    them: (fp32 tensor, magnitude).  For contexts `factor` times as long as those of training:
+    them: (fp32 tensor, on the host unless `device` is given; magnitude).  For contexts `factor` times as long as those of training:
       "positions"  every frequency is divided by factor (arXiv 2306.15595);
       "base"       the base is raised so that the slowest pair turns factor times slower and the fastest as before;
       "parts"      pairs that make fewer than turns[0] turns within `context` positions (those of training) are divided by
-                   factor, those that make more than turns[1] stay, in between both are mixed evenly; q and k grow
-                   by 0.1 ln(factor) + 1 (arXiv 2309.00071)."""
+                   factor, those that make more than turns[1] stay, in between both are mixed in proportion to the number of turns (not to
+                   the pair's index, which gives other frequencies); q and k grow by 0.1 ln(factor) + 1 (arXiv 2309.00071)."""
     import math
 
     import torch
@@ -546,6 +546,11 @@ def rope_freqs(rot, base=10000.0, factor=1.0, scaling="positions", context=None,
     return freqs.to(torch.float32).to(device), magnitude
 
 
+def _together(first, *others):
+    """All on the device of the first one (or in pinned host memory, which the device reads too): a host pointer ends the process."""
+    return all(t is None or t.device == first.device or t.device.type == "cpu" and t.is_pinned() for t in others)
+
+
 def _floats(t):
     import torch
     return t.dtype == torch.float32 and t.dim() == 1 and t.is_contiguous()
@@ -554,11 +559,12 @@ def _floats(t):
 def rope_bf16(x, out, freqs, positions, interleaved=False, inverse=False, magnitude=None):
     """Rotary positions: x, out [total, heads, dim], 16-bit storage tensors that may be views with padded tokens (the first
     heads of a fused projection); out may be x.  The first 2 x len(freqs) dims of each head are turned by positions
-    (int32 [total]) times freqs (fp32, radians): pairs (i, i + len(freqs)), or (2 i, 2 i + 1) with interleaved.  inverse: by the negative
+    (int32 [total]) times freqs (fp32, radians; both on x's device): pairs (i, i + len(freqs)), or (2 i, 2 i + 1) with interleaved.  inverse: by the negative
     angle, the operator's transpose, for gradients.  magnitude: what the turned dims are multiplied with, None for 1."""
     total, heads, dim = x.shape
     assert out.shape == x.shape and _is_bf16(x, out) and _floats(freqs)
     assert _is_int32(positions) and positions.numel() == total
+    assert _together(x, out, freqs, positions), "on different devices"
     args = RopeArgs(x.data_ptr(), out.data_ptr(), freqs.data_ptr(), positions.data_ptr(), total, heads, dim,
                     2 * freqs.numel(), _rows(x, dim), _rows(out, dim),
                     (ROPE_INTERLEAVED if interleaved else 0) | (ROPE_INVERSE if inverse else 0), _scale(magnitude))
@@ -625,6 +631,7 @@ def kv_append_fp8(k, v, cu_seqlens, lens, table, cache, freqs=None, positions=No
     seq_pages, ld_table = _table(table, seqs)
     assert freqs is None or _floats(freqs)
     assert positions is None or (freqs is not None and _is_int32(positions) and positions.numel() == total)
+    assert _together(k, v, cu_seqlens, lens, table, *cache, freqs, positions), "on different devices"
     ptr = lambda t: None if t is None else t.data_ptr()
     args = KvAppendArgs(k.data_ptr(), v.data_ptr(), cu_seqlens.data_ptr(), lens.data_ptr(), table.data_ptr(), ptr(freqs),
                         ptr(positions), *(t.data_ptr() for t in cache), total, seqs, kv_heads, dim, page, pages, seq_pages, ld_table,
@@ -642,6 +649,7 @@ def attn_paged_fp8(q, cache, table, lens, out, scratch=None, scale=None):
     pages, kv_heads, page = _pages(cache, dim)
     seq_pages, ld_table = _table(table, batch)
     assert _is_int32(lens) and lens.numel() == batch
+    assert _together(q, out, *cache, table, lens, scratch), "on different devices"
     size = attn_paged_scratch_bytes(batch, heads, kv_heads, dim, page, seq_pages)
     assert size == 0 if scratch is None else scratch.is_contiguous() and scratch.numel() * scratch.element_size() >= size
     args = AttnPagedArgs(q.data_ptr(), out.data_ptr(), *(t.data_ptr() for t in cache), table.data_ptr(), lens.data_ptr(),
