@@ -403,6 +403,7 @@ def _rows(t, dim=None):
     assert t.stride(-1) == 1 or t.shape[-1] == 1
     row = row if n > 1 else width
     assert row >= width, "rows overlap"
+    assert row < 1 << 32, "rows too far apart"             # (it would wrap)
     return row
 
 
