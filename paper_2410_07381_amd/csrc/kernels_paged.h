@@ -89,16 +89,17 @@ __device__ __forceinline__ int block_exp(uint32_t top) {
   const int e = (int)((top + 0x1FFFFFu) >> 23) - 8;
   return e < 1 ? 1 : e > 254 ? 254 : e;
 }
-// fp64 to fp32 such that rounding the result to fewer than 20 bits is rounding the number itself: cut after 20
-// bits, the last of them set where anything was cut off.  Below 2^-129 that last bit is less than fp32 has, and is lost.  A block's
-// first border between two codes is 2^(e - 137), so what lies below 2^-129 is a zero from e = 8 on; blocks of lower exponents have their
-// keys' codes made once more, from numbers 2^64 times as large.
-constexpr int kTinyExp = 7, kTinyUp = 64;
+// fp64 to fp32 such that rounding the result to a code is rounding the number itself: of the bits behind the first one the four that a code and
+// half a step of it take, and in the twelfth whether anything was cut off.  A block's first border between two codes is 2^(e - 137), 2^-136 or more.
+// Of what lies above it fp32 has the twelfth bit where it is subnormal too, down to 2^-149; what lies below is a zero.  (Cut behind the twentieth
+// it is an instruction less, 32768 tokens 45.8 for 46.1, and the bit is lost below 2^-129, where keys beside a border of the lowest exponents then
+// went to the even code.  Those blocks' codes made once more, behind a branch, made workers up to 60 % slower.)
 __device__ __forceinline__ float cut(double x) {
   const uint64_t b = __builtin_bit_cast(uint64_t, x);
+  const uint32_t hi = (uint32_t)(b >> 32), off = (hi & 0xFFFFu) | (uint32_t)b;
   uint32_t any;                                            // (written out: as an expression it is a comparison and a choice)
-  asm("v_min_u32 %0, 1, %1" : "=v"(any) : "v"((uint32_t)b));
-  return (float)__builtin_bit_cast(double, (uint64_t)((uint32_t)(b >> 32) | any) << 32);
+  asm("v_min_u32 %0, 1, %1" : "=v"(any) : "v"(off));
+  return (float)__builtin_bit_cast(double, (uint64_t)__builtin_amdgcn_perm(hi, any, 0x0706000Cu) << 32);
 }
 // 2^by for by from -127 on, 0 below.
 __device__ __forceinline__ float power_of_two(int by) {
@@ -195,9 +196,8 @@ struct AppendBodyT {
     // Sines and cosines of the lane's pairs, of tokens u0 .. u0 + TOK - 1 of the page.
     extern __shared__ __align__(1024) unsigned char tally_dyn_lds[];
     Turn z[8], *table = reinterpret_cast<Turn *>(tally_dyn_lds) + (FEW ? 0 : wave * (TOK * DIM / 2));
-    int up = 0;                                            // (few tokens: keys are turned 2^up times as large)
     auto make_turns = [&](uint32_t u0) {
-      const double by = (a.magnitude > 0.f ? (double)a.magnitude : 1.0) * (up ? 0x1p64 : 1.0);
+      const double by = a.magnitude > 0.f ? (double)a.magnitude : 1.0;
       if constexpr (FEW) {
         const uint32_t t = u0 + tok;
         int32_t position = base + (int32_t)t;
@@ -322,7 +322,7 @@ struct AppendBodyT {
       const uint32_t t = u0 + tok;
       uint8_t *to_row = b.kp + t * DIM;
       if (live && t >= from && t < to) {
-        const float by = power_of_two(127 - b.ek - (turns ? up : 0));
+        const float by = power_of_two(127 - b.ek);
         const uint32_t p0 = codes4(k[0], k[1], k[2], k[3], by), p1 = codes4(k[4], k[5], k[6], k[7], by);
         const uint32_t q0 = codes4(k[8], k[9], k[10], k[11], by), q1 = codes4(k[12], k[13], k[14], k[15], by);
         const u32x2_nt u = {split ? p0 : __builtin_amdgcn_perm(q0, p0, 0x05010400u), split ? p1 : __builtin_amdgcn_perm(q0, p0, 0x07030602u)};
@@ -377,25 +377,6 @@ struct AppendBodyT {
       }
     };
 
-    // Prompts: new keys of a block of a tiny exponent, once all is stored.  Each lane its own bytes again, a pair at a time: it is hardly
-    // ever done, and is to need no more registers than the way there does.
-    auto store_tiny = [&](uint32_t u0, uint32_t head, int exp) {
-      const uint32_t t = u0 + tok;
-      if (!turns || t < from || t >= to) return;
-      const uint16_t *x = a.k + (uint64_t)(row + (t - from)) * LDK + head * DIM;
-      uint8_t *to_row = a.k_pages + ((((uint64_t)(uint32_t)id * a.kv_heads + head) << shift) + t) * DIM;
-      const float by = power_of_two(127 - exp - kTinyUp);
-#pragma unroll 1
-      for (uint32_t e = 0; e < 8; ++e) {
-        const uint32_t i = one + (split ? e : 2 * e), j = split ? two + e : i + 1;
-        const Turn w = table[tok * (DIM / 2) + e * PIECES + piece];
-        const double p = (double)bf16_lo(x[i]) * 0x1p64, q = (double)bf16_lo(x[j]) * 0x1p64;
-        const int codes = __builtin_amdgcn_cvt_pk_fp8_f32(cut(__builtin_fma(p, w.c, -(q * w.s))) * by, cut(__builtin_fma(q, w.c, p * w.s)) * by, 0, false);
-        to_row[i] = (uint8_t)codes;
-        to_row[j] = (uint8_t)(codes >> 8);
-      }
-    };
-
     __shared__ float s_top[2][2][WAVES];
     // The largest magnitudes over the page's waves.  (A row of 16 lanes has all of theirs, some more than once.)
     auto over_page = [&](float top, uint32_t turn) {
@@ -417,7 +398,6 @@ struct AppendBodyT {
         have = u0;
       }
       grow(b, index, over_page(over_wave(), 0), mine == 0);
-      if (a.rot && b.ek <= kTinyExp) up = kTinyUp, have = ~0u;
       if (have != ~0u) store(have, b, true);
       for (uint32_t u0 = begins; u0 < to && u0 != have; u0 += FEW * TOK) {
         ask(u0, h0);
@@ -432,7 +412,6 @@ struct AppendBodyT {
       const bool live = there && begins < to && begins + kUnit > from, held = there && begins < from;   // new ones in the unit; old ones
       if (live) ask(u0, h0);
       if (live && a.rot) make_turns(u0);
-      uint32_t low = 0;                                    // tiny exponents, four bits for each head
       for (uint32_t i = 0; i < HN && h0 + i < a.kv_heads; ++i) {   // (the same for the whole workgroup)
         uint64_t index = 0;
         Block b{};
@@ -449,11 +428,7 @@ struct AppendBodyT {
         if (!live && !held) continue;
         grow(b, index, top, u0 == 0);
         store(u0, b, live);
-        low |= b.ek <= kTinyExp ? (uint32_t)b.ek << 4 * i : 0u;
       }
-      if (live && a.rot)
-        for (uint32_t head = h0; low; ++head, low >>= 4)
-          if (low & 15) store_tiny(u0, head, (int)(low & 15));
     }
 #endif
   }
