@@ -10,7 +10,7 @@
 //
 // What bounds both is memory, and for small calls one load waiting for another.  Measured (us of a call; what it reads and
 // writes once at the 5.12 TB/s of a copy in brackets; an empty launch is 2.4):
-//   appending, 8 heads of 128: one token 4.7; one for each of 64 sequences 6.2; 24 prompts of 1 to 4096 tokens 25 [16.3]; 32768 tokens 45.7 [39.3];
+//   appending, 8 heads of 128: one token 4.7; one for each of 64 sequences 6.3; 24 prompts of 1 to 4096 tokens 24.1 [16.3]; 32768 tokens 46.0 [39.3];
 //   attention: 4 sequences of up to 512 tokens, 12 heads of 64, 5.8; 16 of up to 3001, 28/4 heads of 128, 12.2 [4.9]; 32 of up to 4096, 32/8,
 //   31.9 [26.3]; 8 of up to 131071 173 to 188 from card to card [210], 6.2 to 5.7 TB/s.
 // FETCH_SIZE and WRITE_SIZE say that either moves what it has to and nothing beside it (append of 32768 tokens 135 MB in and 67 MB out;
@@ -42,16 +42,23 @@ constexpr uint32_t kUnit = 16;                             // tokens side by sid
 // tokens: mostly it is one, and waves for the others would be in its way.  In between, and with more than four pieces to a page
 // (kind 4), a workgroup's four waves take a page's pieces in turn.  Both go through pieces twice where a wave has several.
 //
-// Figures (us, 8 heads of 128).  Sequences x tokens each, kinds 0 / 1: pages of 128, 8 x 1 6.1 / 4.9, 64 x 1 20.1 / 5.4; of 64, 64 x 1 11.5 / 5.4;
-// of 16, 64 x 1 6.4 / 6.2, 64 x 2 7.0 / 8.4, 200 x 2 12.3 / 11.6.  Kinds 0 / 1 / 4: pages of 128, 64 x 2 20.8 / 8.4 / 7.0, 64 x 8 21.3 / 9.8 / 7.1, 200 x 4
-// 59.6 / 12.5 / 14.9; of 64, 64 x 4 12.3 / 8.6 / 6.7, 64 x 8 (kind 0 from here on) 11.6 / 10.8.  127 x 1 and 380 tokens of one sequence, pages of 128:
-// kind 1 46, kind 4 16.
+// Figures (us, 8 heads of 128).  Sequences x tokens each, kinds 0 / 1: pages of 16, 64 x 1 6.4 / 6.2, 64 x 2 7.0 / 8.4, 200 x 2 12.3 / 11.6; of 128,
+// 8 x 1 6.1 / 4.9, 64 x 1 20.1 / 5.4; of 64, 64 x 1 11.5 / 5.4.  Kinds 0 / 1 / 4: pages of 128, 64 x 2 20.4 / 8.5 / 7.0, 64 x 8 21.0 / 9.8 / 7.1, 64 x 15
+// 20.8 / 16.2 / 8.7, 64 x 16 (kind 0 from here on) 20.7 / 16.3 / 8.5, 200 x 4 58.2 / 12.6 / 14.8, 200 x 15 61.5 / 27.7 / 19.1, 400 x 4 119.5 / 20.9 / 27.1; of 64,
+// 64 x 4 12.2 / 8.6 / 6.7, 64 x 8 (kind 0 from here on) 11.4 / 10.8 / 7.3, 200 x 4 28.8 / 13.7 / 14.4, 200 x 8 30.8 / 16.4 / 16.7.  So kind 1 would still be
+// the faster one for hundreds of sequences of up to four tokens, and kind 4 some way beyond its end; the lines are simpler than that.  It
+// is the average that decides: a prompt among single tokens is gone through by one wave a page, or four (pages of 128, 127 x 1 and 380 tokens of one
+// sequence: kind 1 46, kind 4 16).
+//
 // Heads a wave goes through, 1 / 2, one prompt: pages of 16, 7000 tokens 13.5 / 14.2, 8192 14.5 / 12.9, 13504 21.2 / 19.9, 20000 33.4 / 30.0; of 64,
 // 14.7 / 15.7, 15.4 / 13.6, 22.9 / 23.5, 35.6 / 32.9; of 128, 15.5 / 16.6, 17.2 / 16.2, 28.4 / 25.4, 41.7 / 41.5.  2 / 4: pages of 16 and 32, 32768
 // tokens 45.6 / 45.7, 38229 53.5 / 57.3, 54613 73.0 / 76.2, 65536 85.3 / 85.0; of 64, 49.7 / 47.3, 58.3 / 57.9, 78.6 / 78.0, 91.6 / 87.9; of 128, 56.3 / 53.6,
-// 67.2 / 72.0, 91.3 / 94.7, 104.8 / 99.9.  Pages of 16 and 32 never want four, those of 64 and 128 now two and now four,
-// which no size of a call tells beforehand; and with up to four a worker needs 133 to 137 registers, with up to two 120 to 127 (32768 tokens as workers, pages of 64 69.8 and 63.6, of 128
-// 79.1 and 62.1).
+// 67.2 / 72.0, 91.3 / 94.7, 104.8 / 99.9.  Pages of 16 and 32 never want four, those of 64 and 128 now two and now four, which no size of a call
+// tells beforehand; and with up to four a worker needs 133 to 137 registers, with up to two 120 to 127.
+//
+// As workers, 32768 tokens, in the best of the configurations that are tried / as one slice of the whole grid (both from the call to its end, some 13
+// more than a call among others): pages of 16 and 32 68 / 60, of 64 64 / 64, of 128 63 / 71.
+//
 // Tried: 16 tokens of a head of 128 a wave (194 registers, two waves per SIMD; 32768 tokens 47 to 55), the next head's numbers asked for ahead (pages
 // of 128 51 and 48, others the same, registers spilled in workers), a page's id and old bytes asked for earlier (64 tokens 6.4).
 constexpr uint64_t kAppendPieces = 8192;                   // from so many on a wave has two heads
@@ -447,7 +454,10 @@ struct AppendBodyT {
 //
 // 1024 workgroups are what is on the GPU at once (us with 512 / 768 / 1024 / 2048: 32 sequences of up to 4096, 8 K/V heads, 36.6 36.0 34.4 34.6; 8 of up to
 // 131071 223 211 193 195; one of 32768 19.0 20.1 20.2 20.2).  A part has two strips at least (1 / 2 / 4: 16 of up to 3001, 4 K/V heads, 13.5 12.2 12.1; one of
-// 4096, 8 heads, 9.2 9.3 10.4).
+// 4096, 8 heads, 9.2 9.3 10.4).  No more than 256 parts, for one K/V head 256 workgroups (128 / 256 / 512: one of 131071, 8 heads of 128 on one, 18.4 18.6
+// 24.6, 16 of 64 on one, 14.3 13.7 17.4; 4 of up to 65536, 8 on one, 17.7 16.1 17.9): more of them find their part later than they read it sooner.
+// The host knows the table's width and no lengths, so a wide table costs short sequences the second kernel (4 of up to 512 tokens 5.8 with a table for as many,
+// 8.4 with one for 32768; 16 of up to 3001 12.3 and 13.5; 32 of up to 4096 32.1 and 32.1).
 // One part a sequence saves the second kernel.  It pays up to 4 strips whatever the number of workgroups (4 sequences of 512, 12 heads of 64:
 // 5.8, in two parts 8.2; one of 1024, 8 heads, 9.9 and 9.2), up to 8 from 256 workgroups on (8 of 600, 32 heads, 10.8 and 12.1; with 64 of them,
 // 8 of 1024, 8 heads, 10.0 and 9.4), up to 16 from 512 on (64 of up to 2000, 8 heads, 32.8 and 34.9; with 128, 128 of 2000 on one head of 64,

@@ -53,7 +53,11 @@ constexpr uint64_t kInfinityCache = 256ull << 20;          // bytes
 constexpr uint32_t kRopeTable = 2048;                      // pairs of a workgroup's tokens
 constexpr uint32_t kRopeItems = 1024;                      // pieces of 16 dims that a workgroup should have
 
-// Tokens of a logical block: enough for four pieces per thread, while there are four workgroups per compute unit.
+// Tokens of a logical block: enough for four pieces per thread, while there are four workgroups per compute unit.  (us, a token a block / by
+// this rule: 65536 tokens, one head of 64, 45.7 / 8.8; 32768, two of 64, 23.0 / 6.7; 32768, 8 of 128, 37.8 / 28.0; 4097, 8 of 64, 4.4 / 3.6; eight tokens at
+// most / 32: 65536, one of 64, 12.0 / 8.8.  512 / 1024 / 2048 pieces: 32768, 8 of 128, 26.5 / 28.0 / 30.2; 13504, 40 of 128, 47.6 / 51.9 / 55.4, and 44.7 with a
+// token a block: wide rows would gain from fewer; heads of 64 do not mind.  512 / 1024 / 2048 workgroups: 3000, 8 of 64, 3.4 / 3.5 / 4.2; 2048, 40 of 128,
+// 8.5 / 7.9 / 7.9.)  As workers, 13504 tokens, 40 heads, 69, as one slice of the whole grid 67; 4097 35 and 32.
 __host__ __device__ inline uint32_t rope_tokens(const tally_rope_args &a) {
   uint32_t g = 1;
   while (g < 32 && (uint64_t)g * a.heads * (a.dim / 16) < kRopeItems && a.total / (2 * g) >= 1024 && g * a.rot <= kRopeTable) g *= 2;
