@@ -285,3 +285,77 @@ def test_attention_stays_within_its_scratch(env, lens, heads, kv, dim, page, mor
     _run(ctx, torch, B.attn_paged_fp8(_amid(torch, q, 0x7FC0)[0], paged, _amid(torch, table, 0)[0], _dev(torch, np.array(lens, np.int32)), out, scratch), "hi")
     _attn_ok(_host(out), *OP.attn_paged(obf16.decode(q), cache, table, lens))
     assert _beside_is(whole, 0x5A) and _beside_is(whole_out, SENTINEL)
+
+
+@pytest.mark.parametrize("heads,kv,dim,page,width", [(4, 1, 64, 16, 4000), (16, 8, 128, 64, 700), (6, 2, 128, 32, 2000)])
+def test_a_captured_call_as_lengths_change(env, heads, kv, dim, page, width):
+    """A graph of an append and the attention behind it, captured once with a table for the longest, replayed as the lengths on the device go from
+    nothing to all of it and back: in as many parts as there are then, merged by a wave or a workgroup a row, with eager calls between."""
+    B, ctx, torch = env
+    rng = np.random.default_rng(width)
+    batch, new = 3, 2
+    table, pages = _deal(rng, [width] * batch, page)
+    cache = _filled(rng, pages, kv, page, dim)
+    paged, tt = _paged(B, torch, cache), _dev(torch, table)
+    x, q = _bits(rng, (batch * new, 2 * kv, dim)), _bits(rng, (batch, heads, dim))
+    tx, tq, cu = _dev(torch, x), _dev(torch, q), _dev(torch, (np.arange(batch + 1) * new).astype(np.int32))
+    lens = torch.zeros(batch, dtype=torch.int32, device="cuda")
+    out = torch.zeros((batch, heads, dim), dtype=torch.int16, device="cuda")
+    scratch = torch.full((B.attn_paged_scratch_bytes(batch, heads, kv, dim, page, table.shape[1]),), 0xFF, dtype=torch.uint8, device="cuda")
+    assert scratch.numel() > 0
+    kernels = [B.kv_append_fp8(tx[:, :kv], tx[:, kv:], cu, lens, tt, paged), B.attn_paged_fp8(tq, paged, tt, lens, out, scratch)]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=ctx._streams[0]):
+        for kern in kernels:
+            ctx.launch_native(kern, hi=True)
+    # (an append of two tokens counts as the last two: with fewer the first ones have no place)
+    for now in ([0, 0, 0], [1, 0, 2], [130, width, 7], [width, width, width], [width // 2, 300, 129], [2, 0, width - 1], [width, 1, 0]):
+        lens.copy_(_dev(torch, np.array(now, np.int32)))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        cache = OP.append(obf16.decode(x[:, :kv]), obf16.decode(x[:, kv:]), np.arange(batch + 1) * new, now, table, cache)
+        _same(paged, cache, str(now))
+        got = _host(out).copy()
+        _attn_ok(got, *OP.attn_paged(obf16.decode(q), cache, table, now))
+        out.fill_(0)
+        scratch.fill_(0xFF)
+        _run(ctx, torch, kernels[1], "be")
+        assert (_host(out) == got).all()
+
+
+def test_two_calls_at_once(env):
+    """On both streams together, a scratch each: appends to different sequences of one cache, and attention over it."""
+    B, ctx, torch = env
+    rng = np.random.default_rng(31)
+    heads, kv, dim, page, n = 16, 4, 128, 32, 3000
+    table, pages = _deal(rng, [n, n], page)
+    cache = _filled(rng, pages, kv, page, dim)
+    paged = _paged(B, torch, cache)
+    x, q = [_bits(rng, (n, 2 * kv, dim)) for _ in range(2)], _bits(rng, (2, heads, dim))
+    cu, tq = _dev(torch, np.array([0, n], np.int32)), _dev(torch, q)
+    tl, tt = _dev(torch, np.array([n, n], np.int32)), _dev(torch, table)
+    out = torch.zeros((2, heads, dim), dtype=torch.int16, device="cuda")
+    size = B.attn_paged_scratch_bytes(1, heads, kv, dim, page, table.shape[1])
+    assert size > 0
+    appends, attends = [], []
+    for i in range(2):
+        tx = _dev(torch, x[i])
+        appends.append(B.kv_append_fp8(tx[:, :kv], tx[:, kv:], cu, tl[i:i + 1], tt[i:i + 1], paged))
+        attends.append(B.attn_paged_fp8(tq[i:i + 1], paged, tt[i:i + 1], tl[i:i + 1], out[i:i + 1], torch.zeros(size, dtype=torch.uint8, device="cuda")))
+        cache = OP.append(obf16.decode(x[i][:, :kv]), obf16.decode(x[i][:, kv:]), [0, n], [n], table[i:i + 1], cache)
+    want, mass = OP.attn_paged(obf16.decode(q), cache, table, [n, n])
+    first = None
+    for _ in range(20):
+        out.fill_(0)
+        torch.cuda.synchronize()
+        for both in (appends, attends):
+            for i in range(2):
+                ctx.launch_native(both[i], hi=i == 0)
+        torch.cuda.synchronize()
+        got = _host(out).copy()
+        first = got if first is None else first
+        assert (got == first).all()
+    _same(paged, cache)
+    _attn_ok(first, want, mass)
